@@ -38,10 +38,16 @@ EXPORTED = ("dsa3d_forward", "dsa3d_backward", "dsa3d_backward_timed", "dsa3d_ba
             "dsa3d_dwconv3d_forward", "dsa3d_dwconv3d_backward_workspace_size",
             "dsa3d_dwconv3d_backward", "dsa3d_pw_forward", "dsa3d_pw_backward_workspace_size",
             "dsa3d_pw_backward", "dsa3d_win_forward", "dsa3d_win_backward_workspace_size",
-            "dsa3d_win_backward")
+            "dsa3d_win_backward", "dsa3d_seq_forward", "dsa3d_seq_backward_workspace_size",
+            "dsa3d_seq_backward", "dsa3d_relative_buckets", "dsa3d_paged_append",
+            "dsa3d_paged_forward_workspace_size", "dsa3d_paged_forward")
 
 DSA3D_WIN_MAX_TOKENS = 65536
 DSA3D_WIN_BACKWARD_PHASES = 2
+
+DSA3D_SEQ_MAX_SPAN = 2048
+DSA3D_SEQ_MAX_BUCKETS = 256
+DSA3D_PAGED_MAX_BIAS = 6144
 
 
 class dsa3d_desc(ctypes.Structure):
@@ -63,6 +69,29 @@ class dsa3d_win_desc(ctypes.Structure):
                 ("wt", ctypes.c_int32), ("wh", ctypes.c_int32), ("ww", ctypes.c_int32),
                 ("st", ctypes.c_int32), ("sh", ctypes.c_int32), ("sw", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int32)]
+
+
+class dsa3d_seq_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("total_q", ctypes.c_int32),
+                ("total_k", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("causal", ctypes.c_int32), ("rel_min", ctypes.c_int32),
+                ("rel_span", ctypes.c_int32), ("rel_buckets", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("dtype", ctypes.c_int32),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64)]
+
+
+class dsa3d_paged_desc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("total_q", ctypes.c_int32),
+                ("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("max_kv", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("rel_min", ctypes.c_int32), ("rel_span", ctypes.c_int32),
+                ("rel_buckets", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dtype", ctypes.c_int32), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 class Dsa3dError(RuntimeError):
@@ -116,6 +145,21 @@ def load():
         lib.dsa3d_win_backward.argtypes = [wd, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                            ctypes.c_size_t, vp, ctypes.POINTER(vp)]
         lib.dsa3d_win_backward.restype = ctypes.c_int
+        sd, gd = ctypes.POINTER(dsa3d_seq_desc), ctypes.POINTER(dsa3d_paged_desc)
+        lib.dsa3d_seq_forward.argtypes = [sd] + [vp] * 11
+        lib.dsa3d_seq_forward.restype = ctypes.c_int
+        lib.dsa3d_seq_backward_workspace_size.argtypes = [sd]
+        lib.dsa3d_seq_backward_workspace_size.restype = ctypes.c_size_t
+        lib.dsa3d_seq_backward.argtypes = [sd] + [vp] * 16 + [ctypes.c_size_t, vp]
+        lib.dsa3d_seq_backward.restype = ctypes.c_int
+        lib.dsa3d_relative_buckets.argtypes = [ctypes.c_int32] * 3 + [vp] * 3
+        lib.dsa3d_relative_buckets.restype = ctypes.c_int
+        lib.dsa3d_paged_append.argtypes = [gd] + [vp] * 8
+        lib.dsa3d_paged_append.restype = ctypes.c_int
+        lib.dsa3d_paged_forward_workspace_size.argtypes = [gd]
+        lib.dsa3d_paged_forward_workspace_size.restype = ctypes.c_size_t
+        lib.dsa3d_paged_forward.argtypes = [gd] + [vp] * 11 + [ctypes.c_size_t, vp]
+        lib.dsa3d_paged_forward.restype = ctypes.c_int
         lib.dsa3d_backward_workspace_size.argtypes = [pd]
         lib.dsa3d_backward_workspace_size.restype = ctypes.c_size_t
         lib.dsa3d_status_string.argtypes = [ctypes.c_int]
@@ -302,6 +346,93 @@ def dsa3d_win_backward(desc, q, k, v, out, out_res, lse, dout, dq, dk, dv, works
                                    _event_array(events, DSA3D_WIN_BACKWARD_PHASES))
     if check and st != DSA3D_OK:
         raise Dsa3dError(st, "dsa3d_win_backward")
+    return st
+
+
+def make_seq_desc(batch, total_q, total_k, heads, kv_heads, head_dim, causal=False, dtype="bf16",
+                  scale=0.0, rel_min=0, rel_span=0, rel_buckets=0, q_stride=0, k_stride=0,
+                  v_stride=0) -> dsa3d_seq_desc:
+    return dsa3d_seq_desc(batch, total_q, total_k, heads, kv_heads, head_dim, int(bool(causal)),
+                          rel_min, rel_span, rel_buckets, float(scale),
+                          DSA3D_BF16 if dtype == "bf16" else DSA3D_F32, q_stride, k_stride,
+                          v_stride)
+
+
+def dsa3d_seq_forward(desc, q, k, v, cu_q, cu_k, bias_table, bias_map, out, out_res=None, lse=None,
+                      stream=None, check=True) -> int:
+    st = load().dsa3d_seq_forward(ctypes.byref(desc) if desc is not None else None, _ptr(q),
+                                  _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(bias_table),
+                                  _ptr(bias_map), _ptr(out), _ptr(out_res), _ptr(lse),
+                                  _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_seq_forward")
+    return st
+
+
+def dsa3d_seq_backward_workspace_size(desc) -> int:
+    return load().dsa3d_seq_backward_workspace_size(ctypes.byref(desc))
+
+
+def dsa3d_seq_backward(desc, q, k, v, cu_q, cu_k, bias_table, bias_map, out, out_res, lse, dout,
+                       dq, dk, dv, d_table=None, workspace=None, workspace_bytes=0, stream=None,
+                       check=True) -> int:
+    st = load().dsa3d_seq_backward(ctypes.byref(desc) if desc is not None else None, _ptr(q),
+                                   _ptr(k), _ptr(v), _ptr(cu_q), _ptr(cu_k), _ptr(bias_table),
+                                   _ptr(bias_map), _ptr(out), _ptr(out_res), _ptr(lse),
+                                   _ptr(dout), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(d_table),
+                                   _ptr(workspace), workspace_bytes, _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_seq_backward")
+    return st
+
+
+def dsa3d_relative_buckets(buckets, max_distance, both, check=True):
+    """Returns (map, rel_min), the map as a list (None when the call is refused unchecked)."""
+    lo, span = ctypes.c_int32(), ctypes.c_int32()
+    call = load().dsa3d_relative_buckets
+    st = call(buckets, max_distance, int(bool(both)), None, ctypes.byref(lo), ctypes.byref(span))
+    if st != DSA3D_OK:
+        if check:
+            raise Dsa3dError(st, "dsa3d_relative_buckets")
+        return None, st
+    arr = (ctypes.c_int32 * span.value)()
+    call(buckets, max_distance, int(bool(both)), arr, ctypes.byref(lo), ctypes.byref(span))
+    return list(arr), lo.value
+
+
+def make_paged_desc(batch, total_q, heads, kv_heads, head_dim, num_pages, page_size, max_pages,
+                    max_kv=0, causal=True, dtype="bf16", scale=0.0, rel_min=0, rel_span=0,
+                    rel_buckets=0, q_stride=0, k_stride=0, v_stride=0) -> dsa3d_paged_desc:
+    return dsa3d_paged_desc(batch, total_q, heads, kv_heads, head_dim, num_pages, page_size,
+                            max_pages, max_kv, int(bool(causal)), rel_min, rel_span, rel_buckets,
+                            float(scale), DSA3D_BF16 if dtype == "bf16" else DSA3D_F32, q_stride,
+                            k_stride, v_stride)
+
+
+def dsa3d_paged_append(desc, k, v, cu_q, kv_lens, pages, k_pages, v_pages, stream=None,
+                       check=True) -> int:
+    st = load().dsa3d_paged_append(ctypes.byref(desc) if desc is not None else None, _ptr(k),
+                                   _ptr(v), _ptr(cu_q), _ptr(kv_lens), _ptr(pages),
+                                   _ptr(k_pages), _ptr(v_pages), _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_paged_append")
+    return st
+
+
+def dsa3d_paged_forward_workspace_size(desc) -> int:
+    return load().dsa3d_paged_forward_workspace_size(ctypes.byref(desc))
+
+
+def dsa3d_paged_forward(desc, q, k_pages, v_pages, pages, kv_lens, cu_q, bias_table, bias_map, out,
+                        lse=None, workspace=None, workspace_bytes=0, stream=None,
+                        check=True) -> int:
+    st = load().dsa3d_paged_forward(ctypes.byref(desc) if desc is not None else None, _ptr(q),
+                                    _ptr(k_pages), _ptr(v_pages), _ptr(pages), _ptr(kv_lens),
+                                    _ptr(cu_q), _ptr(bias_table), _ptr(bias_map), _ptr(out),
+                                    _ptr(lse), _ptr(workspace), workspace_bytes,
+                                    _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_paged_forward")
     return st
 
 

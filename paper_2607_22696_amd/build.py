@@ -15,7 +15,8 @@ SOURCES = [os.path.join(CSRC, "dsa3d_forward.hip"), os.path.join(CSRC, "dsa3d_ba
            os.path.join(CSRC, "dsa3d_noalloc.hip"),
            os.path.join(CSRC, "dwconv3d.hip"), os.path.join(CSRC, "dsa3d_api.cpp"),
            os.path.join(CSRC, "dwconv3d_api.cpp"), os.path.join(CSRC, "winattn.hip"),
-           os.path.join(CSRC, "winattn_api.cpp")]
+           os.path.join(CSRC, "winattn_api.cpp"), os.path.join(CSRC, "seqattn.hip"),
+           os.path.join(CSRC, "paged.hip"), os.path.join(CSRC, "seq_api.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

@@ -1,0 +1,331 @@
+// Device code shared by the sequence kernels (seqattn.hip, paged.hip): operand tiles in LDS, the
+// matrix products, and the way from a block to its sequence.
+//
+// Products are those of winattn.hip: 32 x 32 blocks with the transposed result (S^T = K Q^T,
+// O^T = V^T P^T), so that a lane owns one query's (or key's) column.  Operand fragments are the
+// same for both storage types: lane l holds row (or column) l % 32 and the 8 consecutive
+// contraction indices 8 (l / 32) .. +7 of a step of 16.  bf16 multiplies them with one
+// v_mfma_f32_32x32x16_bf16; float32 with eight v_mfma_f32_32x32x2_f32, the e-th taking element e
+// of both halves of the wave, which sums the same 16 products in float32.  The result's lane l
+// holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in its element i, for both.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "seq_internal.h"
+
+namespace dsa3d {
+namespace seq {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+struct F32x8 {
+  float x[8];
+};
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kSlack = 8.0f;    // base-2 headroom of a running maximum
+constexpr float kHidden = -1e30f; // bias values at or below this hide a key
+
+template <typename T>
+struct Type;
+template <>
+struct Type<uint16_t> {  // bf16 bit patterns
+  using Frag = bf16x8_t;
+  static constexpr int kKeyTile = 64;
+};
+template <>
+struct Type<float> {
+  using Frag = F32x8;
+  static constexpr int kKeyTile = 32;
+};
+
+__device__ inline f32x16_t mfma(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16_t mfma(const F32x8& a, const F32x8& b, f32x16_t c) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[e], b.x[e], c, 0, 0, 0);
+  return c;
+}
+
+__device__ inline bf16x8_t as_bf16x8(const uint4& u) { return __builtin_bit_cast(bf16x8_t, u); }
+
+__device__ inline uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
+__device__ inline float from_bf16(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+
+// x combined with the value of lane l ^ 32 (v_permlane32_swap: no LDS traffic).
+__device__ inline float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ inline float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Row of a 32-row block that element i of a result holds in this half of the wave.
+__device__ inline int c_row(int i, int hh) { return 8 * (i / 4) + 4 * hh + (i % 4); }
+
+// A tile of ROWS rows x D channels in LDS, rows unpadded, the 16-byte chunks of a row XOR-permuted
+// by a function of the row so that both operand reads are free of bank conflicts.  bf16: as
+// winattn.hip's tiles (16-byte reads of one chunk of 16 consecutive rows, and the transposing
+// 8-byte reads of 4 rows x 64 bytes).  float32: chunk ^ (row % 16), for which 16 consecutive rows'
+// reads of one chunk touch all 64 banks, and a 4-byte read of 32 consecutive channels of one row
+// touches 32 different ones.
+template <typename T, int D, int ROWS, int THREADS = 256>
+struct Tile {
+  static constexpr bool kBf16 = sizeof(T) == 2;
+  static constexpr int CH = 16 / sizeof(T);         // elements per 16-byte chunk
+  static constexpr int KCH = D / CH;                // chunks per row
+  static constexpr int NL = ROWS * KCH / THREADS;   // chunks per thread
+  static constexpr int kStep = THREADS / KCH;       // rows between a thread's chunks
+  static constexpr int kElems = ROWS * D;
+  using Frag = typename Type<T>::Frag;
+  static_assert(D == 64 || D == 128, "head_dim 64 or 128");
+  static_assert(NL * THREADS == ROWS * KCH, "the threads share a tile evenly");
+
+  static __device__ inline int at(int row, int chan) {
+    if constexpr (kBf16) {
+      const int f = D == 128 ? 4 * (row & 3) + ((row >> 2) & 3)
+                             : 4 * ((row >> 1) & 1) + ((row >> 2) & 3);
+      return row * D + (((chan >> 3) ^ f) << 3) + (chan & 7);
+    } else {
+      return row * D + (((chan >> 2) ^ (row & 15)) << 2) + (chan & 3);
+    }
+  }
+
+  static __device__ inline int row_of_thread(int i) { return (int)threadIdx.x / KCH + i * kStep; }
+  static __device__ inline int chan_of_thread() { return ((int)threadIdx.x % KCH) * CH; }
+
+  // Rows 0 .. ROWS - 1 at src + row * stride; rows from `valid` on read as zero (their loads go to
+  // the last valid row, so that no branch is needed).  valid >= 1.
+  static __device__ inline void load(uint4 (&r)[NL], const T* src, int64_t stride, int valid) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = min(row_of_thread(i), valid - 1);
+      r[i] = *reinterpret_cast<const uint4*>(src + row * stride + chan_of_thread());
+    }
+    if (valid < ROWS) {
+#pragma unroll
+      for (int i = 0; i < NL; ++i)
+        if (row_of_thread(i) >= valid) r[i] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  // Tile rows through a table of tensor rows (negative: no such row, reads as zero).
+  static __device__ inline void load(uint4 (&r)[NL], const T* src, int64_t stride,
+                                     const int* tab) {
+    int row[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) row[i] = tab[row_of_thread(i)];
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      r[i] = *reinterpret_cast<const uint4*>(src + (int64_t)max(row[i], 0) * stride +
+                                             chan_of_thread());
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      if (row[i] < 0) r[i] = make_uint4(0, 0, 0, 0);
+  }
+  static __device__ inline void store(T* lds, const uint4 (&r)[NL]) {
+#pragma unroll
+    for (int i = 0; i < NL; ++i)
+      *reinterpret_cast<uint4*>(lds + at(row_of_thread(i), chan_of_thread())) = r[i];
+  }
+
+  // Operand with tile rows as its rows: row r0 + l % 32, channels 16 ks + 8 (l / 32) .. +7.
+  static __device__ inline Frag a_rows(const T* lds, int r0, int ks) {
+    const int lane = threadIdx.x & 63, row = r0 + (lane & 31), c = ks * 16 + (lane >> 5) * 8;
+    if constexpr (kBf16) {
+      return as_bf16x8(*reinterpret_cast<const uint4*>(lds + at(row, c)));
+    } else {
+      F32x8 f;
+      *reinterpret_cast<float4*>(f.x) = *reinterpret_cast<const float4*>(lds + at(row, c));
+      *reinterpret_cast<float4*>(f.x + 4) = *reinterpret_cast<const float4*>(lds + at(row, c + 4));
+      return f;
+    }
+  }
+  // Operand with channels as its rows: channel d0 + l % 32; tile rows 32 kb + 16 p + 4 (l / 32) +
+  // {0..3, 8..11}, the order in which a result's elements 8 p .. 8 p + 7 hold them.  bf16 by
+  // ds_read_b64_tr_b16 as in winattn.hip.
+  static __device__ inline Frag a_cols(const T* lds, int d0, int kb, int p) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (kBf16) {
+      typedef short s4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s4_t lds_s4_t;
+      const int j = lane & 15;
+      const int row = kb * 32 + 16 * p + 4 * (lane >> 5) + (j >> 2);
+      const int chan = d0 + 16 * ((lane >> 4) & 1) + 4 * (j & 3);
+      const s4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + at(row, chan)));
+      const s4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + at(row + 8, chan)));
+      const uint2 ul = __builtin_bit_cast(uint2, lo), uh = __builtin_bit_cast(uint2, hi);
+      return as_bf16x8(make_uint4(ul.x, ul.y, uh.x, uh.y));
+    } else {
+      F32x8 f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f.x[e] = lds[at(kb * 32 + 16 * p + 8 * (e / 4) + 4 * (lane >> 5) + (e % 4),
+                        d0 + (lane & 31))];
+      return f;
+    }
+  }
+};
+
+// This lane's row as the other operand: channels 16 ks + 8 (l / 32) .. +7, zero where !ok.
+template <typename T, int D>
+__device__ inline void load_frag(typename Type<T>::Frag (&f)[D / 16], const T* row, bool ok) {
+  const int hh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int ks = 0; ks < D / 16; ++ks) {
+    if constexpr (sizeof(T) == 2) {
+      uint4 u = make_uint4(0, 0, 0, 0);
+      if (ok) u = *reinterpret_cast<const uint4*>(row + ks * 16 + hh * 8);
+      f[ks] = as_bf16x8(u);
+    } else {
+      float4 a = make_float4(0, 0, 0, 0), b = a;
+      if (ok) {
+        a = *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8);
+        b = *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8 + 4);
+      }
+      *reinterpret_cast<float4*>(f[ks].x) = a;
+      *reinterpret_cast<float4*>(f[ks].x + 4) = b;
+    }
+  }
+}
+
+__device__ inline float frag_at(const bf16x8_t& f, int e) { return (float)f[e]; }
+__device__ inline float frag_at(const F32x8& f, int e) { return f.x[e]; }
+
+// Sixteen result values as fragments (elements 8 p .. 8 p + 7) of the next product, rounded to
+// the nearest bf16, or as they are.
+__device__ inline void to_frags(const float (&x)[16], bf16x8_t (&f)[2]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[p][e] = (__bf16)x[8 * p + e];
+}
+__device__ inline void to_frags(const float (&x)[16], F32x8 (&f)[2]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[p].x[e] = x[8 * p + e];
+}
+// x - bf16(x), exact in float32, rounded once: hi + lo carry x to within 2^-17 |x|.
+__device__ inline void to_low_frags(const float (&x)[16], const bf16x8_t (&hi)[2],
+                                    bf16x8_t (&lo)[2]) {
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) lo[p][e] = (__bf16)(x[8 * p + e] - (float)hi[p][e]);
+}
+
+// Stores 16 values of channel block db (channels 32 db + 8 blk + 4 (l / 32) + j) times mul.
+__device__ inline void store_block(float* row, int db, const f32x16_t& acc, float mul) {
+  const int hh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int blk = 0; blk < 4; ++blk)
+    *reinterpret_cast<float4*>(row + db * 32 + 8 * blk + 4 * hh) =
+        make_float4(acc[4 * blk] * mul, acc[4 * blk + 1] * mul, acc[4 * blk + 2] * mul,
+                    acc[4 * blk + 3] * mul);
+}
+__device__ inline void store_block(uint16_t* row, int db, const f32x16_t& acc, float mul) {
+  const int hh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int blk = 0; blk < 4; ++blk) {
+    __bf16 h[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = (__bf16)(acc[4 * blk + j] * mul);
+    *reinterpret_cast<uint2*>(row + db * 32 + 8 * blk + 4 * hh) = __builtin_bit_cast(uint2, h);
+  }
+}
+
+// ------------------------------------------------------------------- from blocks to sequences
+
+// Rows of the sequence that holds tile `slot`.  Tiles have TILE rows (one row per token and
+// `per` of them); sequence b's tiles are numbered from cu[b] per / TILE + b, which leaves room
+// for them all without knowing the lengths on the host: floor(x + n) - floor(x) + 1 >= ceil(n).
+// b = B stands for the rows behind the last sequence.
+struct Slot {
+  int b, begin, end, tile;  // rows begin .. end - 1 (tokens), tile number within the sequence
+};
+
+__device__ inline int cu_at(const int32_t* cu, int b, int total) {
+  return b == 0 ? 0 : min(max(cu[b], 0), total);
+}
+
+// Largest b in 0 .. B with first(b) <= x, by 64-fold search: each lane looks at one candidate.
+// Ends for any data; uniform over the wave.
+template <typename First>
+__device__ inline int search(int B, int x, const First& first) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = B + 1;
+  while (n > 1) {
+    const int step = (n + 63) / 64, idx = lane * step;
+    const bool ok = idx < n && first(lo + min(idx, n - 1)) <= x;
+    const int cnt = max(__popcll(__ballot(ok)), 1);
+    lo += (cnt - 1) * step;
+    n = min(step, n - (cnt - 1) * step);
+  }
+  return __builtin_amdgcn_readfirstlane(lo);
+}
+
+template <int TILE>
+__device__ inline Slot find_slot(const int32_t* cu, int B, int total, int per, int slot) {
+  const auto first = [&](int b) { return cu_at(cu, b, total) * per / TILE + b; };
+  Slot s;
+  s.b = search(B, slot, first);
+  s.begin = __builtin_amdgcn_readfirstlane(cu_at(cu, s.b, total));
+  s.end = s.b < B ? __builtin_amdgcn_readfirstlane(max(cu_at(cu, s.b + 1, total), s.begin))
+                  : total;
+  s.tile = slot - (s.begin * per / TILE + s.b);
+  if (s.tile < 0) {  // only where cu decreases: no rows
+    s.tile = 0;
+    s.end = s.begin;
+  }
+  return s;
+}
+
+// Keys of sequence b (none for the rows behind the last one).
+__device__ inline void key_rows(const int32_t* cu, int b, int B, int total, int& begin, int& n) {
+  begin = n = 0;
+  if (b >= B) return;
+  begin = __builtin_amdgcn_readfirstlane(cu_at(cu, b, total));
+  n = __builtin_amdgcn_readfirstlane(max(cu_at(cu, b + 1, total) - begin, 0));
+}
+
+// The bias by distance of one head, in base-2 units: -inf where it hides, 0 where it has no
+// bucket.
+__device__ inline float bias_of(const float* table, const int32_t* map, int heads, int buckets,
+                                int head, int idx) {
+  const int c = map[idx];
+  if (c < 0 || c >= buckets) return 0.0f;
+  const float x = table[(int64_t)c * heads + head];
+  return x <= kHidden ? -INFINITY : x * kLog2e;
+}
+
+// Block -> (key head, slot, head within the group).  Blocks go to XCD x % 8, so the blocks of a
+// key head stay on one XCD, whose L2 then serves its keys and values; with key heads that the 8
+// XCDs do not share evenly, each head's tiles are dealt out over `parts` of them, so that early
+// and late tiles (short and long ones under a causal mask) fall on each.  Late tiles come first.
+struct Work {
+  int u, slot, head;
+};
+__device__ inline bool work_of(const Spread& sp, int per, Work& w) {
+  const int x = blockIdx.x % 8;
+  int r = blockIdx.x / 8;
+  const int j = r % per;
+  r /= per;
+  const int su = (r % sp.local) * 8 + x;
+  const int rank = sp.ranks - 1 - r / sp.local;
+  w.u = su % sp.units;
+  w.slot = rank * sp.parts + su / sp.units;
+  w.head = w.u * per + j;
+  return w.slot < sp.slots;
+}
+
+}  // namespace seq
+}  // namespace dsa3d

@@ -13,10 +13,12 @@ import torch
 
 from ._binding import (dsa3d_backward, dsa3d_backward_timed, dsa3d_backward_workspace_size,
                        dsa3d_dwconv3d_backward, dsa3d_dwconv3d_backward_workspace_size,
-                       dsa3d_dwconv3d_forward, dsa3d_forward, dsa3d_pw_backward,
-                       dsa3d_pw_backward_workspace_size, dsa3d_pw_forward, dsa3d_win_backward,
-                       dsa3d_win_backward_workspace_size, dsa3d_win_forward, make_conv_desc,
-                       make_desc, make_win_desc)
+                       dsa3d_dwconv3d_forward, dsa3d_forward, dsa3d_paged_append,
+                       dsa3d_paged_forward, dsa3d_paged_forward_workspace_size, dsa3d_pw_backward,
+                       dsa3d_pw_backward_workspace_size, dsa3d_pw_forward, dsa3d_relative_buckets,
+                       dsa3d_seq_backward, dsa3d_seq_backward_workspace_size, dsa3d_seq_forward,
+                       dsa3d_win_backward, dsa3d_win_backward_workspace_size, dsa3d_win_forward,
+                       make_conv_desc, make_desc, make_paged_desc, make_seq_desc, make_win_desc)
 
 _IO_DTYPES = {torch.bfloat16: "bf16", torch.float32: "f32"}
 
@@ -333,3 +335,279 @@ def win_backward(q, k, v, out, out_res, lse, dout, window=(3, 16, 16), shift=(0,
     dsa3d_win_backward(desc, q, k, v, out, out_res, lse, dout, dq, dk, dv, workspace, need,
                        events=phase_events)
     return dq, dk, dv
+
+
+# ----------------------------------------------------------------------------- packed sequences
+
+def _rows(chk, name, t, heads, head_dim, dtype, device, rows=None):
+    """Checks a packed [rows, heads, head_dim] tensor whose rows may lie any distance apart (a
+    slice of a fused projection) and returns that distance in elements, 0 for none between."""
+    if not isinstance(t, torch.Tensor):
+        chk.problems.append(f"{name}: expected a tensor, got {type(t).__name__}")
+        return 0
+    shape = t.shape
+    if t.dim() != 3 or shape[1] != heads or shape[2] != head_dim or \
+            (rows is not None and shape[0] != rows) or t.dtype != dtype or t.device != device:
+        want = ("rows" if rows is None else rows, heads, head_dim)
+        chk.problems.append(f"{name}: expected {dtype} [{want[0]}, {want[1]}, {want[2]}] on "
+                            f"{device}, got {t.dtype} {tuple(shape)} on {t.device}")
+        return 0
+    if t.is_contiguous():
+        return 0
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+        chk.problems.append(f"{name}: heads and channels of a row must be contiguous")
+        return 0
+    return t.stride(0) if shape[0] > 1 else 0
+
+
+def _ints(chk, name, t, shape, device):
+    chk.tensor(name, t, shape, torch.int32, device)
+
+
+def _cu(chk, name, t, device):
+    """Checks a cu_seqlens tensor and returns the number of sequences."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.numel() < 2:
+        chk.problems.append(f"{name}: expected an int32 tensor of sequences + 1 row offsets")
+        chk.done()
+    _ints(chk, name, t, (t.numel(),), device)
+    return t.numel() - 1
+
+
+def _relative(chk, rel_table, rel_buckets, rel_min, heads, device):
+    """Checks the bias arguments; returns (rel_min, rel_span, rel_buckets) of the descriptor."""
+    if rel_table is None:
+        if rel_buckets is not None:
+            chk.problems.append("rel_buckets: given without rel_table")
+        return 0, 0, 0
+    if not isinstance(rel_table, torch.Tensor) or rel_table.dim() != 2:
+        chk.problems.append("rel_table: expected a float32 [buckets, heads] tensor")
+        chk.done()
+    chk.tensor("rel_table", rel_table, (rel_table.shape[0], heads), torch.float32, device)
+    if not isinstance(rel_buckets, torch.Tensor) or rel_buckets.dim() != 1:
+        chk.problems.append("rel_buckets: expected an int32 tensor, one bucket per distance")
+        chk.done()
+    _ints(chk, "rel_buckets", rel_buckets, tuple(rel_buckets.shape), device)
+    if rel_table.shape[0] < 1 or rel_buckets.numel() < 1:
+        chk.problems.append("rel_table, rel_buckets: empty")
+    return int(rel_min), rel_buckets.numel(), rel_table.shape[0]
+
+
+def _lead_rows(chk, q):
+    """The tensor that fixes type, heads and device of a call on packed rows."""
+    if not isinstance(q, torch.Tensor):
+        chk.problems.append(f"q: expected a tensor, got {type(q).__name__}")
+        chk.done()
+    if q.dim() != 3:
+        chk.problems.append(f"q: expected [rows, heads, head_dim], got shape {tuple(q.shape)}")
+    if q.dtype not in _IO_DTYPES:
+        chk.problems.append(f"q: unsupported dtype {q.dtype}")
+    chk.done()
+    if not q.is_cuda:
+        chk.problems.append(f"q: not a CUDA tensor ({q.device})")
+    return q.device
+
+
+class _Here:
+    """No change of device: the tensors are on the current one."""
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_HERE = _Here()
+
+
+def _on(device):
+    """The tensors' device made current for a launch: kernels and the stream are that device's."""
+    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def relative_buckets(num_buckets=32, max_distance=128, both=True, device="cuda"):
+    """The usual map of distances (key minus query position) to buckets: half of a direction's
+    buckets hold one distance each, the others widen with the logarithm up to max_distance, from
+    where on all distances share the last one.  With `both` keys ahead of the query have buckets
+    of their own.  Returns (rel_buckets, rel_min) as the calls below take them."""
+    values, rel_min = dsa3d_relative_buckets(int(num_buckets), int(max_distance), both)
+    return torch.tensor(values, dtype=torch.int32, device=device), rel_min
+
+
+def _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, rel_min):
+    dev = _lead_rows(chk, q)
+    nq, heads, D = q.shape
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        chk.problems.append("k: expected a [rows, heads, head_dim] tensor")
+        chk.done()
+    nk, kv_heads = k.shape[0], k.shape[1]
+    if kv_heads < 1 or heads % kv_heads:
+        chk.problems.append(f"k: {kv_heads} heads do not divide the {heads} of q")
+    qs = _rows(chk, "q", q, heads, D, q.dtype, dev)
+    ks = _rows(chk, "k", k, kv_heads, D, q.dtype, dev)
+    vs = _rows(chk, "v", v, kv_heads, D, q.dtype, dev, nk)
+    batch = _cu(chk, "cu_q", cu_q, dev)
+    if cu_k is not None:
+        _ints(chk, "cu_k", cu_k, (batch + 1,), dev)
+    elif nk != nq:
+        chk.problems.append(f"k: {nk} rows, but q has {nq} and there is no cu_k")
+    lo, span, buckets = _relative(chk, rel_table, rel_buckets, rel_min, heads, dev)
+    return dev, make_seq_desc(batch, nq, nk, heads, kv_heads, D, causal, _IO_DTYPES[q.dtype],
+                              scale, lo, span, buckets, qs, ks, vs)
+
+
+def seq_forward(q, k, v, cu_q, cu_k=None, causal=False, scale=0.0, rel_table=None,
+                rel_buckets=None, rel_min=0, need_lse=True, need_residual=False, out=None,
+                lse=None, out_res=None):
+    """Attention of packed sequences (bf16 or float32): q [rows, heads, head_dim], k and v
+    [rows, kv_heads, head_dim], rows of a tensor any distance apart, sequence b in rows cu_q[b]
+    .. cu_q[b + 1] - 1 (int32, on the GPU), its keys in those of cu_k (the same where None).
+    `rel_table` (float32 [buckets, heads]) adds rel_table[rel_buckets[distance - rel_min]] to the
+    logits, distances clamped to the ends of rel_buckets (see relative_buckets).
+    Returns (out, lse, out_res).  out_res, the bf16 rounding residual of out, is what a bias
+    gradient in float32 accuracy needs; it is None unless need_residual is set, and for float32
+    tensors, which have none (as lse is None when need_lse is False)."""
+    chk = _Checks("seq_forward")
+    dev, desc = _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, rel_min)
+    need_residual = need_residual and q.dtype == torch.bfloat16
+    chk.optional("out", out, q.shape, q.dtype, dev)
+    if need_lse:
+        chk.optional("lse", lse, q.shape[:2], torch.float32, dev)
+    if need_residual:
+        chk.optional("out_res", out_res, q.shape, q.dtype, dev)
+    chk.done()
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if not need_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+    if not need_residual:
+        out_res = None
+    elif out_res is None:
+        out_res = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    with _on(dev):
+        dsa3d_seq_forward(desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out, out_res, lse)
+    return out, lse, out_res
+
+
+def seq_backward(q, k, v, out, out_res, lse, dout, cu_q, cu_k=None, causal=False, scale=0.0,
+                 rel_table=None, rel_buckets=None, rel_min=0, need_table=True, grads=None,
+                 workspace=None):
+    """Returns (dq, dk, dv) in the type of q, and with rel_table also its gradient (float32; None
+    where need_table is False).  `grads`: tensors to write into, in this order.  out_res may be
+    None (Delta from the rounded out alone)."""
+    chk = _Checks("seq_backward")
+    dev, desc = _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, rel_min)
+    for name, t in (("out", out), ("dout", dout)):
+        chk.tensor(name, t, q.shape, q.dtype, dev)
+    chk.optional("out_res", out_res, q.shape, q.dtype, dev)
+    chk.tensor("lse", lse, q.shape[:2], torch.float32, dev)
+    count = 3 if rel_table is None else 4
+    need_table = need_table and rel_table is not None
+    if grads is not None:
+        if len(grads) != count:
+            chk.problems.append("grads: expected (dq, dk, dv" +
+                                (", d_rel_table)" if count == 4 else ")"))
+        else:
+            for name, t, like in zip(("dq", "dk", "dv"), grads, (q, k, k)):
+                chk.tensor(name, t, like.shape, q.dtype, dev)
+            if need_table:
+                chk.tensor("d_rel_table", grads[3], rel_table.shape, torch.float32, dev)
+    chk.workspace(workspace, dev)
+    chk.done()
+    if grads is None:
+        grads = [torch.empty(x.shape, dtype=q.dtype, device=dev) for x in (q, k, k)]
+        if count == 4:
+            grads.append(torch.empty(rel_table.shape, dtype=torch.float32, device=dev)
+                         if need_table else None)
+    need = dsa3d_seq_backward_workspace_size(desc)
+    if workspace is None or workspace.numel() < need:
+        workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
+    d_table = grads[3] if need_table else None
+    with _on(dev):
+        dsa3d_seq_backward(desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out, out_res, lse,
+                           dout, grads[0], grads[1], grads[2], d_table, workspace, need)
+    return tuple(grads[:3]) if count == 3 else (*grads[:3], d_table)
+
+
+# ----------------------------------------------------------------------------- a paged cache
+
+def _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q, dtype, device):
+    """Checks the cache; returns (requests, num_pages, page_size, kv_heads, head_dim, columns)."""
+    if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
+        chk.problems.append("k_pages: expected [pages, page_size, kv_heads, head_dim]")
+        chk.done()
+    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
+        chk.tensor(name, t, k_pages.shape, dtype, device)
+    batch = _cu(chk, "cu_q", cu_q, device)
+    _ints(chk, "kv_lens", kv_lens, (batch,), device)
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
+        chk.problems.append("pages: expected an int32 [requests, columns] tensor")
+        chk.done()
+    _ints(chk, "pages", pages, (batch, pages.shape[1]), device)
+    return (batch, *k_pages.shape, pages.shape[1])
+
+
+def paged_append(k, v, k_pages, v_pages, pages, kv_lens, cu_q):
+    """Writes the new tokens' k, v [rows, kv_heads, head_dim] (packed by cu_q, rows any distance
+    apart) into the pages k_pages, v_pages [pages, page_size, kv_heads, head_dim], in place.
+    Request b holds kv_lens[b] tokens with the new ones, token j of them in row j % page_size of
+    page pages[b, j // page_size]; a token whose page number is outside the tensors is dropped."""
+    chk = _Checks("paged_append")
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        chk.problems.append("k: expected a [rows, kv_heads, head_dim] tensor")
+        chk.done()
+    if k.dtype not in _IO_DTYPES:
+        chk.problems.append(f"k: unsupported dtype {k.dtype}")
+        chk.done()
+    if not k.is_cuda:
+        chk.problems.append(f"k: not a CUDA tensor ({k.device})")
+    dev = k.device
+    batch, num, size, heads, D, columns = _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q,
+                                                 k.dtype, dev)
+    ks = _rows(chk, "k", k, heads, D, k.dtype, dev)
+    vs = _rows(chk, "v", v, heads, D, k.dtype, dev, k.shape[0])
+    chk.done()
+    desc = make_paged_desc(batch, k.shape[0], heads, heads, D, num, size, columns,
+                           dtype=_IO_DTYPES[k.dtype], k_stride=ks, v_stride=vs)
+    with _on(dev):
+        dsa3d_paged_append(desc, k, v, cu_q, kv_lens, pages, k_pages, v_pages)
+
+
+def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=0.0,
+                  rel_table=None, rel_buckets=None, rel_min=0, max_kv=0, need_lse=False, out=None,
+                  lse=None, workspace=None):
+    """Attention of the newest tokens q [rows, heads, head_dim] (packed by cu_q; one or more per
+    request) over the tokens their requests hold in pages (see paged_append; the new ones' k and v
+    are there already).  `max_kv`: a bound of kv_lens that the caller knows (0: what the page
+    table can hold); a near one lets the work be dealt out better.  Returns (out, lse)."""
+    chk = _Checks("paged_forward")
+    dev = _lead_rows(chk, q)
+    nq, heads, D = q.shape
+    qs = _rows(chk, "q", q, heads, D, q.dtype, dev)
+    batch, num, size, kv_heads, kD, columns = _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q,
+                                                     q.dtype, dev)
+    if kD != D or kv_heads < 1 or heads % kv_heads:
+        chk.problems.append(f"k_pages: {kv_heads} heads x {kD} for queries of {heads} x {D}")
+    lo, span, buckets = _relative(chk, rel_table, rel_buckets, rel_min, heads, dev)
+    chk.optional("out", out, q.shape, q.dtype, dev)
+    if need_lse:
+        chk.optional("lse", lse, q.shape[:2], torch.float32, dev)
+    chk.workspace(workspace, dev)
+    chk.done()
+    desc = make_paged_desc(batch, nq, heads, kv_heads, D, num, size, columns, int(max_kv), causal,
+                           _IO_DTYPES[q.dtype], scale, lo, span, buckets, qs)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if not need_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+    need = dsa3d_paged_forward_workspace_size(desc)
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    with _on(dev):
+        dsa3d_paged_forward(desc, q, k_pages, v_pages, pages, kv_lens, cu_q, rel_table,
+                            rel_buckets, out, lse, workspace, need)
+    return out, lse
