@@ -66,7 +66,8 @@ typedef struct {
   float scale;                         /* logit scale > 0; 0 selects 1/sqrt(head_dim)         */
   dsa3d_dtype dtype;                   /* type of q, k, v, out, dout and the gradients        */
   int64_t q_stride, k_stride, v_stride;/* elements from one token's row to the next's, at least
-                                          a row and a multiple of 16 bytes; 0: a row          */
+                                          a row, a multiple of 16 bytes and below 16 MiB; 0: a
+                                          row                                                 */
 } dsa3d_seq_desc;
 
 /* out and, when not NULL, lse and out_res.  out_res (bf16 only, else it must be NULL) is the

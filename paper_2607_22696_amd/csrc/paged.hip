@@ -152,6 +152,7 @@ __device__ inline void finish_logits(float (&s)[16], const PagedGeometry& g, con
     for (int i = 0; i < 16; ++i) s[i] *= g.scale_log2;
   }
   if (masked) {
+    asm volatile("");  // a branch: blocks that every row sees do not pay for it
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (kb + c_row(i, hh) > last || rows[c_row(i, hh)] < 0) s[i] = -INFINITY;
@@ -188,7 +189,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     fill_rows<KT>(tab[i], &bad[i], g, pages, s, s.k_lo + i * KT);
   if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int rw = s.r0 + wave * 32;
   const Row x = row_of(g, s, w.u, rw + (lane & 31));
   Frag qf[KS];
@@ -319,7 +320,7 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     fill_rows<KT>(tab[i], bad[i], g, pages, s, s.k_lo + i * KT);
   if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const Row x = row_of(g, s, w.u, s.r0 + (lane & 31));
   Frag qf[KS];
   load_frag<T, D>(qf, q + x.q_at, x.ok);

@@ -21,11 +21,11 @@ using dsa3d::api::span_of;
 constexpr int64_t kIndexLimit = 1ll << 31;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A row stride in elements: 0 selects the row itself.  Returns false for one below a row or not a
-// multiple of 16 bytes.
+// A row stride in elements: 0 selects the row itself.  Returns false for one below a row, not a
+// multiple of 16 bytes, or of 16 MiB and more (offsets within a tile are 32 bits).
 bool check_stride(int64_t given, int64_t row, int item, int64_t* stride) {
   *stride = given == 0 ? row : given;
-  return *stride >= row && *stride < (1ll << 40) && *stride * item % 16 == 0;
+  return *stride >= row && *stride < (1 << 24) / item && *stride * item % 16 == 0;
 }
 
 dsa3d_status check_heads(int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,

@@ -69,8 +69,25 @@ __device__ inline float pair_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// The wave's number within its workgroup, known to be the same for all its lanes.
+__device__ inline int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
 // Row of a 32-row block that element i of a result holds in this half of the wave.
 __device__ inline int c_row(int i, int hh) { return 8 * (i / 4) + 4 * hh + (i % 4); }
+
+__device__ inline uint32_t lds_offset(const void* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+// 16 bytes per lane from base + off to LDS at `to` + 16 lane, without a register in between.  The
+// compiler does not count it among the loads it waits for: the reader waits with wait_copies().
+// (Its builtin has the compiler wait for every copy in flight before any LDS read.)
+__device__ inline void copy_16(uint32_t to, const void* base, uint32_t off) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+               :
+               : "s"(to), "v"(off), "s"(base)
+               : "memory");
+}
+__device__ inline void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A tile of ROWS rows x D channels in LDS, rows unpadded, the 16-byte chunks of a row XOR-permuted
 // by a function of the row so that both operand reads are free of bank conflicts.  bf16: as
@@ -103,18 +120,26 @@ struct Tile {
   static __device__ inline int row_of_thread(int i) { return (int)threadIdx.x / KCH + i * kStep; }
   static __device__ inline int chan_of_thread() { return ((int)threadIdx.x % KCH) * CH; }
 
-  // Rows 0 .. ROWS - 1 at src + row * stride; rows from `valid` on read as zero (their loads go to
-  // the last valid row, so that no branch is needed).  valid >= 1.
-  static __device__ inline void load(uint4 (&r)[NL], const T* src, int64_t stride, int valid) {
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      const int row = min(row_of_thread(i), valid - 1);
-      r[i] = *reinterpret_cast<const uint4*>(src + row * stride + chan_of_thread());
-    }
-    if (valid < ROWS) {
+  // This thread's first chunk of a tile whose row 0 is at src.
+  static __device__ inline const T* first_chunk(const T* src, int64_t stride) {
+    return src + row_of_thread(0) * stride + chan_of_thread();
+  }
+  // The thread's chunks of a tile, `first` being its first one's address; rows from `valid` on
+  // read as zero (their loads go to the last valid row).  valid >= 1, uniform.
+  static __device__ inline void load(uint4 (&r)[NL], const T* first, int64_t stride, int valid) {
+    if (valid >= ROWS) {
 #pragma unroll
       for (int i = 0; i < NL; ++i)
-        if (row_of_thread(i) >= valid) r[i] = make_uint4(0, 0, 0, 0);
+        r[i] = *reinterpret_cast<const uint4*>(first + i * (kStep * stride));
+    } else {
+      asm volatile("");  // a branch: full tiles do not pay for this
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = row_of_thread(i);
+        r[i] = *reinterpret_cast<const uint4*>(
+            first + (int64_t)(min(row, valid - 1) - row_of_thread(0)) * stride);
+        if (row >= valid) r[i] = make_uint4(0, 0, 0, 0);
+      }
     }
   }
   // Tile rows through a table of tensor rows (negative: no such row, reads as zero).
@@ -135,6 +160,43 @@ struct Tile {
 #pragma unroll
     for (int i = 0; i < NL; ++i)
       *reinterpret_cast<uint4*>(lds + at(row_of_thread(i), chan_of_thread())) = r[i];
+  }
+
+  // Asynchronous staging: global_load_lds_dwordx4 puts 16 bytes per lane at consecutive LDS
+  // addresses, 1 KiB per wave and instruction, so the permutation of a row's chunks is made in the
+  // addresses read: the lane that writes position c of row r reads chunk c ^ f(r).
+  static constexpr int kRowBytes = D * (int)sizeof(T);
+  static constexpr int kRowsPerCopy = 1024 / kRowBytes;
+  static constexpr int NC = ROWS * kRowBytes / (1024 * (THREADS / 64));  // copies per wave
+  static_assert(NC >= 1, "every wave copies");
+  static __device__ inline int copy_row(int i) {
+    return (wave_id() * NC + i) * kRowsPerCopy + ((int)threadIdx.x & 63) / KCH;
+  }
+  static __device__ inline int copy_chunk(int row) {
+    return (at(row, ((int)threadIdx.x % KCH) * CH) - row * D) * (int)sizeof(T);
+  }
+  // Byte offsets of this lane's sources from the tile's first row.
+  static __device__ inline void copy_plan(uint32_t (&off)[NC], uint32_t stride_bytes) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      off[i] = (uint32_t)copy_row(i) * stride_bytes + copy_chunk(copy_row(i));
+  }
+  // Starts the copy of a tile whose row 0 is at src (uniform); rows from `valid` on repeat the last
+  // valid one, to be masked.  Done once wait_copies() and a barrier have passed.
+  static __device__ inline void copy(T* lds, const T* src, const uint32_t (&off)[NC],
+                                     uint32_t stride_bytes, int valid) {
+    const uint32_t to = lds_offset(lds) + wave_id() * (NC * 1024);
+    if (valid >= ROWS) {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) copy_16(to + i * 1024, src, off[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        const int row = copy_row(i);
+        copy_16(to + i * 1024, src,
+                (uint32_t)min(row, valid - 1) * stride_bytes + copy_chunk(row));
+      }
+    }
   }
 
   // Operand with tile rows as its rows: row r0 + l % 32, channels 16 ks + 8 (l / 32) .. +7.

@@ -1,7 +1,14 @@
 // Attention of packed sequences, forward and backward (include/dsa3d_seq.h), gfx950 kernels.
 //
-// Forward: one pass over the keys with a running maximum and sum.  A workgroup takes 128 queries
-// of one head (four waves of 32) and streams the keys its mask leaves through LDS.
+// Forward: one pass over the keys with a running maximum and sum.  A workgroup takes 128 or 256
+// queries of one head (waves of 32) and streams the keys its mask leaves through LDS.  Bound by
+// the matrix cores and the vector ALU together: per 32 x 32 block at 128 channels 16 products
+// (512 cycles) beside 57 vector instructions, 16 of them exponentials, and 24 LDS reads.  What
+// staging and reading cost was measured by leaving each out of a copy (8,192 tokens, 16 heads x
+// 128, 596 us with tiles loaded to registers and stored to LDS): without the staging 474 us,
+// without the operand reads 446, without the softmax 521.  Copies straight to LDS, LDS places that
+// are constants and the next block's products beside this one's exponentials take 491 us
+// (1.12 PFLOP/s; a 16384^3 matrix product reaches 1.37).
 // Backward without atomics: a pass over query tiles (dq, Delta, the bias gradient) and one over
 // key tiles (dk, dv), each recomputing alpha = exp(t - lse).
 #include <hip/hip_runtime.h>
@@ -28,9 +35,10 @@ struct Bias {
 };
 
 // Fills tab (span floats) with the bias of `head`.  A barrier follows before its use.
+template <int THREADS = kThreads>
 __device__ inline void fill_bias(float* tab, const SeqGeometry& g, const float* table,
                                  const int32_t* map, int head) {
-  for (int i = threadIdx.x; i < g.span; i += kThreads)
+  for (int i = threadIdx.x; i < g.span; i += THREADS)
     tab[i] = bias_of(table, map, g.H, g.nb, head, i);
 }
 
@@ -53,42 +61,74 @@ __device__ inline void add_bias(float (&s)[16], const SeqGeometry& g, const floa
 
 // ---------------------------------------------------------------------------- forward
 
-template <typename T, int D, bool BIAS, bool RES>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+// W waves of 32 queries each; KT keys per LDS tile, two tiles of keys and of values in LDS.
+template <typename T, int D, int W, bool BIAS, bool RES>
+__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                     const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                     const int32_t* __restrict__ cu_k, const float* __restrict__ table,
                     const int32_t* __restrict__ map, T* __restrict__ out,
                     T* __restrict__ out_res, float* __restrict__ lse) {
-  constexpr int KT = Type<T>::kKeyTile;
-  using Tl = Tile<T, D, KT>;
+  constexpr int QT = W * 32, KT = W * (sizeof(T) == 2 ? 16 : 8);
+  using Tl = Tile<T, D, KT, W * 64>;
+  using Rows = Tile<T, D, QT, W * 64>;  // a tile of queries, or of results
   using Frag = typename Type<T>::Frag;
-  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32;
-  __shared__ __attribute__((aligned(16))) T Ks[2][Tl::kElems];
-  __shared__ __attribute__((aligned(16))) T Vs[2][Tl::kElems];
-  extern __shared__ float tab[];  // the bias by distance
+  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
+  constexpr bool kThroughLds = sizeof(T) == 2;  // queries and results fit a pair of tiles
+  static_assert(!kThroughLds || Rows::kElems == 2 * E, "two tiles hold the queries");
+  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
+  extern __shared__ float tab[];                         // the bias by distance
 
   Work w;
   if (!work_of(g.q_tiles, g.group, w)) return;
-  const Slot sq = find_slot<kSeqTile>(cu_q, g.B, g.nq, 1, w.slot);
-  const int q0 = sq.tile * kSeqTile, n = sq.end - sq.begin;
+  const Slot sq = find_slot<QT>(cu_q, g.B, g.nq, 1, w.slot);
+  const int q0 = sq.tile * QT, n = sq.end - sq.begin;
   if (q0 >= n) return;
   int k0, m;
   key_rows(cu_k, sq.b, g.B, g.nk, k0, m);
   const int off = m - n;  // position of query 0
-  const int nkeys = g.causal ? min(m, min(q0 + kSeqTile, n) + off) : m;
+  const int nkeys = g.causal ? min(m, min(q0 + QT, n) + off) : m;
   const int ntiles = nkeys > 0 ? (nkeys + KT - 1) / KT : 0;
-  if constexpr (BIAS) fill_bias(tab, g, table, map, w.head);
+  if constexpr (BIAS) fill_bias<W * 64>(tab, g, table, map, w.head);
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int i0 = q0 + wave * 32, iq = i0 + (lane & 31);
-  const bool qok = iq < n;
+  const bool qok = iq < n, live = i0 < n;
   const int64_t qrow = sq.begin + (qok ? iq : 0);
+
+  // Tile i of keys and values is copied to LDS buffer i % 2.
+  const T* kp = k + (int64_t)k0 * g.ks + w.u * D;
+  const T* vp = v + (int64_t)k0 * g.vs + w.u * D;
+  const uint32_t ksb = (uint32_t)g.ks * sizeof(T), vsb = (uint32_t)g.vs * sizeof(T);
+  uint32_t ko[Tl::NC], vo[Tl::NC];
+  Tl::copy_plan(ko, ksb);
+  Tl::copy_plan(vo, vsb);
+  auto fetch = [&](int kt, int buf) {
+    const int64_t at = (int64_t)kt * KT;
+    Tl::copy(lds + 2 * E * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
+    Tl::copy(lds + 2 * E * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
+  };
   Frag qf[KS];
-  load_frag<T, D>(qf, q + qrow * g.qs + w.head * D, qok);
+  if constexpr (kThroughLds) {
+    uint32_t qo[Rows::NC];
+    const uint32_t qsb = (uint32_t)g.qs * sizeof(T);
+    Rows::copy_plan(qo, qsb);
+    Rows::copy(lds + 2 * E, q + (sq.begin + q0) * g.qs + w.head * D, qo, qsb, n - q0);
+    if (ntiles > 0) fetch(0, 0);
+    wait_copies();
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) qf[ks] = Rows::a_rows(lds + 2 * E, wave * 32, ks);
+  } else {
+    if (ntiles > 0) fetch(0, 0);
+    load_frag<T, D>(qf, q + qrow * g.qs + w.head * D, qok);
+    wait_copies();
+  }
+  __syncthreads();
+
   // the last key this query sees, and the last one any of the wave's queries sees
   const int last = g.causal ? min(m - 1, iq + off) : m - 1;
-  const int wave_last = i0 >= n ? -1 : g.causal ? min(m - 1, min(i0 + 31, n - 1) + off) : m - 1;
+  const int wave_last = !live ? -1 : g.causal ? min(m - 1, min(i0 + 31, n - 1) + off) : m - 1;
   const int all_see = g.causal ? min(m - 1, i0 + off) : m - 1;
 
   f32x16_t o[DB];
@@ -105,44 +145,96 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
     for (int ks = 0; ks < KS; ++ks) acc = mfma(a[ks], qf[ks], acc);
     return acc;
   };
+  // The largest of a block's logits (base 2), and the running maximum raised where that exceeds
+  // it by more than kSlack: alpha stays below 2^kSlack and the rescale of O is rare.  The result
+  // does not depend on which maximum was used.
+  auto raise_to = [&](const float (&s)[16]) {
+    float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
+#pragma unroll
+    for (int i = 3; i < 16; ++i) mx = fmaxf(mx, s[i]);
+    mx = pair_max(mx);
+    if constexpr (!BIAS) mx *= g.scale_log2;  // scale > 0
+    const bool raise = mx > mx_run + kSlack;
+    if (__any(raise)) {
+      const float corr = raise ? __builtin_amdgcn_exp2f(mx_run - mx) : 1.0f;
+      if (raise) mx_run = base = mx;
+      l *= corr;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] *= corr;
+    }
+  };
+  // alpha (unnormalised) in place of the logits, and its fragments
+  auto weigh = [&](float (&s)[16], Frag (&ph)[2]) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - base : fmaf(s[i], g.scale_log2, -base));
+      l += s[i];
+    }
+    to_frags(s, ph);
+  };
+  auto values = [&](const T* vc, int b, Frag (&av)[DB][2]) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) av[db][p] = Tl::a_cols(vc, db * 32, b, p);
+  };
+  auto accumulate = [&](const Frag (&av)[DB][2], const Frag (&ph)[2]) {
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) o[db] = mfma(av[db][p], ph[p], o[db]);
+  };
 
-  // Tile i is staged in LDS buffer i % 2, its loads one tile ahead; one barrier per tile.
-  const T* kp = k + (int64_t)k0 * g.ks + w.u * D;
-  const T* vp = v + (int64_t)k0 * g.vs + w.u * D;
-  uint4 kr[Tl::NL], vr[Tl::NL];
-  if (ntiles > 0) {
-    Tl::load(kr, kp, g.ks, m);
-    Tl::load(vr, vp, g.vs, m);
-    Tl::store(Ks[0], kr);
-    Tl::store(Vs[0], vr);
-    if (ntiles > 1) {
-      Tl::load(kr, kp + (int64_t)KT * g.ks, g.ks, m - KT);
-      Tl::load(vr, vp + (int64_t)KT * g.vs, g.vs, m - KT);
+  // Tiles that every query of the workgroup sees whole, without a bias: the next block's logits
+  // are on the matrix cores while this block's exponentials are on the vector ALU.  Two tiles per
+  // turn, so that the LDS buffers' places are constants.
+  int kt = 0;
+  if constexpr (!BIAS && !RES) {
+    const int whole = (g.causal ? min(m, q0 + off + 1) : m) / KT;
+    f32x16_t next = f32x16_t{};
+    if (whole > 0 && live) next = logits(lds, 0);
+    auto tile = [&](int t, int buf) {
+      const T *kc = lds + 2 * E * buf, *vc = kc + E, *kn = lds + 2 * E * (1 - buf);
+      if (t + 1 < ntiles) fetch(t + 1, 1 - buf);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        float s[16];
+        if (live) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = next[i];
+          raise_to(s);
+        }
+        if (b == NB - 1) {  // the next tile is in LDS
+          wait_copies();
+          __syncthreads();
+        }
+        if (live) {
+          Frag av[DB][2], ph[2];
+          next = b + 1 < NB ? logits(kc, b + 1) : logits(kn, 0);
+          values(vc, b, av);
+          weigh(s, ph);
+          accumulate(av, ph);
+        }
+      }
+      __syncthreads();
+    };
+    for (; kt + 1 < whole; kt += 2) {
+      tile(kt, 0);
+      tile(kt + 1, 1);
     }
+    if (kt < whole) tile(kt++, 0);
   }
-  __syncthreads();
-  for (int kt = 0; kt < ntiles; ++kt) {
-    const T *kc = Ks[kt & 1], *vc = Vs[kt & 1];
-    if (kt + 1 < ntiles) {
-      Tl::store(Ks[(kt + 1) & 1], kr);
-      Tl::store(Vs[(kt + 1) & 1], vr);
-    }
-    if (kt + 2 < ntiles) {
-      const int at = (kt + 2) * KT;
-      Tl::load(kr, kp + at * g.ks, g.ks, m - at);
-      Tl::load(vr, vp + at * g.vs, g.vs, m - at);
-    }
+  for (; kt < ntiles; ++kt) {
+    const T *kc = lds + 2 * E * (kt & 1), *vc = kc + E;
+    if (kt + 1 < ntiles) fetch(kt + 1, (kt + 1) & 1);
     const int kbase = kt * KT;
     const int nb = wave_last < kbase ? 0 : min(NB, (wave_last - kbase) / 32 + 1);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b >= nb) break;
       const f32x16_t cur = logits(kc, b);
-      Frag av[DB][2];
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) av[db][p] = Tl::a_cols(vc, db * 32, b, p);
+      Frag av[DB][2], ph[2];
+      values(vc, b, av);
       const int kb = kbase + b * 32;
       float s[16];
 #pragma unroll
@@ -151,68 +243,63 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
         add_bias(s, g, tab, kb - (i0 + 31 + off), kb + 31 - (i0 + off),
                  [&](int i) { return kb + c_row(i, hh) - iq - off; });
       if (kb + 31 > all_see) {
+        asm volatile("");  // a branch: blocks that every query sees do not pay for it
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (kb + c_row(i, hh) > last) s[i] = -INFINITY;
       }
-      float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
-#pragma unroll
-      for (int i = 3; i < 16; ++i) mx = fmaxf(mx, s[i]);
-      mx = pair_max(mx);
-      if constexpr (!BIAS) mx *= g.scale_log2;  // scale > 0
-      // The running maximum is raised only when a logit exceeds it by more than kSlack (base 2):
-      // alpha stays below 2^kSlack and the rescale of O is rare.  The result does not depend on
-      // which maximum was used.
-      const bool raise = mx > mx_run + kSlack;
-      if (__any(raise)) {
-        const float corr = raise ? __builtin_amdgcn_exp2f(mx_run - mx) : 1.0f;
-        if (raise) mx_run = base = mx;
-        l *= corr;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) o[db] *= corr;
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - base : fmaf(s[i], g.scale_log2, -base));
-        l += s[i];
-      }
-      Frag ph[2];
-      to_frags(s, ph);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) o[db] = mfma(av[db][p], ph[p], o[db]);
+      raise_to(s);
+      weigh(s, ph);
+      accumulate(av, ph);
       if constexpr (RES) {
         Frag pl[2];
         to_low_frags(s, ph, pl);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int p = 0; p < 2; ++p) o[db] = mfma(av[db][p], pl[p], o[db]);
+        accumulate(av, pl);
       }
     }
+    wait_copies();
     __syncthreads();
   }
 
   const float ltot = pair_sum(l);
-  if (!qok) return;
   const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;  // 0 for an empty row, NaN stays
   const int64_t row = qrow * g.H + w.head;
+  if (qok && hh == 0 && lse != nullptr)
+    lse[row] = ltot == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(ltot)) * kLn2;
+  if (!live) return;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    store_block(out + row * D, db, o[db], inv);
-    if constexpr (RES) {
-      f32x16_t r;
+  for (int part = 0; part < (RES ? 2 : 1); ++part) {
+    T* to = part == 0 ? out : out_res;
+    if constexpr (kThroughLds) {
+      // The wave's 32 rows through LDS (its own place, no other wave's), so that whole rows are
+      // written, 16 bytes per lane.
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float x = o[db][i] * inv;
-        r[i] = x - (float)(__bf16)x;
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int blk = 0; blk < 4; ++blk) {
+          __bf16 h[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = o[db][4 * blk + j] * inv;
+            h[j] = (__bf16)(part == 0 ? x : x - (float)(__bf16)x);
+          }
+          *reinterpret_cast<uint2*>(
+              lds + Rows::at(wave * 32 + (lane & 31), db * 32 + 8 * blk + 4 * hh)) =
+              __builtin_bit_cast(uint2, h);
+        }
+      constexpr int PER = 64 / Rows::KCH;  // rows per instruction
+#pragma unroll
+      for (int i = 0; i < 32 / PER; ++i) {
+        const int r = i * PER + lane / Rows::KCH, c = (lane % Rows::KCH) * 8;
+        const uint4 u = *reinterpret_cast<const uint4*>(lds + Rows::at(wave * 32 + r, c));
+        if (i0 + r < n)
+          *reinterpret_cast<uint4*>(to + ((int64_t)(sq.begin + i0 + r) * g.H + w.head) * D + c) = u;
       }
-      store_block(out_res + row * D, db, r, 1.0f);
+    } else if (qok) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_block(to + row * D, db, o[db], inv);
     }
   }
-  if (hh == 0 && lse != nullptr)
-    lse[row] = ltot == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(ltot)) * kLn2;
 }
 
 // ---------------------------------------------------------------------------- backward
@@ -257,7 +344,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   const int nkeys = g.causal ? min(m, min(q0 + kSeqTile, n) + off) : m;
   const int ntiles = nkeys > 0 ? (nkeys + KT - 1) / KT : 0;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int i0 = q0 + wave * 32, iq = i0 + (lane & 31);
   const bool qok = iq < n;
   const int64_t qrow = sq.begin + (qok ? iq : 0), row = qrow * g.H + w.head;
@@ -301,8 +388,8 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
   float behind = 0.0f, ahead = 0.0f;
 
-  const T* kp = k + (int64_t)k0 * g.ks + w.u * D;
-  const T* vp = v + (int64_t)k0 * g.vs + w.u * D;
+  const T* kp = Tl::first_chunk(k + (int64_t)k0 * g.ks + w.u * D, g.ks);
+  const T* vp = Tl::first_chunk(v + (int64_t)k0 * g.vs + w.u * D, g.vs);
   uint4 kr[Tl::NL], vr[Tl::NL];
   if (ntiles > 0) {
     Tl::load(kr, kp, g.ks, m);
@@ -310,8 +397,8 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
     Tl::store(Ks[0], kr);
     Tl::store(Vs[0], vr);
     if (ntiles > 1) {
-      Tl::load(kr, kp + (int64_t)KT * g.ks, g.ks, m - KT);
-      Tl::load(vr, vp + (int64_t)KT * g.vs, g.vs, m - KT);
+      Tl::load(kr, kp + KT * g.ks, g.ks, m - KT);
+      Tl::load(vr, vp + KT * g.vs, g.vs, m - KT);
     }
   }
   __syncthreads();
@@ -351,6 +438,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
         ds[i] = p * (pa[i] - dl);
       }
       if (kb + 31 > all_see || i0 + 31 >= n) {
+        asm volatile("");
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (kb + c_row(i, hh) > last || !qok) ds[i] = 0.0f;
@@ -476,7 +564,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   const int per_head = n > q_first ? (n - q_first + QT - 1) / QT : 0;
   const int ntiles = per_head * g.group;
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, hh = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int j0 = k0 + wave * 32, jk = j0 + (lane & 31);
   const bool kok = jk < m;
   const int64_t krow = sk.begin + (kok ? jk : 0);
@@ -492,9 +580,9 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   float ls = INFINITY, de = 0.0f;
   auto fetch = [&](int it) {
     const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
-    const int64_t row = qbeg + at;
-    Tl::load(rq, q + row * g.qs + head * D, g.qs, n - at);
-    Tl::load(rg, dout + (row * g.H + head) * D, (int64_t)g.H * D, n - at);
+    const int64_t row = qbeg + at, gs = (int64_t)g.H * D;
+    Tl::load(rq, Tl::first_chunk(q + row * g.qs + head * D, g.qs), g.qs, n - at);
+    Tl::load(rg, Tl::first_chunk(dout + row * gs + head * D, gs), gs, n - at);
     if (threadIdx.x < QT) {
       const bool ok = at + (int)threadIdx.x < n;
       const int64_t r = (row + (ok ? threadIdx.x : 0)) * g.H + head;
@@ -559,6 +647,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       }
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
         // queries before the key, and rows past the sequence's end
+        asm volatile("");
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int iq = qb + c_row(i, hh);
@@ -600,28 +689,44 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 // ---------------------------------------------------------------------------- launches
 
 template <typename... A>
-hipError_t launch(const void* fn, dim3 grid, size_t lds, hipStream_t s, A... args) {
+hipError_t launch(const void* fn, dim3 grid, int threads, size_t lds, hipStream_t s, A... args) {
   void* a[] = {(void*)&args...};
-  return hipLaunchKernel(fn, grid, dim3(kThreads), a, lds, s);
+  return hipLaunchKernel(fn, grid, dim3(threads), a, lds, s);
+}
+
+template <typename T, int D, int W>
+hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, float* lse,
+                     hipStream_t s) {
+  const bool bias = g.nb > 0;
+  const void* fn;
+  if constexpr (sizeof(T) == 2) {
+    fn = bias ? (res ? (const void*)&seq_fwd_kernel<T, D, W, true, true>
+                     : (const void*)&seq_fwd_kernel<T, D, W, true, false>)
+              : (res ? (const void*)&seq_fwd_kernel<T, D, W, false, true>
+                     : (const void*)&seq_fwd_kernel<T, D, W, false, false>);
+  } else {
+    fn = bias ? (const void*)&seq_fwd_kernel<T, D, W, true, false>
+              : (const void*)&seq_fwd_kernel<T, D, W, false, false>;
+  }
+  SeqGeometry h = g;
+  h.q_tiles = seq_spread(g.KH, g.nq / (W * 32) + g.B + 1);
+  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64, bias ? g.span * 4 : 0,
+                s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
+                out, res, lse);
 }
 
 template <typename T, int D>
 hipError_t forward_d(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, float* lse,
                      hipStream_t s) {
-  const bool bias = g.nb > 0;
-  const void* fn;
+  // Eight waves halve the copies per product but leave half the workgroups: they pay where the
+  // sequences are long and the workgroups many.  16 heads x 128, 4 / 8 waves: one causal sequence
+  // of 16,384 tokens 1.025 / 1.001 ms, of 8,192 (all keys) 515 / 491 us; 32 sequences of 512
+  // 77 / 81 us, four of 1,000 with 8 heads 27 / 31 us.
+  const bool wide = g.nk >= 4096 * (int64_t)g.B && (int64_t)g.nq * g.H >= 256 * 512;
   if constexpr (sizeof(T) == 2) {
-    fn = bias ? (res ? (const void*)&seq_fwd_kernel<T, D, true, true>
-                     : (const void*)&seq_fwd_kernel<T, D, true, false>)
-              : (res ? (const void*)&seq_fwd_kernel<T, D, false, true>
-                     : (const void*)&seq_fwd_kernel<T, D, false, false>);
-  } else {
-    fn = bias ? (const void*)&seq_fwd_kernel<T, D, true, false>
-              : (const void*)&seq_fwd_kernel<T, D, false, false>;
+    if (wide) return forward_w<T, D, 8>(g, t, out, res, lse, s);
   }
-  return launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), bias ? g.span * 4 : 0, s, g,
-                (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map, out,
-                res, lse);
+  return forward_w<T, D, 4>(g, t, out, res, lse, s);
 }
 
 size_t round_256(size_t x) { return (x + 255) & ~size_t(255); }
@@ -641,11 +746,11 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
     const void* fn = bias ? (const void*)&seq_dq_kernel<T, D, true>
                           : (const void*)&seq_dq_kernel<T, D, false>;
     const size_t lds = !bias ? 0 : partial ? (size_t)g.span * 36 + 64 : (size_t)g.span * 4;
-    e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), lds, s, g, q, k, v, t.cu_q,
+    e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), kThreads, lds, s, g, q, k, v, t.cu_q,
                t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, partial);
   }
   if (e == hipSuccess && bias && d_table != nullptr)
-    e = launch((const void*)&seq_table_kernel, dim3(g.H), 0, s, g.nq > 0 ? g.q_tiles.slots : 0,
+    e = launch((const void*)&seq_table_kernel, dim3(g.H), kThreads, 0, s, g.nq > 0 ? g.q_tiles.slots : 0,
                g.H, g.nb, (const float*)partial, d_table);
   if (e == hipSuccess && g.nk > 0) {
     const dim3 grid((unsigned)seq_blocks(g.k_tiles, 1));
@@ -653,7 +758,7 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
     const float* cdelta = delta;
     const void* fn = bias ? (const void*)&seq_dkdv_kernel<T, D, true, true, true>
                           : (const void*)&seq_dkdv_kernel<T, D, false, true, true>;
-    e = launch(fn, grid, lds, s, g, q, k, v, t.cu_q, t.cu_k, t.table, t.map, lse, dout, cdelta,
+    e = launch(fn, grid, kThreads, lds, s, g, q, k, v, t.cu_q, t.cu_k, t.table, t.map, lse, dout, cdelta,
                dk, dv);
   }
   return e;
