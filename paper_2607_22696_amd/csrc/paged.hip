@@ -271,9 +271,9 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     __syncthreads();
   }
   const float ltot = pair_sum(sm.l);
-  if (!x.ok) return;
   const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;
   const float l2 = ltot == 0.0f ? -INFINITY : sm.base + __builtin_amdgcn_logf(ltot);
+  if (!x.ok) return;
   if (g.splits == 1) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) store_block(out + x.out_at * D, db, o[db], inv);

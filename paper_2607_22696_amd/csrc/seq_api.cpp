@@ -102,8 +102,9 @@ dsa3d_status check_seq(const dsa3d_seq_desc* d, bool own_keys, dsa3d::SeqGeometr
   g->scale_log2 = g->scale * kLog2e;
   g->q_tiles = dsa3d::seq_spread(g->KH, g->nq / dsa3d::kSeqTile + g->B + 1);
   g->k_tiles = dsa3d::seq_spread(g->KH, g->nk / dsa3d::kSeqTile + g->B + 1);
+  g->parts = dsa3d::seq_backward_parts(*g);
   if (dsa3d::seq_blocks(g->q_tiles, g->group) >= kIndexLimit ||
-      dsa3d::seq_blocks(g->k_tiles, 1) >= kIndexLimit)
+      dsa3d::seq_blocks(g->k_tiles, g->parts) >= kIndexLimit)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->k = strided_bytes(d->total_k, g->ks, krow, s->item);

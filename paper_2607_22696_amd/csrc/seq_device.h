@@ -87,6 +87,14 @@ __device__ inline void copy_16(uint32_t to, const void* base, uint32_t off) {
                : "s"(to), "v"(off), "s"(base)
                : "memory");
 }
+// The same with 4 bytes per lane, from base + first floats + off bytes.
+__device__ inline void copy_4(uint32_t to, const float* base, uint32_t off, int64_t first) {
+  base += first;
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
+               :
+               : "s"(to), "v"(off), "s"(base)
+               : "memory");
+}
 __device__ inline void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // A tile of ROWS rows x D channels in LDS, rows unpadded, the 16-byte chunks of a row XOR-permuted
@@ -294,6 +302,7 @@ __device__ inline void store_block(float* row, int db, const f32x16_t& acc, floa
         make_float4(acc[4 * blk] * mul, acc[4 * blk + 1] * mul, acc[4 * blk + 2] * mul,
                     acc[4 * blk + 3] * mul);
 }
+
 __device__ inline void store_block(uint16_t* row, int db, const f32x16_t& acc, float mul) {
   const int hh = (threadIdx.x & 63) >> 5;
 #pragma unroll
@@ -302,6 +311,43 @@ __device__ inline void store_block(uint16_t* row, int db, const f32x16_t& acc, f
 #pragma unroll
     for (int j = 0; j < 4; ++j) h[j] = (__bf16)(acc[4 * blk + j] * mul);
     *reinterpret_cast<uint2*>(row + db * 32 + 8 * blk + 4 * hh) = __builtin_bit_cast(uint2, h);
+  }
+}
+
+// A wave's 32 results (lane l's column is row l % 32) times mul to rows `first` .. of `to`, `stride`
+// elements apart, as far as there are `rows`.  bf16 rows pass through LDS, in the wave's own 32
+// rows of `lds`, so that they are written whole, 16 bytes per lane; RES writes what the rounding
+// to bf16 leaves instead.
+template <typename T, int D, bool RES = false>
+__device__ inline void store_rows(T* lds, const f32x16_t (&o)[D / 32], float mul, T* to,
+                                  int64_t stride, int rows) {
+  const int lane = threadIdx.x & 63, hh = lane >> 5;
+  if constexpr (sizeof(T) == 2) {
+    using Rows = Tile<T, D, 32, 64>;
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        __bf16 h[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float x = o[db][4 * blk + j] * mul;
+          h[j] = (__bf16)(RES ? x - (float)(__bf16)x : x);
+        }
+        *reinterpret_cast<uint2*>(lds + Rows::at(lane & 31, db * 32 + 8 * blk + 4 * hh)) =
+            __builtin_bit_cast(uint2, h);
+      }
+    constexpr int PER = 64 / Rows::KCH;  // rows per instruction
+    const int c = (lane % Rows::KCH) * 8;
+#pragma unroll
+    for (int i = 0; i < 32 / PER; ++i) {
+      const int r = i * PER + lane / Rows::KCH;
+      const uint4 u = *reinterpret_cast<const uint4*>(lds + Rows::at(r, c));
+      if (r < rows) *reinterpret_cast<uint4*>(to + r * stride + c) = u;
+    }
+  } else if ((lane & 31) < rows) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) store_block(to + (lane & 31) * stride, db, o[db], mul);
   }
 }
 

@@ -23,6 +23,7 @@ struct SeqGeometry {
   float scale, scale_log2;
   int64_t qs, ks, vs;     // elements between token rows
   Spread q_tiles, k_tiles;
+  int parts;              // parts of a key tile's queries in the dk/dv pass
 };
 
 constexpr int kSeqTile = 128;  // queries (forward, dq) or keys (dk, dv) per workgroup
@@ -41,6 +42,7 @@ struct SeqTensors {
 
 hipError_t launch_seq_forward(const SeqGeometry& g, bool bf16, const SeqTensors& t, void* out,
                               void* out_res, float* lse, hipStream_t stream);
+int seq_backward_parts(const SeqGeometry& g);
 size_t seq_backward_workspace(const SeqGeometry& g, bool want_table);
 hipError_t launch_seq_backward(const SeqGeometry& g, bool bf16, const SeqTensors& t,
                                const void* out, const void* out_res, const float* lse,

@@ -267,50 +267,22 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   if (qok && hh == 0 && lse != nullptr)
     lse[row] = ltot == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(ltot)) * kLn2;
   if (!live) return;
-#pragma unroll
-  for (int part = 0; part < (RES ? 2 : 1); ++part) {
-    T* to = part == 0 ? out : out_res;
-    if constexpr (kThroughLds) {
-      // The wave's 32 rows through LDS (its own place, no other wave's), so that whole rows are
-      // written, 16 bytes per lane.
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int blk = 0; blk < 4; ++blk) {
-          __bf16 h[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float x = o[db][4 * blk + j] * inv;
-            h[j] = (__bf16)(part == 0 ? x : x - (float)(__bf16)x);
-          }
-          *reinterpret_cast<uint2*>(
-              lds + Rows::at(wave * 32 + (lane & 31), db * 32 + 8 * blk + 4 * hh)) =
-              __builtin_bit_cast(uint2, h);
-        }
-      constexpr int PER = 64 / Rows::KCH;  // rows per instruction
-#pragma unroll
-      for (int i = 0; i < 32 / PER; ++i) {
-        const int r = i * PER + lane / Rows::KCH, c = (lane % Rows::KCH) * 8;
-        const uint4 u = *reinterpret_cast<const uint4*>(lds + Rows::at(wave * 32 + r, c));
-        if (i0 + r < n)
-          *reinterpret_cast<uint4*>(to + ((int64_t)(sq.begin + i0 + r) * g.H + w.head) * D + c) = u;
-      }
-    } else if (qok) {
-#pragma unroll
-      for (int db = 0; db < DB; ++db) store_block(to + row * D, db, o[db], inv);
-    }
-  }
+  const int64_t first = ((int64_t)(sq.begin + i0) * g.H + w.head) * D, step = (int64_t)g.H * D;
+  store_rows<T, D>(lds + wave * 32 * D, o, inv, out + first, step, n - i0);
+  if constexpr (RES)
+    store_rows<T, D, true>(lds + wave * 32 * D, o, inv, out_res + first, step, n - i0);
 }
 
 // ---------------------------------------------------------------------------- backward
 
 // dq pass: 128 queries of one head against the keys they see,
 //   alpha = exp2(t - lse),  dP^T = V dout^T,  dS = alpha (dP - Delta),  dq^T += K^T dS^T,
-// and Delta = <dout, out + out_res>, kept for the dk/dv pass.  The bias gradient sums dS by
-// distance: distances inside the table in LDS, in an array of their own for each half of each
-// wave, where one instruction's 32 lanes have 32 different distances (queries i .. i + 31 and one
-// key), so that no two of its additions meet and the order of all is the program's; distances at
-// and beyond the ends in a register per lane.  The workgroup's sums by bucket go to `partial`.
+// and Delta = <dout, out + out_res>, kept with lse log2(e) for the dk/dv pass, head by head.  The
+// bias gradient sums dS by distance: distances inside the table in LDS, in an array of their own
+// for each half of each wave, where one instruction's 32 lanes have 32 different distances
+// (queries i .. i + 31 and one key), so that no two of its additions meet and the order of all is
+// the program's; distances at and beyond the ends in a register per lane.  The workgroup's sums by
+// bucket go to `partial`.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
@@ -319,13 +291,12 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
                    const int32_t* __restrict__ map, const T* __restrict__ out,
                    const T* __restrict__ out_res, const float* __restrict__ lse,
                    const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta,
-                   float* __restrict__ partial) {
+                   float* __restrict__ lse2_out, float* __restrict__ partial) {
   constexpr int KT = Type<T>::kKeyTile;
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
-  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32;
-  __shared__ __attribute__((aligned(16))) T Ks[2][Tl::kElems];
-  __shared__ __attribute__((aligned(16))) T Vs[2][Tl::kElems];
+  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
+  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
   extern __shared__ float tab[];  // bias by distance; 8 arrays of sums by distance; 8 x 2 ends
 
   Work w;
@@ -344,9 +315,22 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   const int nkeys = g.causal ? min(m, min(q0 + kSeqTile, n) + off) : m;
   const int ntiles = nkeys > 0 ? (nkeys + KT - 1) / KT : 0;
 
+  const T* kp = k + (int64_t)k0 * g.ks + w.u * D;
+  const T* vp = v + (int64_t)k0 * g.vs + w.u * D;
+  const uint32_t ksb = (uint32_t)g.ks * sizeof(T), vsb = (uint32_t)g.vs * sizeof(T);
+  uint32_t ko[Tl::NC], vo[Tl::NC];
+  Tl::copy_plan(ko, ksb);
+  Tl::copy_plan(vo, vsb);
+  auto fetch = [&](int kt, int buf) {
+    const int64_t at = (int64_t)kt * KT;
+    Tl::copy(lds + 2 * E * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
+    Tl::copy(lds + 2 * E * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
+  };
+  if (ntiles > 0) fetch(0, 0);
+
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int i0 = q0 + wave * 32, iq = i0 + (lane & 31);
-  const bool qok = iq < n;
+  const bool qok = iq < n, live = i0 < n;
   const int64_t qrow = sq.begin + (qok ? iq : 0), row = qrow * g.H + w.head;
   float* sums = tab + g.span + (wave * 2 + hh) * g.span;
   if constexpr (BIAS) {
@@ -375,12 +359,15 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
     }
     dl = pair_sum(part);
   }
-  if (qok && hh == 0) delta[row] = dl;
   // an empty row (lse = -inf) gets alpha = exp2(-inf) = 0
   const float lse_row = qok ? lse[row] : -INFINITY;
   const float lse2 = lse_row == -INFINITY ? INFINITY : lse_row * kLog2e;
+  if (qok && hh == 0) {
+    delta[(int64_t)w.head * g.nq + qrow] = dl;
+    lse2_out[(int64_t)w.head * g.nq + qrow] = lse2;
+  }
   const int last = g.causal ? min(m - 1, iq + off) : m - 1;
-  const int wave_last = i0 >= n ? -1 : g.causal ? min(m - 1, min(i0 + 31, n - 1) + off) : m - 1;
+  const int wave_last = !live ? -1 : g.causal ? min(m - 1, min(i0 + 31, n - 1) + off) : m - 1;
   const int all_see = g.causal ? min(m - 1, i0 + off) : m - 1;
 
   f32x16_t acc[DB];
@@ -388,42 +375,71 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
   float behind = 0.0f, ahead = 0.0f;
 
-  const T* kp = Tl::first_chunk(k + (int64_t)k0 * g.ks + w.u * D, g.ks);
-  const T* vp = Tl::first_chunk(v + (int64_t)k0 * g.vs + w.u * D, g.vs);
-  uint4 kr[Tl::NL], vr[Tl::NL];
-  if (ntiles > 0) {
-    Tl::load(kr, kp, g.ks, m);
-    Tl::load(vr, vp, g.vs, m);
-    Tl::store(Ks[0], kr);
-    Tl::store(Vs[0], vr);
-    if (ntiles > 1) {
-      Tl::load(kr, kp + KT * g.ks, g.ks, m - KT);
-      Tl::load(vr, vp + KT * g.vs, g.vs, m - KT);
+  // S^T = K Q^T and dP^T = V dout^T of a block
+  auto products = [&](const T* kc, int b, f32x16_t& sa, f32x16_t& pa) {
+    sa = f32x16_t{};
+    pa = f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sa = mfma(Tl::a_rows(kc, b * 32, ks), qf[ks], sa);
+      pa = mfma(Tl::a_rows(kc + E, b * 32, ks), gf[ks], pa);
     }
-  }
+  };
+  auto accumulate = [&](const T* kc, int b, const float (&ds)[16]) {
+    Frag df[2];
+    to_frags(ds, df);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        acc[db] = mfma(Tl::a_cols(kc, db * 32, b, p), df[p], acc[db]);
+  };
+  wait_copies();
   __syncthreads();
-  for (int kt = 0; kt < ntiles; ++kt) {
-    const T *kc = Ks[kt & 1], *vc = Vs[kt & 1];
-    if (kt + 1 < ntiles) {
-      Tl::store(Ks[(kt + 1) & 1], kr);
-      Tl::store(Vs[(kt + 1) & 1], vr);
+
+  // As in the forward: tiles that every query sees whole, the next block's products beside this
+  // block's vector work; then the tiles with a mask or a bias.
+  int kt = 0;
+  if constexpr (!BIAS) {
+    const int whole = q0 + kSeqTile <= n ? (g.causal ? min(m, max(q0 + off + 1, 0)) : m) / KT : 0;
+    f32x16_t sa, pa;
+    if (whole > 0) products(lds, 0, sa, pa);
+    auto tile = [&](int t, int buf) {
+      const T *kc = lds + 2 * E * buf, *kn = lds + 2 * E * (1 - buf);
+      if (t + 1 < ntiles) fetch(t + 1, 1 - buf);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        float ds[16];
+        const f32x16_t s0 = sa, p0 = pa;
+        if (b == NB - 1) {  // the next tile is in LDS
+          wait_copies();
+          __syncthreads();
+        }
+        if (b + 1 < NB) products(kc, b + 1, sa, pa);
+        else products(kn, 0, sa, pa);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          ds[i] = __builtin_amdgcn_exp2f(fmaf(s0[i], g.scale_log2, -lse2)) * (p0[i] - dl);
+        accumulate(kc, b, ds);
+      }
+      __syncthreads();
+    };
+    for (; kt + 1 < whole; kt += 2) {
+      tile(kt, 0);
+      tile(kt + 1, 1);
     }
-    if (kt + 2 < ntiles) {
-      const int at = (kt + 2) * KT;
-      Tl::load(kr, kp + at * g.ks, g.ks, m - at);
-      Tl::load(vr, vp + at * g.vs, g.vs, m - at);
-    }
+    if (kt < whole) tile(kt++, 0);
+  }
+  for (; kt < ntiles; ++kt) {
+    const T* kc = lds + 2 * E * (kt & 1);
+    if (kt + 1 < ntiles) fetch(kt + 1, (kt + 1) & 1);
     const int kbase = kt * KT;
     const int nb = wave_last < kbase ? 0 : min(NB, (wave_last - kbase) / 32 + 1);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       if (b >= nb) break;
-      f32x16_t sa = f32x16_t{}, pa = f32x16_t{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        sa = mfma(Tl::a_rows(kc, b * 32, ks), qf[ks], sa);
-        pa = mfma(Tl::a_rows(vc, b * 32, ks), gf[ks], pa);
-      }
+      f32x16_t sa, pa;
+      products(kc, b, sa, pa);
       const int kb = kbase + b * 32;
       float s[16], ds[16];
 #pragma unroll
@@ -465,22 +481,16 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
           }
         }
       }
-      Frag df[2];
-      to_frags(ds, df);
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-          acc[db] = mfma(Tl::a_cols(kc, db * 32, b, p), df[p], acc[db]);
+      accumulate(kc, b, ds);
     }
+    wait_copies();
     __syncthreads();
   }
-  if (qok) {
-#pragma unroll
-    for (int db = 0; db < DB; ++db) store_block(dq + row * D, db, acc[db], g.scale);
-  }
+  if (live)
+    store_rows<T, D>(lds + wave * 32 * D, acc, g.scale,
+                     dq + ((int64_t)(sq.begin + i0) * g.H + w.head) * D, (int64_t)g.H * D, n - i0);
   if (BIAS && partial != nullptr) {
-    // the lanes' ends join the wave's arrays lane by lane pairs in a fixed tree
+    // the lanes' ends join in a fixed tree
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
       behind += __shfl_xor(behind, d);
@@ -533,27 +543,29 @@ __global__ __launch_bounds__(256) void seq_table_kernel(int slots, int heads, in
 // dk/dv pass: 128 keys of one key head (wave w owns keys 32 w .. +31, lanes l and l ^ 32 share
 // key l % 32) against the queries that see them, head by head of the group:
 //   S = Q K^T,  dP = dout V^T,  dv^T += dout^T alpha,  dk^T += Q^T dS.
-template <typename T, int D, bool BIAS, bool DK, bool DV>
+// With PARTS the (head, query tile) pairs of a key tile are dealt out to several workgroups,
+// whose float32 sums seq_join_kernel adds.
+template <typename T, int D, bool BIAS, bool PARTS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
-    sizeof(T) == 2 && !(DK && DV && D == 128) ? 2 : 1, 2)))
+    sizeof(T) == 2 && D == 64 ? 2 : 1, sizeof(T) == 2 && D == 64 ? 2 : 1)))
 void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                      const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                      const int32_t* __restrict__ cu_k, const float* __restrict__ table,
-                     const int32_t* __restrict__ map, const float* __restrict__ lse,
-                     const T* __restrict__ dout, const float* __restrict__ delta,
-                     T* __restrict__ dk, T* __restrict__ dv) {
+                     const int32_t* __restrict__ map, const float* __restrict__ delta,
+                     const float* __restrict__ lse2, const T* __restrict__ dout,
+                     T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ part_dk,
+                     float* __restrict__ part_dv) {
   constexpr int QT = Type<T>::kKeyTile;
   using Tl = Tile<T, D, QT>;
   using Frag = typename Type<T>::Frag;
-  constexpr int KS = D / 16, DB = D / 32, NB = QT / 32;
-  __shared__ __attribute__((aligned(16))) T Qs[2][Tl::kElems];
-  __shared__ __attribute__((aligned(16))) T Gs[2][Tl::kElems];
-  __shared__ __attribute__((aligned(16))) float Ls[2][QT];  // lse log2(e); +inf where none
-  __shared__ __attribute__((aligned(16))) float Dl[2][QT];  // Delta
+  constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
+  __shared__ __attribute__((aligned(16))) T lds[4 * E];     // queries, douts of tile 0, of tile 1
+  __shared__ __attribute__((aligned(16))) float stat[2][2][64];  // lse log2(e), Delta of a tile
   extern __shared__ float tab[];
 
   Work w;
-  if (!work_of(g.k_tiles, 1, w)) return;
+  if (!work_of(g.k_tiles, PARTS ? g.parts : 1, w)) return;
+  const int part = PARTS ? w.head - w.u * g.parts : 0;
   const Slot sk = find_slot<kSeqTile>(cu_k, g.B, g.nk, 1, w.slot);
   const int k0 = sk.tile * kSeqTile, m = sk.end - sk.begin;
   if (k0 >= m) return;
@@ -562,127 +574,201 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   const int off = m - n;
   const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;  // first tile with a query that sees
   const int per_head = n > q_first ? (n - q_first + QT - 1) / QT : 0;
-  const int ntiles = per_head * g.group;
+  const int all = per_head * g.group;
+  const int t0 = PARTS ? (int)((int64_t)all * part / g.parts) : 0;
+  const int t1 = PARTS ? (int)((int64_t)all * (part + 1) / g.parts) : all;
 
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
+  const uint32_t qsb = (uint32_t)g.qs * sizeof(T), gsb = (uint32_t)g.H * Tl::kRowBytes;
+  uint32_t qo[Tl::NC], go[Tl::NC];
+  Tl::copy_plan(qo, qsb);
+  Tl::copy_plan(go, gsb);
+  auto fetch = [&](int it, int buf) {
+    const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
+    const int64_t row = qbeg + at;
+    Tl::copy(lds + 2 * E * buf, q + row * g.qs + head * D, qo, qsb, n - at);
+    Tl::copy(lds + 2 * E * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
+    if (wave < 2)  // 64 rows' statistics, past the tile's end as far as there are rows
+      copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
+             (uint32_t)min((int64_t)lane, g.nq - 1 - row) * 4u, (int64_t)head * g.nq + row);
+  };
+  if (t0 < t1) fetch(t0, 0);
+
   const int j0 = k0 + wave * 32, jk = j0 + (lane & 31);
-  const bool kok = jk < m;
+  const bool kok = jk < m, live = j0 < m;
   const int64_t krow = sk.begin + (kok ? jk : 0);
   Frag kf[KS], vf[KS];
   load_frag<T, D>(kf, k + krow * g.ks + w.u * D, kok);
-  if constexpr (DK) load_frag<T, D>(vf, v + krow * g.vs + w.u * D, kok);
+  load_frag<T, D>(vf, v + krow * g.vs + w.u * D, kok);
 
   f32x16_t dka[DB], dva[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) dka[db] = dva[db] = f32x16_t{};
 
-  uint4 rq[Tl::NL], rg[Tl::NL];
-  float ls = INFINITY, de = 0.0f;
-  auto fetch = [&](int it) {
-    const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
-    const int64_t row = qbeg + at, gs = (int64_t)g.H * D;
-    Tl::load(rq, Tl::first_chunk(q + row * g.qs + head * D, g.qs), g.qs, n - at);
-    Tl::load(rg, Tl::first_chunk(dout + row * gs + head * D, gs), gs, n - at);
-    if (threadIdx.x < QT) {
-      const bool ok = at + (int)threadIdx.x < n;
-      const int64_t r = (row + (ok ? threadIdx.x : 0)) * g.H + head;
-      const float x = ok ? lse[r] : -INFINITY;
-      ls = x == -INFINITY ? INFINITY : x * kLog2e;
-      de = ok && DK ? delta[r] : 0.0f;
+  // S = Q K^T and dP = dout V^T of a block: the operands are read together, then multiplied
+  auto products = [&](const T* qc, int b, f32x16_t& sa, f32x16_t& pa) {
+    Frag aq[KS], ag[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      aq[ks] = Tl::a_rows(qc, b * 32, ks);
+      ag[ks] = Tl::a_rows(qc + E, b * 32, ks);
+    }
+    sa = f32x16_t{};
+    pa = f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      sa = mfma(aq[ks], kf[ks], sa);
+      pa = mfma(ag[ks], vf[ks], pa);
     }
   };
-  auto stage = [&](int buf) {
-    Tl::store(Qs[buf], rq);
-    Tl::store(Gs[buf], rg);
-    if (threadIdx.x < QT) {
-      Ls[buf][threadIdx.x] = ls;
-      Dl[buf][threadIdx.x] = de;
+  // alpha in place of the logits (base 2 where there is a bias), and dS
+  auto weigh = [&](int buf, int b, float (&s)[16], const f32x16_t& pa, float (&ds)[16]) {
+#pragma unroll
+    for (int blk = 0; blk < 4; ++blk) {
+      const int at = b * 32 + 8 * blk + 4 * hh;
+      const float4 l4 = *reinterpret_cast<const float4*>(&stat[buf][0][at]);
+      const float4 d4 = *reinterpret_cast<const float4*>(&stat[buf][1][at]);
+      const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * blk + j;
+        s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - lv[j] : fmaf(s[i], g.scale_log2, -lv[j]));
+        ds[i] = s[i] * (pa[i] - dl[j]);
+      }
     }
   };
-  if (ntiles > 0) {
-    fetch(0);
-    stage(0);
-    if (ntiles > 1) fetch(1);
-  }
-  for (int it = 0; it < ntiles; ++it) {
+  auto accumulate = [&](const T* qc, int b, const float (&p)[16], const float (&ds)[16]) {
+    Frag pf[2], df[2];
+    to_frags(p, pf);
+    to_frags(ds, df);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        dva[db] = mfma(Tl::a_cols(qc + E, db * 32, b, i), pf[i], dva[db]);
+        dka[db] = mfma(Tl::a_cols(qc, db * 32, b, i), df[i], dka[db]);
+      }
+  };
+  wait_copies();
+
+  int it = t0;
+  while (it < t1) {
+    const int in_head = it % per_head, qbase = q_first + in_head * QT;
     if constexpr (BIAS) {
-      if (it % per_head == 0) {
+      if (it == t0 || in_head == 0) {
         __syncthreads();  // the previous head's table is no longer read
         fill_bias(tab, g, table, map, w.u * g.group + it / per_head);
       }
     }
     __syncthreads();
-    const T *Qc = Qs[it & 1], *Gc = Gs[it & 1];
-    const float *Lc = Ls[it & 1], *Dc = Dl[it & 1];
-    if (it + 1 < ntiles) stage((it + 1) & 1);
-    if (it + 2 < ntiles) fetch(it + 2);
-    const int qbase = q_first + it % per_head * QT;
+    // Tiles of this head whose queries all exist and see all of the workgroup's keys, without a
+    // bias: the next block's products beside this block's vector work.
+    // (From an even tile on, so that the LDS buffers' places are constants.)
+    const int to_end = min(t1 - it, (n - qbase) / QT);  // full tiles up to the head's end
+    if (!BIAS && sizeof(T) == 2 && to_end > 0 && ((it - t0) & 1) == 0 &&
+        (!g.causal || qbase + off >= k0 + kSeqTile - 1)) {
+      f32x16_t sa, pa;
+      auto tile = [&](int t, int buf) {
+        const T *qc = lds + 2 * E * buf, *qn = lds + 2 * E * (1 - buf);
+        if (t + 1 < t1) fetch(t + 1, 1 - buf);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          float s[16], ds[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = sa[i];
+          const f32x16_t p0 = pa;
+          if (b == NB - 1) {  // the next tile is in LDS
+            wait_copies();
+            __syncthreads();
+          }
+          if (b + 1 < NB) products(qc, b + 1, sa, pa);
+          else products(qn, 0, sa, pa);
+          weigh(buf, b, s, p0, ds);
+          accumulate(qc, b, s, ds);
+        }
+        __syncthreads();
+      };
+      products(lds, 0, sa, pa);
+      const int end = it + to_end;
+      for (; it + 1 < end; it += 2) {
+        tile(it, 0);
+        tile(it + 1, 1);
+      }
+      if (it < end) tile(it++, 0);
+      continue;
+    }
+    const int buf = (it - t0) & 1;
+    const T* qc = lds + 2 * E * buf;
+    if (it + 1 < t1) fetch(it + 1, 1 - buf);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int qb = qbase + b * 32;
-      if (qb >= n || j0 >= m || (g.causal && qb + 31 + off < j0)) continue;
-      f32x16_t sa = f32x16_t{}, pa = f32x16_t{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        sa = mfma(Tl::a_rows(Qc, b * 32, ks), kf[ks], sa);
-        if constexpr (DK) pa = mfma(Tl::a_rows(Gc, b * 32, ks), vf[ks], pa);
-      }
+      if (qb >= n || !live || (g.causal && qb + 31 + off < j0)) continue;
+      f32x16_t sa, pa;
+      products(qc, b, sa, pa);
       float s[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = sa[i];
       if constexpr (BIAS)
         add_bias(s, g, tab, j0 - (qb + 31 + off), j0 + 31 - (qb + off),
                  [&](int i) { return jk - qb - c_row(i, hh) - off; });
-#pragma unroll
-      for (int blk = 0; blk < 4; ++blk) {
-        const float4 l4 = *reinterpret_cast<const float4*>(Lc + b * 32 + 8 * blk + 4 * hh);
-        const float4 d4 = *reinterpret_cast<const float4*>(Dc + b * 32 + 8 * blk + 4 * hh);
-        const float lv[4] = {l4.x, l4.y, l4.z, l4.w}, dl[4] = {d4.x, d4.y, d4.z, d4.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int i = 4 * blk + j;
-          s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - lv[j] : fmaf(s[i], g.scale_log2, -lv[j]));
-          if constexpr (DK) ds[i] = s[i] * (pa[i] - dl[j]);
-        }
-      }
+      weigh(buf, b, s, pa, ds);
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
         // queries before the key, and rows past the sequence's end
         asm volatile("");
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int iq = qb + c_row(i, hh);
-          if (iq >= n || (g.causal && iq + off < jk)) {
-            s[i] = 0.0f;
-            if constexpr (DK) ds[i] = 0.0f;
-          }
+          if (iq >= n || (g.causal && iq + off < jk)) s[i] = ds[i] = 0.0f;
         }
       }
-      if constexpr (DV) {
-        Frag pf[2];
-        to_frags(s, pf);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            dva[db] = mfma(Tl::a_cols(Gc, db * 32, b, p), pf[p], dva[db]);
-      }
-      if constexpr (DK) {
-        Frag df[2];
-        to_frags(ds, df);
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int p = 0; p < 2; ++p)
-            dka[db] = mfma(Tl::a_cols(Qc, db * 32, b, p), df[p], dka[db]);
-      }
+      accumulate(qc, b, s, ds);
     }
+    wait_copies();
+    ++it;
   }
-  if (!kok) return;
-  const int64_t row = (krow * g.KH + w.u) * D;
+  __syncthreads();
+  if (!live) return;
+  if constexpr (PARTS) {
+    if (!kok) return;
+    const int64_t row = (((int64_t)part * g.nk + krow) * g.KH + w.u) * D;
 #pragma unroll
-  for (int db = 0; db < DB; ++db) {
-    if constexpr (DK) store_block(dk + row, db, dka[db], g.scale);
-    if constexpr (DV) store_block(dv + row, db, dva[db], 1.0f);
+    for (int db = 0; db < DB; ++db) {
+      store_block(part_dk + row, db, dka[db], g.scale);
+      store_block(part_dv + row, db, dva[db], 1.0f);
+    }
+  } else {
+    const int64_t first = ((int64_t)(sk.begin + j0) * g.KH + w.u) * D, step = (int64_t)g.KH * D;
+    store_rows<T, D>(lds + wave * 32 * D, dka, g.scale, dk + first, step, m - j0);
+    store_rows<T, D>(lds + wave * 32 * D, dva, 1.0f, dv + first, step, m - j0);
+  }
+}
+
+// Adds the parts of dk and dv in their order and rounds: four values per thread, `count` groups of
+// four in each part.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void seq_join_kernel(int64_t count, int parts,
+                                                            const float4* __restrict__ part_dk,
+                                                            const float4* __restrict__ part_dv,
+                                                            T* __restrict__ dk,
+                                                            T* __restrict__ dv) {
+  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= count) return;
+  const float4* from = blockIdx.y == 0 ? part_dk : part_dv;
+  T* to = (blockIdx.y == 0 ? dk : dv) + i * 4;
+  float4 sum = from[i];
+  for (int p = 1; p < parts; ++p) {
+    const float4 x = from[p * count + i];
+    sum.x += x.x;
+    sum.y += x.y;
+    sum.z += x.z;
+    sum.w += x.w;
+  }
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(to) = sum;
+  } else {
+    const uint16_t h[4] = {to_bf16(sum.x), to_bf16(sum.y), to_bf16(sum.z), to_bf16(sum.w)};
+    *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, h);
   }
 }
 
@@ -731,35 +817,63 @@ hipError_t forward_d(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
 
 size_t round_256(size_t x) { return (x + 255) & ~size_t(255); }
 
+// The backward's workspace: Delta and lse log2(e) [heads][rows], the bias gradient's bucket sums,
+// and the parts of dk and dv.
+struct Workspace {
+  size_t lse2, partial, part_dk, part_dv, bytes;
+};
+Workspace workspace_of(const SeqGeometry& g, bool want_table) {
+  Workspace w;
+  size_t at = round_256((size_t)g.nq * g.H * 4);
+  w.lse2 = at;
+  at *= 2;
+  w.partial = at;
+  if (want_table) at += round_256((size_t)g.q_tiles.slots * g.H * g.nb * 4);
+  w.part_dk = at;
+  const size_t part = g.parts > 1 ? round_256((size_t)g.parts * g.nk * g.KH * g.D * 4) : 0;
+  w.part_dv = at + part;
+  w.bytes = at + 2 * part;
+  return w;
+}
+
 template <typename T, int D>
 hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, const T* res,
                       const float* lse, const T* dout, T* dq, T* dk, T* dv, float* d_table,
                       void* workspace, hipStream_t s) {
-  const bool bias = g.nb > 0;
+  const bool bias = g.nb > 0, want_table = bias && d_table != nullptr;
   const T *q = (const T*)t.q, *k = (const T*)t.k, *v = (const T*)t.v;
-  float* delta = (float*)workspace;
-  float* partial = bias && d_table != nullptr
-                       ? (float*)((char*)workspace + round_256((size_t)g.nq * g.H * 4))
-                       : nullptr;
+  const Workspace at = workspace_of(g, want_table);
+  char* ws = (char*)workspace;
+  float *delta = (float*)ws, *lse2 = (float*)(ws + at.lse2);
+  float* partial = want_table ? (float*)(ws + at.partial) : nullptr;
+  float* part_dk = g.parts > 1 ? (float*)(ws + at.part_dk) : nullptr;
+  float* part_dv = g.parts > 1 ? (float*)(ws + at.part_dv) : nullptr;
   hipError_t e = hipSuccess;
   if (g.nq > 0) {
     const void* fn = bias ? (const void*)&seq_dq_kernel<T, D, true>
                           : (const void*)&seq_dq_kernel<T, D, false>;
     const size_t lds = !bias ? 0 : partial ? (size_t)g.span * 36 + 64 : (size_t)g.span * 4;
-    e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), kThreads, lds, s, g, q, k, v, t.cu_q,
-               t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, partial);
+    e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), kThreads, lds, s, g, q, k, v,
+               t.cu_q, t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, lse2, partial);
   }
-  if (e == hipSuccess && bias && d_table != nullptr)
-    e = launch((const void*)&seq_table_kernel, dim3(g.H), kThreads, 0, s, g.nq > 0 ? g.q_tiles.slots : 0,
-               g.H, g.nb, (const float*)partial, d_table);
+  if (e == hipSuccess && want_table)
+    e = launch((const void*)&seq_table_kernel, dim3(g.H), kThreads, 0, s,
+               g.nq > 0 ? g.q_tiles.slots : 0, g.H, g.nb, (const float*)partial, d_table);
   if (e == hipSuccess && g.nk > 0) {
-    const dim3 grid((unsigned)seq_blocks(g.k_tiles, 1));
-    const size_t lds = bias ? (size_t)g.span * 4 : 0;
-    const float* cdelta = delta;
-    const void* fn = bias ? (const void*)&seq_dkdv_kernel<T, D, true, true, true>
-                          : (const void*)&seq_dkdv_kernel<T, D, false, true, true>;
-    e = launch(fn, grid, kThreads, lds, s, g, q, k, v, t.cu_q, t.cu_k, t.table, t.map, lse, dout, cdelta,
-               dk, dv);
+    const dim3 grid((unsigned)seq_blocks(g.k_tiles, g.parts));
+    const void* fn = g.parts > 1 ? (bias ? (const void*)&seq_dkdv_kernel<T, D, true, true>
+                                         : (const void*)&seq_dkdv_kernel<T, D, false, true>)
+                                 : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
+                                         : (const void*)&seq_dkdv_kernel<T, D, false, false>);
+    e = launch(fn, grid, kThreads, bias ? (size_t)g.span * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
+               t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
+               part_dv);
+  }
+  if (e == hipSuccess && g.nk > 0 && g.parts > 1) {
+    const int64_t count = (int64_t)g.nk * g.KH * D / 4;
+    e = launch((const void*)&seq_join_kernel<T>,
+               dim3((unsigned)((count + kThreads - 1) / kThreads), 2), kThreads, 0, s, count,
+               g.parts, (const float4*)part_dk, (const float4*)part_dv, dk, dv);
   }
   return e;
 }
@@ -786,10 +900,17 @@ hipError_t launch_seq_forward(const SeqGeometry& g, bool bf16, const SeqTensors&
                    : forward_d<float, 128>(g, t, (float*)out, nullptr, lse, s);
 }
 
+// Parts of the dk/dv pass.  Key heads x key tiles workgroups do the work of all heads of a group;
+// where they are fewer than two per compute unit, the (head, query tile) pairs are dealt out to up
+// to 16 parts.  Key tiles are estimated from the rows and sequences.
+int seq_backward_parts(const SeqGeometry& g) {
+  const int64_t blocks = (int64_t)g.KH * std::max<int64_t>(1, g.nk / kSeqTile);
+  const int64_t most = std::min<int64_t>(16, (int64_t)g.group * std::max(1, g.nq / g.B / 256));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(512 / blocks, most));
+}
+
 size_t seq_backward_workspace(const SeqGeometry& g, bool want_table) {
-  size_t need = round_256((size_t)g.nq * g.H * 4);
-  if (want_table) need += round_256((size_t)g.q_tiles.slots * g.H * g.nb * 4);
-  return need;
+  return workspace_of(g, want_table).bytes;
 }
 
 hipError_t launch_seq_backward(const SeqGeometry& g, bool bf16, const SeqTensors& t,
