@@ -34,11 +34,13 @@ struct Type;
 template <>
 struct Type<uint16_t> {  // bf16 bit patterns
   using Frag = bf16x8_t;
+  using Alpha = _Float16;  // how one wave hands weights to another
   static constexpr int kKeyTile = 64;
 };
 template <>
 struct Type<float> {
   using Frag = F32x8;
+  using Alpha = float;
   static constexpr int kKeyTile = 32;
 };
 
@@ -293,6 +295,43 @@ __device__ inline void to_low_frags(const float (&x)[16], const bf16x8_t (&hi)[2
     for (int e = 0; e < 8; ++e) lo[p][e] = (__bf16)(x[8 * p + e] - (float)hi[p][e]);
 }
 
+// Sixteen values of a lane to LDS and back.
+__device__ inline void hand_over(_Float16* to, const float (&x)[16]) {
+  typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    f16x8_t h;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) h[e] = (_Float16)x[8 * p + e];
+    *reinterpret_cast<f16x8_t*>(to + 8 * p) = h;
+  }
+}
+__device__ inline void take_over(const _Float16* from, float (&x)[16]) {
+  typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const f16x8_t h = *reinterpret_cast<const f16x8_t*>(from + 8 * p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[8 * p + e] = (float)h[e];
+  }
+}
+__device__ inline void hand_over(float* to, const float (&x)[16]) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p)
+    *reinterpret_cast<float4*>(to + 4 * p) =
+        make_float4(x[4 * p], x[4 * p + 1], x[4 * p + 2], x[4 * p + 3]);
+}
+__device__ inline void take_over(const float* from, float (&x)[16]) {
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const float4 y = *reinterpret_cast<const float4*>(from + 4 * p);
+    x[4 * p] = y.x;
+    x[4 * p + 1] = y.y;
+    x[4 * p + 2] = y.z;
+    x[4 * p + 3] = y.w;
+  }
+}
+
 // Stores 16 values of channel block db (channels 32 db + 8 blk + 4 (l / 32) + j) times mul.
 __device__ inline void store_block(float* row, int db, const f32x16_t& acc, float mul) {
   const int hh = (threadIdx.x & 63) >> 5;
@@ -418,17 +457,19 @@ __device__ inline float bias_of(const float* table, const int32_t* map, int head
 // Block -> (key head, slot, head within the group).  Blocks go to XCD x % 8, so the blocks of a
 // key head stay on one XCD, whose L2 then serves its keys and values; with key heads that the 8
 // XCDs do not share evenly, each head's tiles are dealt out over `parts` of them, so that early
-// and late tiles (short and long ones under a causal mask) fall on each.  Late tiles come first.
+// and late tiles (short and long ones under a causal mask) fall on each.  The long ones come first:
+// late tiles of queries, early tiles of keys.
 struct Work {
   int u, slot, head;
 };
+template <bool LATE_FIRST = true>
 __device__ inline bool work_of(const Spread& sp, int per, Work& w) {
   const int x = blockIdx.x % 8;
   int r = blockIdx.x / 8;
   const int j = r % per;
   r /= per;
   const int su = (r % sp.local) * 8 + x;
-  const int rank = sp.ranks - 1 - r / sp.local;
+  const int rank = LATE_FIRST ? sp.ranks - 1 - r / sp.local : r / sp.local;
   w.u = su % sp.units;
   w.slot = rank * sp.parts + su / sp.units;
   w.head = w.u * per + j;

@@ -244,9 +244,10 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
                  [&](int i) { return kb + c_row(i, hh) - iq - off; });
       if (kb + 31 > all_see) {
         asm volatile("");  // a branch: blocks that every query sees do not pay for it
+        const int seen = last - kb - 4 * hh;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (kb + c_row(i, hh) > last) s[i] = -INFINITY;
+          if (c_row(i, 0) > seen) s[i] = -INFINITY;
       }
       raise_to(s);
       weigh(s, ph);
@@ -455,9 +456,10 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
       }
       if (kb + 31 > all_see || i0 + 31 >= n) {
         asm volatile("");
+        const int seen = qok ? last - kb - 4 * hh : -1;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (kb + c_row(i, hh) > last || !qok) ds[i] = 0.0f;
+          if (c_row(i, 0) > seen) ds[i] = 0.0f;
       }
       if (BIAS && partial != nullptr) {
         const int end = g.span - 1;
@@ -540,14 +542,13 @@ __global__ __launch_bounds__(256) void seq_table_kernel(int slots, int heads, in
   }
 }
 
-// dk/dv pass: 128 keys of one key head (wave w owns keys 32 w .. +31, lanes l and l ^ 32 share
-// key l % 32) against the queries that see them, head by head of the group:
+// dk/dv pass at 64 channels: 128 keys of one key head (wave w owns keys 32 w .. +31, lanes l and
+// l ^ 32 share key l % 32) against the queries that see them, head by head of the group:
 //   S = Q K^T,  dP = dout V^T,  dv^T += dout^T alpha,  dk^T += Q^T dS.
 // With PARTS the (head, query tile) pairs of a key tile are dealt out to several workgroups,
 // whose float32 sums seq_join_kernel adds.
 template <typename T, int D, bool BIAS, bool PARTS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(
-    sizeof(T) == 2 && D == 64 ? 2 : 1, sizeof(T) == 2 && D == 64 ? 2 : 1)))
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                      const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                      const int32_t* __restrict__ cu_k, const float* __restrict__ table,
@@ -564,7 +565,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   extern __shared__ float tab[];
 
   Work w;
-  if (!work_of(g.k_tiles, PARTS ? g.parts : 1, w)) return;
+  if (!work_of<false>(g.k_tiles, PARTS ? g.parts : 1, w)) return;
   const int part = PARTS ? w.head - w.u * g.parts : 0;
   const Slot sk = find_slot<kSeqTile>(cu_k, g.B, g.nk, 1, w.slot);
   const int k0 = sk.tile * kSeqTile, m = sk.end - sk.begin;
@@ -588,9 +589,9 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     const int64_t row = qbeg + at;
     Tl::copy(lds + 2 * E * buf, q + row * g.qs + head * D, qo, qsb, n - at);
     Tl::copy(lds + 2 * E * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
-    if (wave < 2)  // 64 rows' statistics, past the tile's end as far as there are rows
+    if (wave < 2)  // the rows' statistics; past the sequence's end the last row's
       copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
-             (uint32_t)min((int64_t)lane, g.nq - 1 - row) * 4u, (int64_t)head * g.nq + row);
+             (uint32_t)min(lane, n - at - 1) * 4u, (int64_t)head * g.nq + row);
   };
   if (t0 < t1) fetch(t0, 0);
 
@@ -716,11 +717,10 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
         // queries before the key, and rows past the sequence's end
         asm volatile("");
+        const int from = g.causal ? jk - off - qb - 4 * hh : 0, to = n - qb - 4 * hh;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int iq = qb + c_row(i, hh);
-          if (iq >= n || (g.causal && iq + off < jk)) s[i] = ds[i] = 0.0f;
-        }
+        for (int i = 0; i < 16; ++i)
+          if (c_row(i, 0) < from || c_row(i, 0) >= to) s[i] = ds[i] = 0.0f;
       }
       accumulate(qc, b, s, ds);
     }
@@ -741,6 +741,203 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     const int64_t first = ((int64_t)(sk.begin + j0) * g.KH + w.u) * D, step = (int64_t)g.KH * D;
     store_rows<T, D>(lds + wave * 32 * D, dka, g.scale, dk + first, step, m - j0);
     store_rows<T, D>(lds + wave * 32 * D, dva, 1.0f, dv + first, step, m - j0);
+  }
+}
+
+// dk/dv pass at 128 channels, where a wave has no room for both sums: two waves share 32 keys (lanes l and l ^ 32 of each share key l % 32):
+//   waves 0 - 3:  S = Q K^T,  alpha,  dv^T += dout^T alpha
+//   waves 4 - 7:  dP = dout V^T,  dS = alpha (dP - Delta),  dk^T += Q^T dS
+// so that each has one operand and one sum in registers (two waves per SIMD) and two of the four
+// products.  The second takes alpha from the first through LDS, one query tile later: float16 of
+// 2^14 alpha (11 bits down to 2^-28), which is what its lanes hold of the same block.  Measured
+// for 8,192 tokens, 16 heads x 128, all keys: both sums in one wave, one wave per SIMD, 1.44 ms
+// (matrix cores 30% busy); in one wave at two waves per SIMD, operands read as they are used,
+// 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this 1.18 ms (40% busy).
+constexpr float kAlphaScale = 14.0f;  // base 2
+
+template <typename T, bool BIAS, bool PARTS>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
+                     const T* __restrict__ v, const int32_t* __restrict__ cu_q,
+                     const int32_t* __restrict__ cu_k, const float* __restrict__ table,
+                     const int32_t* __restrict__ map, const float* __restrict__ delta,
+                     const float* __restrict__ lse2, const T* __restrict__ dout,
+                     T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ part_dk,
+                     float* __restrict__ part_dv) {
+  constexpr int D = 128, QT = Type<T>::kKeyTile;
+  using Tl = Tile<T, D, QT, 512>;
+  using Frag = typename Type<T>::Frag;
+  using Alpha = typename Type<T>::Alpha;
+  constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
+  // three tiles of queries and douts: the first waves', the second waves', the next
+  __shared__ __attribute__((aligned(16))) T lds[6 * E];
+  __shared__ __attribute__((aligned(16))) Alpha alpha[3][NB][4][64][16];
+  __shared__ __attribute__((aligned(16))) float stat[3][2][64];  // lse log2(e), Delta of a tile
+  extern __shared__ float tab[];
+
+  Work w;
+  if (!work_of<false>(g.k_tiles, PARTS ? g.parts : 1, w)) return;
+  const int part = PARTS ? w.head - w.u * g.parts : 0;
+  const Slot sk = find_slot<kSeqTile>(cu_k, g.B, g.nk, 1, w.slot);
+  const int k0 = sk.tile * kSeqTile, m = sk.end - sk.begin;
+  if (k0 >= m) return;
+  int qbeg, n;
+  key_rows(cu_q, sk.b, g.B, g.nq, qbeg, n);
+  const int off = m - n;
+  const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;  // first tile with a query that sees
+  const int per_head = n > q_first ? (n - q_first + QT - 1) / QT : 0;
+  const int all = per_head * g.group;
+  const int t0 = PARTS ? (int)((int64_t)all * part / g.parts) : 0;
+  const int t1 = PARTS ? (int)((int64_t)all * (part + 1) / g.parts) : all;
+
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
+  const uint32_t qsb = (uint32_t)g.qs * sizeof(T), gsb = (uint32_t)g.H * Tl::kRowBytes;
+  uint32_t qo[Tl::NC], go[Tl::NC];
+  Tl::copy_plan(qo, qsb);
+  Tl::copy_plan(go, gsb);
+  auto fetch = [&](int it, int buf) {
+    const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
+    const int64_t row = qbeg + at;
+    Tl::copy(lds + 2 * E * buf, q + row * g.qs + head * D, qo, qsb, n - at);
+    Tl::copy(lds + 2 * E * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
+    if (wave < 2)  // the rows' statistics; past the sequence's end the last row's
+      copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
+             (uint32_t)min(lane, n - at - 1) * 4u, (int64_t)head * g.nq + row);
+  };
+  if (t0 < t1) fetch(t0, 0);
+
+  const int pair = wave & 3;
+  const bool second = wave >= 4;
+  const int j0 = k0 + pair * 32, jk = j0 + (lane & 31);
+  const bool kok = jk < m, live = j0 < m;
+  const int64_t krow = sk.begin + (kok ? jk : 0);
+  Frag wf[KS];  // K or V
+  load_frag<T, D>(wf, (second ? v + krow * g.vs : k + krow * g.ks) + w.u * D, kok);
+  f32x16_t sum[DB];  // dv or dk
+#pragma unroll
+  for (int db = 0; db < DB; ++db) sum[db] = f32x16_t{};
+  wait_copies();
+
+  // x of a block: S or dP
+  auto products = [&](const T* rows, int b) {
+    f32x16_t x = f32x16_t{};
+    if constexpr (sizeof(T) == 2) {
+      Frag a[KS];
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(rows, b * 32, ks);
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) x = mfma(a[ks], wf[ks], x);
+    } else {  // no room for them all
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        x = mfma(Tl::a_rows(rows, b * 32, ks), wf[ks], x);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    return x;
+  };
+  // Block b of tile `mine` in LDS buffer `buf`; qb: its first query.
+  auto block = [&](int buf, int b, int qb, const f32x16_t& x) {
+    const T* cols = lds + 2 * E * buf + (second ? 0 : E);
+    float y[16];
+    const float* st = &stat[buf][second ? 1 : 0][b * 32 + 4 * hh];
+    Alpha* al = alpha[buf][b][pair][lane];
+    if (!second) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = x[i];
+      if constexpr (BIAS)
+        add_bias(y, g, tab, j0 - (qb + 31 + off), j0 + 31 - (qb + off),
+                 [&](int i) { return jk - qb - c_row(i, hh) - off; });
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        const float4 l4 = *reinterpret_cast<const float4*>(st + 8 * blk);
+        const float lv[4] = {l4.x, l4.y, l4.z, l4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int i = 4 * blk + j;
+          const float at = kAlphaScale - lv[j];
+          y[i] = __builtin_amdgcn_exp2f(BIAS ? y[i] + at : fmaf(y[i], g.scale_log2, at));
+        }
+      }
+      if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
+        // queries before the key, and rows past the sequence's end
+        asm volatile("");
+        const int from = g.causal ? jk - off - qb - 4 * hh : 0, to = n - qb - 4 * hh;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (c_row(i, 0) < from || c_row(i, 0) >= to) y[i] = 0.0f;
+      }
+      hand_over(al, y);
+    } else {
+      take_over(al, y);
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        const float4 d4 = *reinterpret_cast<const float4*>(st + 8 * blk);
+        const float dl[4] = {d4.x, d4.y, d4.z, d4.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[4 * blk + j] *= x[4 * blk + j] - dl[j];
+      }
+    }
+    Frag f[2];
+    to_frags(y, f);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        sum[db] = mfma(Tl::a_cols(cols, db * 32, b, p), f[p], sum[db]);
+  };
+
+  // Step i: the first waves work on tile t0 + i, the second ones on the tile before it.  Tile i is
+  // in buffer i % 3, which the calls below have as a constant.
+  const int steps = t1 - t0;
+  auto run = [&](int step, int in, int out, int next) {
+    __syncthreads();
+    if constexpr (BIAS) {
+      if (step < steps && (step == 0 || (t0 + step) % per_head == 0)) {
+        fill_bias<512>(tab, g, table, map, w.u * g.group + (t0 + step) / per_head);
+        __syncthreads();
+      }
+    }
+    if (step + 1 < steps) fetch(t0 + step + 1, next);
+    auto tile = [&](int mine, int buf) {
+      const int qb = q_first + (t0 + mine) % per_head * QT;
+      if (g.causal && qb + QT - 1 + off < j0) return;  // the same for both waves
+      const T* rows = lds + 2 * E * buf + (second ? E : 0);
+      f32x16_t x = products(rows, 0);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f32x16_t y = f32x16_t{};
+        if (b + 1 < NB) y = products(rows, b + 1);
+        block(buf, b, qb + b * 32, x);
+        x = y;
+      }
+    };
+    if (live) {
+      if (!second) {
+        if (step < steps) tile(step, in);
+      } else if (step > 0) {
+        tile(step - 1, out);
+      }
+    }
+    wait_copies();
+  };
+  for (int step = 0; step <= steps; step += 3) {
+    run(step, 0, 2, 1);
+    if (step + 1 <= steps) run(step + 1, 1, 0, 2);
+    if (step + 2 <= steps) run(step + 2, 2, 1, 0);
+  }
+  __syncthreads();
+  if (!live) return;
+  const float mul = (second ? g.scale : 1.0f) * 0x1p-14f;
+  if constexpr (PARTS) {
+    if (!kok) return;
+    float* to = (second ? part_dk : part_dv) + (((int64_t)part * g.nk + krow) * g.KH + w.u) * D;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) store_block(to, db, sum[db], mul);
+  } else {
+    store_rows<T, D>(lds + wave * 32 * D, sum, mul,
+                     (second ? dk : dv) + ((int64_t)(sk.begin + j0) * g.KH + w.u) * D,
+                     (int64_t)g.KH * D, m - j0);
   }
 }
 
@@ -861,11 +1058,19 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
                g.nq > 0 ? g.q_tiles.slots : 0, g.H, g.nb, (const float*)partial, d_table);
   if (e == hipSuccess && g.nk > 0) {
     const dim3 grid((unsigned)seq_blocks(g.k_tiles, g.parts));
-    const void* fn = g.parts > 1 ? (bias ? (const void*)&seq_dkdv_kernel<T, D, true, true>
-                                         : (const void*)&seq_dkdv_kernel<T, D, false, true>)
-                                 : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
-                                         : (const void*)&seq_dkdv_kernel<T, D, false, false>);
-    e = launch(fn, grid, kThreads, bias ? (size_t)g.span * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
+    const bool parts = g.parts > 1;
+    const void* fn;
+    if constexpr (D == 64)
+      fn = parts ? (bias ? (const void*)&seq_dkdv_kernel<T, D, true, true>
+                         : (const void*)&seq_dkdv_kernel<T, D, false, true>)
+                 : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
+                         : (const void*)&seq_dkdv_kernel<T, D, false, false>);
+    else
+      fn = parts ? (bias ? (const void*)&seq_dkdv_pair_kernel<T, true, true>
+                         : (const void*)&seq_dkdv_pair_kernel<T, false, true>)
+                 : (bias ? (const void*)&seq_dkdv_pair_kernel<T, true, false>
+                         : (const void*)&seq_dkdv_pair_kernel<T, false, false>);
+    e = launch(fn, grid, D == 64 ? kThreads : 512, bias ? (size_t)g.span * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
                t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
                part_dv);
   }
@@ -901,12 +1106,13 @@ hipError_t launch_seq_forward(const SeqGeometry& g, bool bf16, const SeqTensors&
 }
 
 // Parts of the dk/dv pass.  Key heads x key tiles workgroups do the work of all heads of a group;
-// where they are fewer than two per compute unit, the (head, query tile) pairs are dealt out to up
-// to 16 parts.  Key tiles are estimated from the rows and sequences.
+// where they are fewer than two per compute unit (four under a causal mask, where the first tiles
+// have twice the average work), the (head, query tile) pairs are dealt out to up to 16 parts.  Key
+// tiles are estimated from the rows and sequences.
 int seq_backward_parts(const SeqGeometry& g) {
   const int64_t blocks = (int64_t)g.KH * std::max<int64_t>(1, g.nk / kSeqTile);
   const int64_t most = std::min<int64_t>(16, (int64_t)g.group * std::max(1, g.nq / g.B / 256));
-  return (int)std::max<int64_t>(1, std::min<int64_t>(512 / blocks, most));
+  return (int)std::max<int64_t>(1, std::min<int64_t>((g.causal ? 1024 : 512) / blocks, most));
 }
 
 size_t seq_backward_workspace(const SeqGeometry& g, bool want_table) {
