@@ -177,19 +177,17 @@ def make_desc(B, T, H, W, heads, head_dim, kt, kh, kw, dtype="bf16", scale=0.0) 
 
 def _ptr(x):
     """Device pointer of a tensor (or an int address, or None for NULL)."""
-    if x is None:
-        return None
-    if isinstance(x, int):
+    if x is None or type(x) is int:
         return x
     return x.data_ptr()
 
 
 def _stream(stream):
+    if type(stream) is int:
+        return stream
     if stream is None:
         import torch
         return torch.cuda.current_stream().cuda_stream
-    if isinstance(stream, int):
-        return stream
     return stream.cuda_stream
 
 

@@ -35,6 +35,7 @@ struct Span1 {
   int n, m, off;     // new tokens, held tokens (also those not attended to), position of token 0
   int r0, rows;      // first row of the tile, rows of the request
   int k_lo, k_hi;    // keys of this part that any of its rows sees
+  bool only;         // this part has all of them: no join
   int seen;          // keys below this exist for the call
 };
 
@@ -56,9 +57,14 @@ __device__ inline bool locate(const PagedGeometry& g, const int32_t* cu_q, const
     const int i_last = div_by(min(s.r0 + TILE, s.rows) - 1, g.group_mul, g.group_shift);
     hi = min(hi, s.off + i_last + 1);
   }
-  s.k_lo = split * g.part;
-  s.k_hi = min(hi, s.k_lo + g.part);
-  return true;
+  // The keys that the tile sees, in at most g.splits parts of at least g.part.
+  constexpr int kStep = kFewKeys;  // parts begin at tiles
+  const int even = (max(hi, 0) + g.splits - 1) / g.splits;
+  const int part = max(g.part, (even + kStep - 1) / kStep * kStep);
+  s.k_lo = min(split * (int64_t)part, (int64_t)max(hi, 0));
+  s.k_hi = min((int64_t)hi, (int64_t)s.k_lo + part);
+  s.only = hi <= part;
+  return !(s.only && split > 0);
 }
 
 // Cache rows (page * page_size + row) of keys base .. base + KT - 1 into tab; -1 where there is
@@ -81,6 +87,11 @@ __device__ inline void fill_rows(int* tab, int* bad, const PagedGeometry& g, con
   }
 }
 
+// What the join reads of a part: its log-sum-exp (base 2); kDone as the first part's where the
+// row needs no join.
+constexpr float kDone = INFINITY;
+__device__ inline float part_lse(float l2) { return l2 == INFINITY ? NAN : l2; }
+
 struct Row {
   int i, head;    // token of the request, head
   bool ok;
@@ -99,16 +110,16 @@ __device__ inline Row row_of(const PagedGeometry& g, const Span1& s, int u, int 
 }
 
 // Running softmax of one query over 32-key blocks (lanes l and l ^ 32 keep identical maxima and
-// a sum each over their half of the keys).
+// a sum each over their half of the keys).  The logits are `scale` times the values given (base 2).
 struct Softmax {
   float top = -INFINITY, base = 0.0f, l = 0.0f;
 
   template <int DB>
-  __device__ inline void step(float (&s)[16], f32x16_t (&o)[DB]) {
+  __device__ inline void raise_to(const float (&s)[16], float scale, f32x16_t (&o)[DB]) {
     float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
     for (int i = 3; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    mx = pair_max(mx);
+    mx = pair_max(mx) * scale;  // scale > 0
     const bool raise = mx > top + kSlack;
     if (__any(raise)) {
       const float corr = raise ? __builtin_amdgcn_exp2f(top - mx) : 1.0f;
@@ -117,9 +128,11 @@ struct Softmax {
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] *= corr;
     }
+  }
+  __device__ inline void weigh(float (&s)[16], float scale) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(s[i] - base);
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], scale, -base));
       l += s[i];
     }
   }
@@ -134,33 +147,45 @@ __device__ inline void fill_bias(float* tab, const PagedGeometry& g, const float
   }
 }
 
-// Logits in base-2 units with bias and mask: element i is key kb + c_row(i), a row's token stands
-// at position pos.  rows: the block's cache rows (-1: no key).
-template <bool BIAS>
-__device__ inline void finish_logits(float (&s)[16], const PagedGeometry& g, const float* tab,
-                                     int head_in_group, int kb, int pos, int last, bool masked,
-                                     const int* rows) {
+// The logits in base-2 units where there is a bias (their scale is 1 then): element i is key
+// kb + c_row(i), the row's token stands at position pos.
+__device__ inline void add_bias(float (&s)[16], const PagedGeometry& g, const float* tab,
+                                int head_in_group, int kb, int pos) {
   const int hh = (threadIdx.x & 63) >> 5;
-  if constexpr (BIAS) {
-    const float* t = tab + head_in_group * g.span;
+  const float* t = tab + head_in_group * g.span;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      s[i] = fmaf(s[i], g.scale_log2,
-                  t[min(max(kb + c_row(i, hh) - pos - g.rel_min, 0), g.span - 1)]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] *= g.scale_log2;
-  }
-  if (masked) {
-    asm volatile("");  // a branch: blocks that every row sees do not pay for it
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (kb + c_row(i, hh) > last || rows[c_row(i, hh)] < 0) s[i] = -INFINITY;
-  }
+  for (int i = 0; i < 16; ++i)
+    s[i] = fmaf(s[i], g.scale_log2,
+                t[min(max(kb + c_row(i, hh) - pos - g.rel_min, 0), g.span - 1)]);
 }
 
 // ------------------------------------------------------------------------- many rows
 
+// Where the cache rows of the 64 keys from `base` on lie, in bytes, by the first wave.  A key without a place (past the
+// part's keys, or a page number outside the tensors) gets the row of one that has one, so that
+// what is copied is what some query sees, and is left out of the mask; a tile with none has mask 0
+// and rows that are never read.
+template <typename T>
+__device__ inline void fill_tile(int64_t* tab, uint64_t* mask, const PagedGeometry& g,
+                                 const int32_t* pages, const Span1& s, int base, int keys) {
+  if (threadIdx.x < 64) {
+    const int j = base + (int)threadIdx.x;
+    int row = -1;
+    if ((int)threadIdx.x < keys && j < s.k_hi) {
+      const int page = div_by(j, g.page_mul, g.page_shift);
+      const int p = pages[(int64_t)s.b * g.max_pages + page];
+      if (p >= 0 && p < g.num_pages) row = p * g.page_size + (j - page * g.page_size);
+    }
+    const uint64_t there = __ballot(row >= 0);
+    const int some = there != 0 ? __shfl(row, __ffsll((unsigned long long)there) - 1) : 0;
+    if ((int)threadIdx.x < keys)
+      tab[threadIdx.x] = (row >= 0 ? row : some) * (g.ks * (int)sizeof(T));
+    if (threadIdx.x == 0) *mask = there;
+  }
+}
+
+// As the forward of seqattn.hip (tiles copied straight to LDS, a tile's second block multiplied
+// beside the first one's softmax), through the page table.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __restrict__ k,
@@ -172,11 +197,10 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   constexpr int KT = Type<T>::kKeyTile;
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
-  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32;
-  __shared__ __attribute__((aligned(16))) T Ks[2][Tl::kElems];
-  __shared__ __attribute__((aligned(16))) T Vs[2][Tl::kElems];
-  __shared__ int tab[kRing][KT];
-  __shared__ int bad[kRing];
+  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
+  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
+  __shared__ int64_t tab[kRing][KT];
+  __shared__ uint64_t there[kRing];
   extern __shared__ float bias[];
 
   Work w;
@@ -186,24 +210,22 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   if (!locate<kManyRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
   for (int i = 0; i < 3 && i < ntiles; ++i)
-    fill_rows<KT>(tab[i], &bad[i], g, pages, s, s.k_lo + i * KT);
+    fill_tile<T>(tab[i], &there[i], g, pages, s, s.k_lo + i * KT, KT);
   if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
 
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int rw = s.r0 + wave * 32;
+  const bool live = rw < s.rows;
   const Row x = row_of(g, s, w.u, rw + (lane & 31));
   Frag qf[KS];
   load_frag<T, D>(qf, q + x.q_at, x.ok);
   const int pos = s.off + x.i;
   const int last = g.causal ? min(s.seen - 1, pos) : s.seen - 1;
-  int wave_last = -1, all_see = s.seen - 1;
-  if (rw < s.rows) {
-    wave_last = s.seen - 1;
-    if (g.causal) {
-      all_see = min(all_see, s.off + div_by(rw, g.group_mul, g.group_shift));
-      wave_last = min(wave_last, s.off + div_by(min(rw + 31, s.rows - 1), g.group_mul,
-                                                g.group_shift));
-    }
+  int wave_last = live ? s.seen - 1 : -1, all_see = s.seen - 1;
+  if (live && g.causal) {
+    all_see = min(all_see, s.off + div_by(rw, g.group_mul, g.group_shift));
+    wave_last = min(wave_last, s.off + div_by(min(rw + 31, s.rows - 1), g.group_mul,
+                                              g.group_shift));
   }
 
   f32x16_t o[DB];
@@ -211,80 +233,129 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
   Softmax sm;
   const T *kp = k + w.u * D, *vp = v + w.u * D;
-  uint4 kr[Tl::NL], vr[Tl::NL];
-  __syncthreads();
-  if (ntiles > 0) {
-    Tl::load(kr, kp, g.ks, tab[0]);
-    Tl::load(vr, vp, g.vs, tab[0]);
-    Tl::store(Ks[0], kr);
-    Tl::store(Vs[0], vr);
-    if (ntiles > 1) {
-      Tl::load(kr, kp, g.ks, tab[1]);
-      Tl::load(vr, vp, g.vs, tab[1]);
-    }
-  }
-  __syncthreads();
-  for (int kt = 0; kt < ntiles; ++kt) {
-    const T *kc = Ks[kt & 1], *vc = Vs[kt & 1];
-    if (kt + 1 < ntiles) {
-      Tl::store(Ks[(kt + 1) & 1], kr);
-      Tl::store(Vs[(kt + 1) & 1], vr);
-    }
-    if (kt + 2 < ntiles) {
-      Tl::load(kr, kp, g.ks, tab[(kt + 2) % kRing]);
-      Tl::load(vr, vp, g.vs, tab[(kt + 2) % kRing]);
-    }
+  auto fetch = [&](int kt, int buf) {
+    Tl::copy(lds + 2 * E * buf, kp, lds + 2 * E * buf + E, vp, tab[kt % kRing]);
+  };
+  auto products = [&](const T* kc, int b) {
+    Frag a[KS];
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(kc, b * 32, ks);
+    f32x16_t acc = f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) acc = mfma(a[ks], qf[ks], acc);
+    return acc;
+  };
+  const float scale = BIAS ? 1.0f : g.scale_log2;
+  auto accumulate = [&](const T* vc, int b, const float (&t)[16]) {
+    Frag pf[2];
+    to_frags(t, pf);
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        o[db] = mfma(Tl::a_cols(vc, db * 32, b, p), pf[p], o[db]);
+  };
+  auto advance = [&](int kt, int buf) {
+    if (kt + 1 < ntiles) fetch(kt + 1, 1 - buf);
     if (kt + 3 < ntiles)
-      fill_rows<KT>(tab[(kt + 3) % kRing], &bad[(kt + 3) % kRing], g, pages, s,
-                    s.k_lo + (kt + 3) * KT);
+      fill_tile<T>(tab[(kt + 3) % kRing], &there[(kt + 3) % kRing], g, pages, s,
+                s.k_lo + (kt + 3) * KT, KT);
+  };
+  auto mask_of = [&](int kt) {
+    const uint64_t m = there[kt % kRing];
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32 |
+           (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+  };
+  constexpr uint64_t kFull = KT == 64 ? ~0ull : (1ull << KT) - 1;
+
+  __syncthreads();
+  if (ntiles > 0) fetch(0, 0);
+  wait_copies();
+  __syncthreads();
+  // Tiles that all of the workgroup's rows see whole, as in seqattn.hip's forward
+  const int first_sees = g.causal ? s.off + div_by(s.r0, g.group_mul, g.group_shift) : s.seen - 1;
+  const int whole = BIAS ? 0 : max(min(s.k_hi, first_sees + 1) - s.k_lo, 0) / KT;
+  int kt = 0;
+  while (kt < ntiles) {
+    if ((kt & 1) == 0 && kt < whole && mask_of(kt) == kFull) {
+      f32x16_t next = f32x16_t{};
+      if (live) next = products(lds, 0);
+      auto tile = [&](int t, int buf) {
+        const T *kc = lds + 2 * E * buf, *kn = lds + 2 * E * (1 - buf);
+        advance(t, buf);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          float y[16];
+          if (live) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = next[i];
+            sm.raise_to(y, scale, o);
+          }
+          if (b == NB - 1) {  // the next tile is in LDS
+            wait_copies();
+            __syncthreads();
+          }
+          if (live) {
+            next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
+            sm.weigh(y, scale);
+            accumulate(kc + E, b, y);
+          }
+        }
+        __syncthreads();
+      };
+      do {
+        tile(kt++, 0);
+        if (kt >= whole || mask_of(kt) != kFull) break;
+        tile(kt++, 1);
+      } while (kt < whole && mask_of(kt) == kFull);
+      continue;
+    }
+    const T* kc = lds + 2 * E * (kt & 1);
+    advance(kt, kt & 1);
     const int kbase = s.k_lo + kt * KT;
-    const int nb = wave_last < kbase ? 0 : min(NB, (wave_last - kbase) / 32 + 1);
-    const bool some_bad = bad[kt % kRing] != 0;
+    const uint64_t mask = mask_of(kt);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      if (b >= nb) break;
-      Frag a[KS];
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(kc, b * 32, ks);
-      f32x16_t acc = f32x16_t{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) acc = mfma(a[ks], qf[ks], acc);
-      Frag av[DB][2];
-#pragma unroll
-      for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int p = 0; p < 2; ++p) av[db][p] = Tl::a_cols(vc, db * 32, b, p);
-      float t[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) t[i] = acc[i];
       const int kb = kbase + b * 32;
-      finish_logits<BIAS>(t, g, bias, x.head - w.u * g.group, kb, pos, last,
-                          some_bad || kb + 31 > all_see, tab[kt % kRing] + b * 32);
-      sm.step(t, o);
-      Frag pf[2];
-      to_frags(t, pf);
+      const uint32_t bits = (uint32_t)(mask >> (b * 32));
+      if (bits == 0 || wave_last < kb) continue;
+      const f32x16_t x0 = products(kc, b);
+      float y[16];
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int i = 0; i < 16; ++i) y[i] = x0[i];
+      if constexpr (BIAS) add_bias(y, g, bias, x.head - w.u * g.group, kb, pos);
+      if (bits != ~0u || kb + 31 > all_see) {
+        asm volatile("");  // a branch: blocks that every row sees do not pay for it
+        const int seen = last - kb - 4 * hh;
+        const uint32_t mine = bits >> (4 * hh);
 #pragma unroll
-        for (int p = 0; p < 2; ++p) o[db] = mfma(av[db][p], pf[p], o[db]);
+        for (int i = 0; i < 16; ++i)
+          if (c_row(i, 0) > seen || (mine >> c_row(i, 0) & 1) == 0) y[i] = -INFINITY;
+      }
+      sm.raise_to(y, scale, o);
+      sm.weigh(y, scale);
+      accumulate(kc + E, b, y);
     }
+    wait_copies();
     __syncthreads();
+    ++kt;
   }
   const float ltot = pair_sum(sm.l);
   const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;
   const float l2 = ltot == 0.0f ? -INFINITY : sm.base + __builtin_amdgcn_logf(ltot);
   if (!x.ok) return;
-  if (g.splits == 1) {
+  if (s.only) {
 #pragma unroll
     for (int db = 0; db < DB; ++db) store_block(out + x.out_at * D, db, o[db], inv);
     if (hh == 0 && lse != nullptr) lse[x.out_at] = l2 * kLn2;
+    if (hh == 0 && g.splits > 1) part_l[x.out_at * g.splits] = kDone;
   } else {
-    const int64_t at = (int64_t)split * g.nq * g.H + x.out_at;
+    const int64_t at = x.out_at * g.splits + split;
     if (ltot != 0.0f) {  // the join skips the parts of a row without keys
 #pragma unroll
       for (int db = 0; db < DB; ++db) store_block(part_o + at * D, db, o[db], inv);
     }
-    if (hh == 0) part_l[at] = l2;
+    if (hh == 0) part_l[at] = part_lse(l2);
   }
 }
 
@@ -363,10 +434,17 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
       float t[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) t[i] = acc[i];
-      finish_logits<BIAS>(t, g, bias, x.head - w.u * g.group, kb, pos, last,
-                          bad[kt % kRing][wave / 2] != 0 || kb + 31 > all_see,
-                          tab[kt % kRing] + wave * 32);
-      sm.step(t, o);
+      if constexpr (BIAS) add_bias(t, g, bias, x.head - w.u * g.group, kb, pos);
+      if (bad[kt % kRing][wave / 2] != 0 || kb + 31 > all_see) {
+        asm volatile("");  // a branch: blocks that every row sees do not pay for it
+        const int* rows = tab[kt % kRing] + wave * 32;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (kb + c_row(i, hh) > last || rows[c_row(i, hh)] < 0) t[i] = -INFINITY;
+      }
+      const float scale = BIAS ? 1.0f : g.scale_log2;
+      sm.raise_to(t, scale, o);
+      sm.weigh(t, scale);
       Frag pf[2];
       to_frags(t, pf);
 #pragma unroll
@@ -421,7 +499,7 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
                                    : (tr == -INFINITY ? 0.0f : tr) + __builtin_amdgcn_logf(total);
     const float4 y = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
     const Row z = row_of(g, s, w.u, s.r0 + r);
-    if (g.splits == 1) {
+    if (s.only) {
       T* to = out + z.out_at * D + chunk * 4;
       if constexpr (sizeof(T) == 4) {
         *reinterpret_cast<float4*>(to) = y;
@@ -430,27 +508,30 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
         *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, h);
       }
       if (chunk == 0 && lse != nullptr) lse[z.out_at] = l2 * kLn2;
+      if (chunk == 0 && g.splits > 1) part_l[z.out_at * g.splits] = kDone;
     } else {
-      const int64_t at = (int64_t)split * g.nq * g.H + z.out_at;
+      const int64_t at = z.out_at * g.splits + split;
       if (total != 0.0f) *reinterpret_cast<float4*>(part_o + at * D + chunk * 4) = y;
-      if (chunk == 0) part_l[at] = l2;
+      if (chunk == 0) part_l[at] = part_lse(l2);
     }
   }
 }
 
-// Joins the parts of each row: weights 2^(l - max l), one wave per row.
+// Joins the parts of each row: weights 2^(l - max l).  One wave per row, a quarter or half of it
+// per part, four channels per lane; rows that one workgroup finished are left as they are.
 template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void paged_join_kernel(int64_t rows, int splits,
                                                               const float* __restrict__ part_o,
                                                               const float* __restrict__ part_l,
                                                               T* __restrict__ out,
                                                               float* __restrict__ lse) {
-  constexpr int PER = D / 64;
+  constexpr int LANES = D / 4, SIDES = 64 / LANES;  // lanes per part, parts at a time
   const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, side = lane / LANES, c = lane % LANES * 4;
   if (row >= rows) return;
   // lane s holds part s's log-sum-exp (at most 64 parts)
-  const float mine = lane < splits ? part_l[lane * rows + row] : -INFINITY;
+  const float mine = lane < splits ? part_l[row * splits + lane] : -INFINITY;
+  if (__shfl(mine, 0) == kDone) return;
   float top = mine;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -458,20 +539,35 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(int64_t rows, int 
   float total = weight;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-  float sum[PER] = {};
-  for (int s = 0; s < splits; ++s) {
-    const float ws = __shfl(weight, s);
-    if (__shfl(mine, s) == -INFINITY) continue;  // nothing was written for this part
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s = side; s < splits; s += SIDES) {
+    const float ws = __shfl(weight, s), ls = __shfl(mine, s);
+    if (ls != -INFINITY) {  // else nothing was written for this part
+      const float4 x = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
+      sum.x = fmaf(ws, x.x, sum.x);
+      sum.y = fmaf(ws, x.y, sum.y);
+      sum.z = fmaf(ws, x.z, sum.z);
+      sum.w = fmaf(ws, x.w, sum.w);
+    }
+  }
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-      sum[j] = fmaf(ws, part_o[(s * rows + row) * D + lane * PER + j], sum[j]);
+  for (int d = 32; d >= LANES; d >>= 1) {
+    sum.x += __shfl_xor(sum.x, d);
+    sum.y += __shfl_xor(sum.y, d);
+    sum.z += __shfl_xor(sum.z, d);
+    sum.w += __shfl_xor(sum.w, d);
   }
   const float inv = total > 0.0f ? 1.0f / total : total;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const float y = sum[j] * inv;
-    if constexpr (sizeof(T) == 4) out[row * D + lane * PER + j] = y;
-    else out[row * D + lane * PER + j] = to_bf16(y);
+  if (side == 0) {
+    T* to = out + row * D + c;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4*>(to) =
+          make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+    } else {
+      const uint16_t h[4] = {to_bf16(sum.x * inv), to_bf16(sum.y * inv), to_bf16(sum.z * inv),
+                             to_bf16(sum.w * inv)};
+      *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, h);
+    }
   }
   if (lane == 0 && lse != nullptr)
     lse[row] = total == 0.0f ? -INFINITY
@@ -541,22 +637,37 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
 
 }  // namespace
 
-// Rows per workgroup and parts of the keys.  32 rows where the requests have no more on average.
-// Parts: enough that the key heads, tiles and parts make about kTarget workgroups (eight per
-// compute unit, so that requests of different lengths even out), but none below kLeast keys, for
-// which the float32 results a part writes and the join reads would weigh against its keys.
-void paged_plan(PagedGeometry& g, bool) {
-  constexpr int kTarget = 2048, kLeast = 512, kMost = 64;
+// Rows per workgroup: 32 where the requests have no more on average.  Parts of the keys (`splits` at
+// most, of `part` keys at least; a tile whose keys fit one part has no join):
+//  - few rows: reading is all, so the key heads, requests and parts make up to 2,048 workgroups,
+//    which also evens out requests of different lengths, in parts of 1,024 keys, or of 512 where
+//    that leaves the card half empty.  64 requests of 200 to 8,000 tokens, 32 / 8 heads x 128:
+//    238 us in parts of 2,048 keys, 219 of 1,024, 215 of 512; one of 4,000: 63, 28, 19 us; four of
+//    30,000: 105, 110, 113 us.
+//  - many rows: a part's float32 results are written and read again, which weighs more than uneven
+//    ends: parts of 4,096 keys, or as many as fill the card (512 workgroups).  1,024 new of 16,384
+//    tokens: 340 us in parts of 2,048, 312 of 4,096; chunks of 512, 801, 300 and single tokens:
+//    265 and 236 us.
+void paged_plan(PagedGeometry& g) {
+  constexpr int kMost = 64;
   const int64_t rows = (int64_t)g.nq * g.group;
   g.tile = rows <= (int64_t)kFewRows * g.B ? kFewRows : kManyRows;
   const int64_t tiles = std::max<int64_t>((rows + g.tile - 1) / g.tile, std::min(g.B, g.nq));
-  const int64_t want = kTarget / std::max<int64_t>(1, tiles * g.KH);
-  const int most = std::min(kMost, std::max(1, g.max_kv / kLeast));
-  g.splits = (int)std::min<int64_t>(std::max<int64_t>(want, 1), most);
-  const int step = kFewKeys;  // parts begin at tiles
-  g.part = (int)(((int64_t)g.max_kv + g.splits - 1) / g.splits + step - 1) / step * step;
-  g.part = std::max(g.part, step);
-  g.splits = std::max(1, (int)(((int64_t)g.max_kv + g.part - 1) / g.part));
+  const int64_t units = std::max<int64_t>(1, tiles * g.KH);
+  int64_t splits;
+  if (g.tile == kFewRows) {
+    g.part = units * g.max_kv >= 512 * 1024 ? 1024 : 512;
+    splits = std::min<int64_t>(2048 / units, g.max_kv / g.part);
+  } else {
+    const int64_t fill = (512 + units - 1) / units;
+    splits = std::min<int64_t>(2048 / units, g.max_kv / 4096);
+    g.part = 4096;
+    if (splits < fill) {
+      g.part = (int)std::max<int64_t>(512, g.max_kv / fill);
+      splits = std::min<int64_t>(fill, g.max_kv / g.part);
+    }
+  }
+  g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, kMost));
   g.tiles = seq_spread(g.KH, (int)(rows / g.tile) + g.B + 1);
 }
 

@@ -282,7 +282,9 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     g->ks = g->vs = krow;
   }
   const int64_t held = (int64_t)d->max_pages * d->page_size;
-  const int64_t most = d->max_kv > 0 ? std::min<int64_t>(d->max_kv, held) : held;
+  const int64_t most = d->num_pages == 0 ? 0  // no cache: no tokens
+                       : d->max_kv > 0   ? std::min<int64_t>(d->max_kv, held)
+                                         : held;
   if (!append && most > (1 << 30)) return DSA3D_ERR_INVALID_SHAPE;
   g->B = d->batch;
   g->nq = d->total_q;
@@ -304,7 +306,7 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     return DSA3D_ERR_UNSUPPORTED;
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
-  dsa3d::paged_plan(*g, d->dtype == DSA3D_BF16);
+  dsa3d::paged_plan(*g);
   if (dsa3d::seq_blocks(g->tiles, g->splits) >= kIndexLimit) return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->out = (uint64_t)d->total_q * qrow * s->item;

@@ -89,6 +89,13 @@ __device__ inline void copy_16(uint32_t to, const void* base, uint32_t off) {
                : "s"(to), "v"(off), "s"(base)
                : "memory");
 }
+// The same from an address per lane.
+__device__ inline void copy_16(uint32_t to, const void* from) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
+               :
+               : "s"(to), "v"(from)
+               : "memory");
+}
 // The same with 4 bytes per lane, from base + first floats + off bytes.
 __device__ inline void copy_4(uint32_t to, const float* base, uint32_t off, int64_t first) {
   base += first;
@@ -180,7 +187,10 @@ struct Tile {
   static constexpr int NC = ROWS * kRowBytes / (1024 * (THREADS / 64));  // copies per wave
   static_assert(NC >= 1, "every wave copies");
   static __device__ inline int copy_row(int i) {
-    return (wave_id() * NC + i) * kRowsPerCopy + ((int)threadIdx.x & 63) / KCH;
+    return (i * (THREADS / 64) + wave_id()) * kRowsPerCopy + ((int)threadIdx.x & 63) / KCH;
+  }
+  static __device__ inline uint32_t copy_to(const T* lds, int i) {
+    return lds_offset(lds) + (i * (THREADS / 64) + wave_id()) * 1024;
   }
   static __device__ inline int copy_chunk(int row) {
     return (at(row, ((int)threadIdx.x % KCH) * CH) - row * D) * (int)sizeof(T);
@@ -195,17 +205,28 @@ struct Tile {
   // valid one, to be masked.  Done once wait_copies() and a barrier have passed.
   static __device__ inline void copy(T* lds, const T* src, const uint32_t (&off)[NC],
                                      uint32_t stride_bytes, int valid) {
-    const uint32_t to = lds_offset(lds) + wave_id() * (NC * 1024);
     if (valid >= ROWS) {
 #pragma unroll
-      for (int i = 0; i < NC; ++i) copy_16(to + i * 1024, src, off[i]);
+      for (int i = 0; i < NC; ++i) copy_16(copy_to(lds, i), src, off[i]);
     } else {
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const int row = copy_row(i);
-        copy_16(to + i * 1024, src,
+        copy_16(copy_to(lds, i), src,
                 (uint32_t)min(row, valid - 1) * stride_bytes + copy_chunk(row));
       }
+    }
+  }
+
+  // Starts the copies of tile rows of two tensors that lie `tab` bytes from src and src2.
+  static __device__ inline void copy(T* lds, const T* src, T* lds2, const T* src2,
+                                     const int64_t* tab) {
+#pragma unroll
+    for (int i = 0; i < NC; ++i) {
+      const int row = copy_row(i);
+      const int64_t at = tab[row] + copy_chunk(row);
+      copy_16(copy_to(lds, i), reinterpret_cast<const char*>(src) + at);
+      copy_16(copy_to(lds2, i), reinterpret_cast<const char*>(src2) + at);
     }
   }
 
@@ -460,7 +481,7 @@ __device__ inline float bias_of(const float* table, const int32_t* map, int head
 // and late tiles (short and long ones under a causal mask) fall on each.  The long ones come first:
 // late tiles of queries, early tiles of keys.
 struct Work {
-  int u, slot, head;
+  int u, slot, head;  // head: u * per + the block's number among the `per` of its slot
 };
 template <bool LATE_FIRST = true>
 __device__ inline bool work_of(const Spread& sp, int per, Work& w) {

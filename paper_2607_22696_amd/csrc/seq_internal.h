@@ -60,12 +60,12 @@ struct PagedGeometry {
   float scale, scale_log2;
   int64_t qs, ks, vs;
   int tile;     // rows (tokens x heads of a group) per workgroup
-  int splits;   // parts of the keys, of `part` keys each
+  int splits;   // most parts of a tile's keys, and least keys of a part
   int part;
   Spread tiles;
 };
 
-void paged_plan(PagedGeometry& g, bool bf16);
+void paged_plan(PagedGeometry& g);
 size_t paged_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,
                                 const void* k_pages, const void* v_pages, const int32_t* pages,

@@ -31,6 +31,9 @@ class _Checks:
         self.problems = []
 
     def tensor(self, name, t, shape, dtype, device):
+        if isinstance(t, torch.Tensor) and t.dtype == dtype and t.shape == shape and \
+                t.device == device and t.is_contiguous():
+            return
         if not isinstance(t, torch.Tensor):
             self.problems.append(f"{name}: expected a tensor, got {type(t).__name__}")
             return
@@ -346,6 +349,9 @@ def _rows(chk, name, t, heads, head_dim, dtype, device, rows=None):
         chk.problems.append(f"{name}: expected a tensor, got {type(t).__name__}")
         return 0
     shape = t.shape
+    if shape == (rows, heads, head_dim) and t.dtype == dtype and t.device == device and \
+            t.is_contiguous():
+        return 0
     if t.dim() != 3 or shape[1] != heads or shape[2] != head_dim or \
             (rows is not None and shape[0] != rows) or t.dtype != dtype or t.device != device:
         want = ("rows" if rows is None else rows, heads, head_dim)
@@ -369,7 +375,7 @@ def _cu(chk, name, t, device):
     if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.numel() < 2:
         chk.problems.append(f"{name}: expected an int32 tensor of sequences + 1 row offsets")
         chk.done()
-    _ints(chk, name, t, (t.numel(),), device)
+    chk.tensor(name, t, t.shape, torch.int32, device)
     return t.numel() - 1
 
 
@@ -407,22 +413,25 @@ def _lead_rows(chk, q):
     return q.device
 
 
-class _Here:
-    """No change of device: the tensors are on the current one."""
-
-    def __enter__(self):
-        return self
-
-    def __exit__(self, *exc):
-        return False
+# The current stream's handle, without the Stream object around it where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-_HERE = _Here()
+def _launch(device, call, *args, **kw):
+    """The call on the current stream of the tensors' device, with that device current."""
+    index = device.index
+    if index == torch.cuda.current_device():
+        call(*args, stream=_raw_stream(index), **kw)
+    else:
+        with torch.cuda.device(device):
+            call(*args, stream=_raw_stream(index), **kw)
 
 
-def _on(device):
-    """The tensors' device made current for a launch: kernels and the stream are that device's."""
-    return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+def _like(t, device):
+    """A new contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else \
+        torch.empty(t.shape, dtype=t.dtype, device=device)
 
 
 def relative_buckets(num_buckets=32, max_distance=128, both=True, device="cuda"):
@@ -443,16 +452,17 @@ def _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, r
     nk, kv_heads = k.shape[0], k.shape[1]
     if kv_heads < 1 or heads % kv_heads:
         chk.problems.append(f"k: {kv_heads} heads do not divide the {heads} of q")
-    qs = _rows(chk, "q", q, heads, D, q.dtype, dev)
-    ks = _rows(chk, "k", k, kv_heads, D, q.dtype, dev)
-    vs = _rows(chk, "v", v, kv_heads, D, q.dtype, dev, nk)
+    dtype = q.dtype
+    qs = _rows(chk, "q", q, heads, D, dtype, dev, nq)
+    ks = _rows(chk, "k", k, kv_heads, D, dtype, dev, nk)
+    vs = _rows(chk, "v", v, kv_heads, D, dtype, dev, nk)
     batch = _cu(chk, "cu_q", cu_q, dev)
     if cu_k is not None:
         _ints(chk, "cu_k", cu_k, (batch + 1,), dev)
     elif nk != nq:
         chk.problems.append(f"k: {nk} rows, but q has {nq} and there is no cu_k")
     lo, span, buckets = _relative(chk, rel_table, rel_buckets, rel_min, heads, dev)
-    return dev, make_seq_desc(batch, nq, nk, heads, kv_heads, D, causal, _IO_DTYPES[q.dtype],
+    return dev, make_seq_desc(batch, nq, nk, heads, kv_heads, D, causal, _IO_DTYPES[dtype],
                               scale, lo, span, buckets, qs, ks, vs)
 
 
@@ -477,7 +487,7 @@ def seq_forward(q, k, v, cu_q, cu_k=None, causal=False, scale=0.0, rel_table=Non
         chk.optional("out_res", out_res, q.shape, q.dtype, dev)
     chk.done()
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = _like(q, dev)
     if not need_lse:
         lse = None
     elif lse is None:
@@ -485,9 +495,9 @@ def seq_forward(q, k, v, cu_q, cu_k=None, causal=False, scale=0.0, rel_table=Non
     if not need_residual:
         out_res = None
     elif out_res is None:
-        out_res = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    with _on(dev):
-        dsa3d_seq_forward(desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out, out_res, lse)
+        out_res = _like(q, dev)
+    _launch(dev, dsa3d_seq_forward, desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out,
+            out_res, lse)
     return out, lse, out_res
 
 
@@ -517,17 +527,15 @@ def seq_backward(q, k, v, out, out_res, lse, dout, cu_q, cu_k=None, causal=False
     chk.workspace(workspace, dev)
     chk.done()
     if grads is None:
-        grads = [torch.empty(x.shape, dtype=q.dtype, device=dev) for x in (q, k, k)]
+        grads = [_like(x, dev) for x in (q, k, k)]
         if count == 4:
-            grads.append(torch.empty(rel_table.shape, dtype=torch.float32, device=dev)
-                         if need_table else None)
+            grads.append(_like(rel_table, dev) if need_table else None)
     need = dsa3d_seq_backward_workspace_size(desc)
     if workspace is None or workspace.numel() < need:
         workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=dev)
     d_table = grads[3] if need_table else None
-    with _on(dev):
-        dsa3d_seq_backward(desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out, out_res, lse,
-                           dout, grads[0], grads[1], grads[2], d_table, workspace, need)
+    _launch(dev, dsa3d_seq_backward, desc, q, k, v, cu_q, cu_k, rel_table, rel_buckets, out,
+            out_res, lse, dout, grads[0], grads[1], grads[2], d_table, workspace, need)
     return tuple(grads[:3]) if count == 3 else (*grads[:3], d_table)
 
 
@@ -538,15 +546,16 @@ def _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q, dtype, device):
     if not isinstance(k_pages, torch.Tensor) or k_pages.dim() != 4:
         chk.problems.append("k_pages: expected [pages, page_size, kv_heads, head_dim]")
         chk.done()
-    for name, t in (("k_pages", k_pages), ("v_pages", v_pages)):
-        chk.tensor(name, t, k_pages.shape, dtype, device)
+    shape = k_pages.shape
+    chk.tensor("k_pages", k_pages, shape, dtype, device)
+    chk.tensor("v_pages", v_pages, shape, dtype, device)
     batch = _cu(chk, "cu_q", cu_q, device)
     _ints(chk, "kv_lens", kv_lens, (batch,), device)
     if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
         chk.problems.append("pages: expected an int32 [requests, columns] tensor")
         chk.done()
     _ints(chk, "pages", pages, (batch, pages.shape[1]), device)
-    return (batch, *k_pages.shape, pages.shape[1])
+    return (batch, *shape, pages.shape[1])
 
 
 def paged_append(k, v, k_pages, v_pages, pages, kv_lens, cu_q):
@@ -566,13 +575,12 @@ def paged_append(k, v, k_pages, v_pages, pages, kv_lens, cu_q):
     dev = k.device
     batch, num, size, heads, D, columns = _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q,
                                                  k.dtype, dev)
-    ks = _rows(chk, "k", k, heads, D, k.dtype, dev)
+    ks = _rows(chk, "k", k, heads, D, k.dtype, dev, k.shape[0])
     vs = _rows(chk, "v", v, heads, D, k.dtype, dev, k.shape[0])
     chk.done()
     desc = make_paged_desc(batch, k.shape[0], heads, heads, D, num, size, columns,
                            dtype=_IO_DTYPES[k.dtype], k_stride=ks, v_stride=vs)
-    with _on(dev):
-        dsa3d_paged_append(desc, k, v, cu_q, kv_lens, pages, k_pages, v_pages)
+    _launch(dev, dsa3d_paged_append, desc, k, v, cu_q, kv_lens, pages, k_pages, v_pages)
 
 
 def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=0.0,
@@ -585,7 +593,7 @@ def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=
     chk = _Checks("paged_forward")
     dev = _lead_rows(chk, q)
     nq, heads, D = q.shape
-    qs = _rows(chk, "q", q, heads, D, q.dtype, dev)
+    qs = _rows(chk, "q", q, heads, D, q.dtype, dev, nq)
     batch, num, size, kv_heads, kD, columns = _pages(chk, k_pages, v_pages, pages, kv_lens, cu_q,
                                                      q.dtype, dev)
     if kD != D or kv_heads < 1 or heads % kv_heads:
@@ -599,7 +607,7 @@ def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=
     desc = make_paged_desc(batch, nq, heads, kv_heads, D, num, size, columns, int(max_kv), causal,
                            _IO_DTYPES[q.dtype], scale, lo, span, buckets, qs)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = _like(q, dev)
     if not need_lse:
         lse = None
     elif lse is None:
@@ -607,7 +615,6 @@ def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=
     need = dsa3d_paged_forward_workspace_size(desc)
     if need and (workspace is None or workspace.numel() < need):
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-    with _on(dev):
-        dsa3d_paged_forward(desc, q, k_pages, v_pages, pages, kv_lens, cu_q, rel_table,
-                            rel_buckets, out, lse, workspace, need)
+    _launch(dev, dsa3d_paged_forward, desc, q, k_pages, v_pages, pages, kv_lens, cu_q, rel_table,
+            rel_buckets, out, lse, workspace, need)
     return out, lse
