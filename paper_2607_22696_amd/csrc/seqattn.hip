@@ -27,36 +27,45 @@ using namespace seq;
 
 constexpr int kThreads = 256;
 
-// What a wave needs to know of the bias: the table by distance in LDS and its two ends, which all
-// farther distances share.
-struct Bias {
-  const float* tab;
-  float behind, ahead;
-};
+// The bias of one head in LDS: by distance, with kPad more entries at either end that repeat it, so
+// that a 32 x 32 block whose distances reach into the table reads it without clamping; blocks
+// beyond it share one value.
+constexpr int kPad = 62;
+__host__ __device__ inline int padded(int span) { return span + 2 * kPad; }
+// A block's dS by diagonal: 63 rows of 32 keys, 36 floats apart, per wave.
+constexpr int kSkew = 36, kSkewed = 63 * kSkew;
 
-// Fills tab (span floats) with the bias of `head`.  A barrier follows before its use.
+// A barrier follows before its use.
 template <int THREADS = kThreads>
 __device__ inline void fill_bias(float* tab, const SeqGeometry& g, const float* table,
                                  const int32_t* map, int head) {
-  for (int i = threadIdx.x; i < g.span; i += THREADS)
-    tab[i] = bias_of(table, map, g.H, g.nb, head, i);
+  for (int i = threadIdx.x; i < padded(g.span); i += THREADS)
+    tab[i] = bias_of(table, map, g.H, g.nb, head, min(max(i - kPad, 0), g.span - 1));
 }
 
-// t = s scale (+ bias) in base-2 units for a 32 x 32 block whose distances run from d_lo to d_hi;
-// dist(i) is element i's.
-template <typename Dist>
-__device__ inline void add_bias(float (&s)[16], const SeqGeometry& g, const float* tab, int d_lo,
-                                int d_hi, const Dist& dist) {
-  const int last = g.span - 1;
-  if (d_hi <= g.rel_min || d_lo >= g.rel_min + last) {  // all on one side: one value
-    const float b = tab[d_hi <= g.rel_min ? 0 : last];
+// What turns the values of a block into base-2 logits: mul x + add.
+struct Affine {
+  float mul, add;
+};
+
+// Whether no pair of a block, whose distances run from d_lo to d_hi = d_lo + 62, reaches into the
+// table; the sums' and the reads' places are in range otherwise.
+__device__ inline bool outside(const SeqGeometry& g, int d_lo) {
+  return d_lo + 62 <= g.rel_min || d_lo >= g.rel_min + g.span - 1;
+}
+
+// Adds the bias to a block's values (or says what to add to all of them).  SIGN 1: element i is
+// key c_row(i) of the block and this lane's query; -1: query c_row(i) and this lane's key.  d0 is
+// the distance of element 0.
+template <int SIGN>
+__device__ inline Affine add_bias(float (&s)[16], const SeqGeometry& g, const float* tab, int d_lo,
+                                  int d0) {
+  if (outside(g, d_lo))
+    return {g.scale_log2, tab[d_lo >= g.rel_min ? kPad + g.span - 1 : kPad]};
+  const float* at = tab + kPad + d0 - g.rel_min;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], g.scale_log2, b);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      s[i] = fmaf(s[i], g.scale_log2, tab[min(max(dist(i) - g.rel_min, 0), last)]);
-  }
+  for (int i = 0; i < 16; ++i) s[i] = fmaf(s[i], g.scale_log2, at[SIGN * c_row(i, 0)]);
+  return {1.0f, 0.0f};
 }
 
 // ---------------------------------------------------------------------------- forward
@@ -148,12 +157,11 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   // The largest of a block's logits (base 2), and the running maximum raised where that exceeds
   // it by more than kSlack: alpha stays below 2^kSlack and the rescale of O is rare.  The result
   // does not depend on which maximum was used.
-  auto raise_to = [&](const float (&s)[16]) {
+  auto raise_to = [&](const float (&s)[16], const Affine& f) {
     float mx = fmaxf(fmaxf(s[0], s[1]), s[2]);
 #pragma unroll
     for (int i = 3; i < 16; ++i) mx = fmaxf(mx, s[i]);
-    mx = pair_max(mx);
-    if constexpr (!BIAS) mx *= g.scale_log2;  // scale > 0
+    mx = fmaf(pair_max(mx), f.mul, f.add);  // mul > 0
     const bool raise = mx > mx_run + kSlack;
     if (__any(raise)) {
       const float corr = raise ? __builtin_amdgcn_exp2f(mx_run - mx) : 1.0f;
@@ -164,13 +172,20 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
     }
   };
   // alpha (unnormalised) in place of the logits, and its fragments
-  auto weigh = [&](float (&s)[16], Frag (&ph)[2]) {
+  auto weigh = [&](float (&s)[16], const Affine& f, Frag (&ph)[2]) {
+    const float add = f.add - base;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - base : fmaf(s[i], g.scale_log2, -base));
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], f.mul, add));
       l += s[i];
     }
     to_frags(s, ph);
+  };
+  auto biased = [&](float (&s)[16], int kb) {
+    if constexpr (BIAS)
+      return add_bias<1>(s, g, tab, kb - (i0 + 31 + off), kb + 4 * hh - iq - off);
+    else
+      return Affine{g.scale_log2, 0.0f};
   };
   auto values = [&](const T* vc, int b, Frag (&av)[DB][2]) {
 #pragma unroll
@@ -184,12 +199,19 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
 #pragma unroll
       for (int db = 0; db < DB; ++db) o[db] = mfma(av[db][p], ph[p], o[db]);
   };
+  auto add_low = [&](const Frag (&av)[DB][2], const float (&s)[16], const Frag (&ph)[2]) {
+    if constexpr (RES) {
+      Frag pl[2];
+      to_low_frags(s, ph, pl);
+      accumulate(av, pl);
+    }
+  };
 
-  // Tiles that every query of the workgroup sees whole, without a bias: the next block's logits
-  // are on the matrix cores while this block's exponentials are on the vector ALU.  Two tiles per
-  // turn, so that the LDS buffers' places are constants.
+  // Tiles that every query of the workgroup sees whole: the next block's logits are on the matrix
+  // cores while this block's exponentials are on the vector ALU.  Two tiles per turn, so that the
+  // LDS buffers' places are constants.
   int kt = 0;
-  if constexpr (!BIAS && !RES) {
+  {
     const int whole = (g.causal ? min(m, q0 + off + 1) : m) / KT;
     f32x16_t next = f32x16_t{};
     if (whole > 0 && live) next = logits(lds, 0);
@@ -199,10 +221,12 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         float s[16];
+        Affine f;
         if (live) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = next[i];
-          raise_to(s);
+          f = biased(s, t * KT + b * 32);
+          raise_to(s, f);
         }
         if (b == NB - 1) {  // the next tile is in LDS
           wait_copies();
@@ -212,8 +236,9 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
           Frag av[DB][2], ph[2];
           next = b + 1 < NB ? logits(kc, b + 1) : logits(kn, 0);
           values(vc, b, av);
-          weigh(s, ph);
+          weigh(s, f, ph);
           accumulate(av, ph);
+          add_low(av, s, ph);
         }
       }
       __syncthreads();
@@ -239,9 +264,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
       float s[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = cur[i];
-      if constexpr (BIAS)
-        add_bias(s, g, tab, kb - (i0 + 31 + off), kb + 31 - (i0 + off),
-                 [&](int i) { return kb + c_row(i, hh) - iq - off; });
+      const Affine f = biased(s, kb);
       if (kb + 31 > all_see) {
         asm volatile("");  // a branch: blocks that every query sees do not pay for it
         const int seen = last - kb - 4 * hh;
@@ -249,14 +272,10 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
         for (int i = 0; i < 16; ++i)
           if (c_row(i, 0) > seen) s[i] = -INFINITY;
       }
-      raise_to(s);
-      weigh(s, ph);
+      raise_to(s, f);
+      weigh(s, f, ph);
       accumulate(av, ph);
-      if constexpr (RES) {
-        Frag pl[2];
-        to_low_frags(s, ph, pl);
-        accumulate(av, pl);
-      }
+      add_low(av, s, ph);
     }
     wait_copies();
     __syncthreads();
@@ -279,11 +298,11 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
 // dq pass: 128 queries of one head against the keys they see,
 //   alpha = exp2(t - lse),  dP^T = V dout^T,  dS = alpha (dP - Delta),  dq^T += K^T dS^T,
 // and Delta = <dout, out + out_res>, kept with lse log2(e) for the dk/dv pass, head by head.  The
-// bias gradient sums dS by distance: distances inside the table in LDS, in an array of their own
-// for each half of each wave, where one instruction's 32 lanes have 32 different distances
-// (queries i .. i + 31 and one key), so that no two of its additions meet and the order of all is
-// the program's; distances at and beyond the ends in a register per lane.  The workgroup's sums by
-// bucket go to `partial`.
+// bias gradient sums dS by distance: a block that reaches into the table is written to LDS with
+// its diagonals as rows, whose sums, one per lane, are added to the wave's sums by distance (with
+// LDS atomics, 140 cycles each, the pass took 153 us for 4,096 tokens of 16 heads x 64, 66 without
+// the gradient, and takes 78 this way); the other blocks go to a register per lane and side.  The
+// workgroup's sums by bucket go to `partial`.  Every order is fixed.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
@@ -298,7 +317,9 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
   __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
-  extern __shared__ float tab[];  // bias by distance; 8 arrays of sums by distance; 8 x 2 ends
+  // for the bias gradient the waves' skewed blocks; the bias by distance; the waves' sums by
+  // distance, 8 ends
+  extern __shared__ __attribute__((aligned(16))) float room[];
 
   Work w;
   if (!work_of(g.q_tiles, g.group, w)) return;
@@ -333,11 +354,20 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   const int i0 = q0 + wave * 32, iq = i0 + (lane & 31);
   const bool qok = iq < n, live = i0 < n;
   const int64_t qrow = sq.begin + (qok ? iq : 0), row = qrow * g.H + w.head;
-  float* sums = tab + g.span + (wave * 2 + hh) * g.span;
+  const int stride = padded(g.span);
+  float *tab = room, *all_sums = room, *ends = room, *skewed = room;
+  if (BIAS && partial != nullptr) {
+    tab = room + 4 * kSkewed;
+    all_sums = tab + stride;
+    ends = all_sums + 4 * stride;
+  }
+  const bool want_table = BIAS && partial != nullptr;
   if constexpr (BIAS) {
     fill_bias(tab, g, table, map, w.head);
-    if (partial != nullptr)
-      for (int i = threadIdx.x; i < 8 * g.span; i += kThreads) tab[g.span + i] = 0.0f;
+    if (want_table)
+      for (int i = threadIdx.x; i < 4 * kSkewed; i += kThreads) skewed[i] = 0.0f;
+    if (want_table)
+      for (int i = threadIdx.x; i < 4 * stride; i += kThreads) all_sums[i] = 0.0f;
   }
   Frag qf[KS], gf[KS];
   load_frag<T, D>(qf, q + qrow * g.qs + w.head * D, qok);
@@ -374,7 +404,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   f32x16_t acc[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) acc[db] = f32x16_t{};
-  float behind = 0.0f, ahead = 0.0f;
+  float behind = 0.0f, ahead = 0.0f, inside = 0.0f, p_behind = 0.0f, p_ahead = 0.0f;
 
   // S^T = K Q^T and dP^T = V dout^T of a block
   auto products = [&](const T* kc, int b, f32x16_t& sa, f32x16_t& pa) {
@@ -395,13 +425,68 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
       for (int db = 0; db < DB; ++db)
         acc[db] = mfma(Tl::a_cols(kc, db * 32, b, p), df[p], acc[db]);
   };
+  auto biased = [&](float (&s)[16], int kb) {
+    if constexpr (BIAS)
+      return add_bias<1>(s, g, tab, kb - (i0 + 31 + off), kb + 4 * hh - iq - off);
+    else
+      return Affine{g.scale_log2, 0.0f};
+  };
+  // alpha in place of the logits, and dS
+  auto weigh = [&](float (&s)[16], const Affine& f, const f32x16_t& pa, float (&ds)[16]) {
+    const float add = f.add - lse2;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], f.mul, add));
+      ds[i] = s[i] * (pa[i] - dl);
+    }
+  };
+  // dS by distance: blocks outside the table have one place, the others one per diagonal.  A row's
+  // dS add up to what its Delta is off (times alpha), which the outer places, where alpha is
+  // largest, take back at the end.
+  auto count = [&](const float (&p)[16], const float (&ds)[16], int kb) {
+    if (!want_table) return;
+    const int d_lo = kb - (i0 + 31 + off);
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sum += ds[i];
+    if (outside(g, d_lo)) {
+      float all = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) all += p[i];
+      if (d_lo >= g.rel_min) {
+        ahead += sum;
+        p_ahead += all;
+      } else {
+        behind += sum;
+        p_behind += all;
+      }
+    } else {
+      inside += sum;
+      float* mine = skewed + wave * kSkewed;
+      float* to = mine + (4 * hh - (lane & 31) + 31) * kSkew + 4 * hh;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[c_row(i, 0) * (kSkew + 1)] = ds[i];
+      if (lane < 63) {  // one diagonal per lane
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const float4 x = *reinterpret_cast<const float4*>(mine + lane * kSkew + 4 * r);
+          sum.x += x.x;
+          sum.y += x.y;
+          sum.z += x.z;
+          sum.w += x.w;
+        }
+        all_sums[wave * stride + kPad + d_lo - g.rel_min + lane] += (sum.x + sum.y) + (sum.z + sum.w);
+      }
+    }
+  };
   wait_copies();
   __syncthreads();
 
   // As in the forward: tiles that every query sees whole, the next block's products beside this
   // block's vector work; then the tiles with a mask or a bias.
   int kt = 0;
-  if constexpr (!BIAS) {
+  {
     const int whole = q0 + kSeqTile <= n ? (g.causal ? min(m, max(q0 + off + 1, 0)) : m) / KT : 0;
     f32x16_t sa, pa;
     if (whole > 0) products(lds, 0, sa, pa);
@@ -410,17 +495,19 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
       if (t + 1 < ntiles) fetch(t + 1, 1 - buf);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        float ds[16];
-        const f32x16_t s0 = sa, p0 = pa;
+        float s[16], ds[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = sa[i];
+        const f32x16_t p0 = pa;
+        const Affine f = biased(s, t * KT + b * 32);
         if (b == NB - 1) {  // the next tile is in LDS
           wait_copies();
           __syncthreads();
         }
         if (b + 1 < NB) products(kc, b + 1, sa, pa);
         else products(kn, 0, sa, pa);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          ds[i] = __builtin_amdgcn_exp2f(fmaf(s0[i], g.scale_log2, -lse2)) * (p0[i] - dl);
+        weigh(s, f, p0, ds);
+        count(s, ds, t * KT + b * 32);
         accumulate(kc, b, ds);
       }
       __syncthreads();
@@ -445,44 +532,16 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
       float s[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = sa[i];
-      const int d_lo = kb - (i0 + 31 + off), d_hi = kb + 31 - (i0 + off);
-      if constexpr (BIAS)
-        add_bias(s, g, tab, d_lo, d_hi, [&](int i) { return kb + c_row(i, hh) - iq - off; });
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float p = __builtin_amdgcn_exp2f(BIAS ? s[i] - lse2
-                                                    : fmaf(s[i], g.scale_log2, -lse2));
-        ds[i] = p * (pa[i] - dl);
-      }
+      const Affine f = biased(s, kb);
+      weigh(s, f, pa, ds);
       if (kb + 31 > all_see || i0 + 31 >= n) {
         asm volatile("");
         const int seen = qok ? last - kb - 4 * hh : -1;
 #pragma unroll
         for (int i = 0; i < 16; ++i)
-          if (c_row(i, 0) > seen) ds[i] = 0.0f;
+          if (c_row(i, 0) > seen) s[i] = ds[i] = 0.0f;
       }
-      if (BIAS && partial != nullptr) {
-        const int end = g.span - 1;
-        if (d_hi <= g.rel_min || d_lo >= g.rel_min + end) {
-          float sum = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sum += ds[i];
-          if (d_hi <= g.rel_min) behind += sum;
-          else ahead += sum;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int idx = kb + c_row(i, hh) - iq - off - g.rel_min;
-            if (idx <= 0) {
-              behind += ds[i];
-            } else if (idx >= end) {
-              ahead += ds[i];
-            } else {
-              __builtin_amdgcn_ds_atomic_fadd_f32((__attribute__((address_space(3))) float*)(sums + idx), ds[i]);
-            }
-          }
-        }
-      }
+      count(s, ds, kb);
       accumulate(kc, b, ds);
     }
     wait_copies();
@@ -491,32 +550,48 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   if (live)
     store_rows<T, D>(lds + wave * 32 * D, acc, g.scale,
                      dq + ((int64_t)(sq.begin + i0) * g.H + w.head) * D, (int64_t)g.H * D, n - i0);
-  if (BIAS && partial != nullptr) {
-    // the lanes' ends join in a fixed tree
+  if (want_table) {
+    const float error = pair_sum(behind + inside + ahead);
+    behind -= p_behind * error;
+    ahead -= p_ahead * error;
+    // the lanes' ends join in a fixed tree, the arrays in their order, then the distances of a
+    // bucket: kThreads / width threads each
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
       behind += __shfl_xor(behind, d);
       ahead += __shfl_xor(ahead, d);
     }
-    float* ends = tab + 9 * g.span;
     if (lane == 0) {
       ends[2 * wave] = behind;
       ends[2 * wave + 1] = ahead;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < g.span; i += kThreads) {
+    for (int i = threadIdx.x; i < padded(g.span); i += kThreads) {
       float sum = 0.0f;
 #pragma unroll
-      for (int a = 0; a < 8; ++a) sum += tab[g.span * (1 + a) + i];
-      if (i == 0) sum += (ends[0] + ends[2]) + (ends[4] + ends[6]);
-      if (i == g.span - 1) sum += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+      for (int a = 0; a < 4; ++a) sum += all_sums[a * stride + i];
       tab[i] = sum;
     }
     __syncthreads();
-    for (int c = threadIdx.x; c < g.nb; c += kThreads) {
-      float sum = 0.0f;
-      for (int i = 0; i < g.span; ++i) sum += map[i] == c ? tab[i] : 0.0f;
-      partial[((int64_t)w.slot * g.H + w.head) * g.nb + c] = sum;
+    int* which = reinterpret_cast<int*>(all_sums);
+    for (int i = threadIdx.x; i < padded(g.span); i += kThreads)
+      which[i] = map[min(max(i - kPad, 0), g.span - 1)];
+    __syncthreads();
+    int width = 1;
+    while (width < g.nb) width <<= 1;
+    const int c = threadIdx.x % width, first = threadIdx.x / width, lanes = kThreads / width;
+    float sum = 0.0f;
+    for (int i = first; i < padded(g.span); i += lanes) sum += which[i] == c ? tab[i] : 0.0f;
+    if (first == 0) {
+      if (which[0] == c) sum += (ends[0] + ends[2]) + (ends[4] + ends[6]);
+      if (which[padded(g.span) - 1] == c) sum += (ends[1] + ends[3]) + (ends[5] + ends[7]);
+    }
+    __syncthreads();
+    tab[threadIdx.x] = sum;
+    __syncthreads();
+    if ((int)threadIdx.x < g.nb) {
+      for (int j = 1; j < lanes; ++j) sum += tab[j * width + threadIdx.x];
+      partial[((int64_t)w.slot * g.H + w.head) * g.nb + threadIdx.x] = sum;
     }
   }
 }
@@ -622,8 +697,9 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       pa = mfma(ag[ks], vf[ks], pa);
     }
   };
-  // alpha in place of the logits (base 2 where there is a bias), and dS
-  auto weigh = [&](int buf, int b, float (&s)[16], const f32x16_t& pa, float (&ds)[16]) {
+  // alpha in place of the logits, and dS
+  auto weigh = [&](int buf, int b, float (&s)[16], const Affine& f, const f32x16_t& pa,
+                   float (&ds)[16]) {
 #pragma unroll
     for (int blk = 0; blk < 4; ++blk) {
       const int at = b * 32 + 8 * blk + 4 * hh;
@@ -633,10 +709,16 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int i = 4 * blk + j;
-        s[i] = __builtin_amdgcn_exp2f(BIAS ? s[i] - lv[j] : fmaf(s[i], g.scale_log2, -lv[j]));
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], f.mul, f.add - lv[j]));
         ds[i] = s[i] * (pa[i] - dl[j]);
       }
     }
+  };
+  auto biased = [&](float (&s)[16], int qb) {
+    if constexpr (BIAS)
+      return add_bias<-1>(s, g, tab, j0 - (qb + 31 + off), jk - qb - 4 * hh - off);
+    else
+      return Affine{g.scale_log2, 0.0f};
   };
   auto accumulate = [&](const T* qc, int b, const float (&p)[16], const float (&ds)[16]) {
     Frag pf[2], df[2];
@@ -662,8 +744,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       }
     }
     __syncthreads();
-    // Tiles of this head whose queries all exist and see all of the workgroup's keys, without a
-    // bias: the next block's products beside this block's vector work.
+    // Tiles of this head whose queries all exist and see all of the workgroup's keys: the next
+    // block's products beside this block's vector work.
     // (From an even tile on, so that the LDS buffers' places are constants.)
     const int to_end = min(t1 - it, (n - qbase) / QT);  // full tiles up to the head's end
     if (!BIAS && sizeof(T) == 2 && to_end > 0 && ((it - t0) & 1) == 0 &&
@@ -678,13 +760,14 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = sa[i];
           const f32x16_t p0 = pa;
+          const Affine f = biased(s, q_first + t % per_head * QT + b * 32);
           if (b == NB - 1) {  // the next tile is in LDS
             wait_copies();
             __syncthreads();
           }
           if (b + 1 < NB) products(qc, b + 1, sa, pa);
           else products(qn, 0, sa, pa);
-          weigh(buf, b, s, p0, ds);
+          weigh(buf, b, s, f, p0, ds);
           accumulate(qc, b, s, ds);
         }
         __syncthreads();
@@ -710,10 +793,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       float s[16], ds[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = sa[i];
-      if constexpr (BIAS)
-        add_bias(s, g, tab, j0 - (qb + 31 + off), j0 + 31 - (qb + off),
-                 [&](int i) { return jk - qb - c_row(i, hh) - off; });
-      weigh(buf, b, s, pa, ds);
+      weigh(buf, b, s, biased(s, qb), pa, ds);
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
         // queries before the key, and rows past the sequence's end
         asm volatile("");
@@ -845,9 +925,9 @@ void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __res
     if (!second) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = x[i];
+      Affine f = {g.scale_log2, 0.0f};
       if constexpr (BIAS)
-        add_bias(y, g, tab, j0 - (qb + 31 + off), j0 + 31 - (qb + off),
-                 [&](int i) { return jk - qb - c_row(i, hh) - off; });
+        f = add_bias<-1>(y, g, tab, j0 - (qb + 31 + off), jk - qb - 4 * hh - off);
 #pragma unroll
       for (int blk = 0; blk < 4; ++blk) {
         const float4 l4 = *reinterpret_cast<const float4*>(st + 8 * blk);
@@ -855,8 +935,7 @@ void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __res
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int i = 4 * blk + j;
-          const float at = kAlphaScale - lv[j];
-          y[i] = __builtin_amdgcn_exp2f(BIAS ? y[i] + at : fmaf(y[i], g.scale_log2, at));
+          y[i] = __builtin_amdgcn_exp2f(fmaf(y[i], f.mul, f.add + kAlphaScale - lv[j]));
         }
       }
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
@@ -993,7 +1072,7 @@ hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
   }
   SeqGeometry h = g;
   h.q_tiles = seq_spread(g.KH, g.nq / (W * 32) + g.B + 1);
-  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64, bias ? g.span * 4 : 0,
+  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64, bias ? padded(g.span) * 4 : 0,
                 s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
                 out, res, lse);
 }
@@ -1049,7 +1128,9 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
   if (g.nq > 0) {
     const void* fn = bias ? (const void*)&seq_dq_kernel<T, D, true>
                           : (const void*)&seq_dq_kernel<T, D, false>;
-    const size_t lds = !bias ? 0 : partial ? (size_t)g.span * 36 + 64 : (size_t)g.span * 4;
+    const size_t lds = !bias     ? 0
+                       : partial ? 4 * (5 * (size_t)padded(g.span) + 8 + 4 * kSkewed)
+                                 : 4 * (size_t)padded(g.span);
     e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), kThreads, lds, s, g, q, k, v,
                t.cu_q, t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, lse2, partial);
   }
@@ -1070,7 +1151,7 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
                          : (const void*)&seq_dkdv_pair_kernel<T, false, true>)
                  : (bias ? (const void*)&seq_dkdv_pair_kernel<T, true, false>
                          : (const void*)&seq_dkdv_pair_kernel<T, false, false>);
-    e = launch(fn, grid, D == 64 ? kThreads : 512, bias ? (size_t)g.span * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
+    e = launch(fn, grid, D == 64 ? kThreads : 512, bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
                t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
                part_dv);
   }
