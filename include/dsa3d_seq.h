@@ -26,7 +26,10 @@
  * validation first, no allocation, no synchronisation).  float32 and bf16 storage; logits,
  * softmax statistics and sums are float32.  With bf16, alpha and dS enter their second products
  * rounded to bf16 (half a unit in the last place each, as the output's own rounding), unless
- * out_res is asked for.
+ * out_res is asked for.  float32 products are made of bf16 parts to 2^-20 of a product, and an
+ * infinity in a float32 tensor becomes NaN.  What is hidden has weight 0: a NaN or an infinity
+ * among the keys or values of a sequence can make NaN of queries of that sequence that do not see
+ * it, but never of another sequence's, and what lies behind a sequence's end is never used.
  *
  * Values in device memory cannot be checked on the host.  cu must not decrease; entries outside
  * [0, rows] are clamped to it, so that a wrong one gives wrong results but no access outside the
@@ -86,8 +89,9 @@ dsa3d_status dsa3d_seq_forward(const dsa3d_seq_desc* desc, const void* q, const 
                                const float* bias_table, const int32_t* bias_map, void* out,
                                void* out_res, float* lse, hipStream_t stream);
 
-/* Workspace bytes dsa3d_seq_backward needs (0 for a descriptor it would reject): 4 per query
- * row and head, and with a bias 4 rel_buckets per head and 128-query tile. */
+/* Workspace bytes dsa3d_seq_backward needs (0 for a descriptor it would reject): 8 per query
+ * row and head, with a bias 4 rel_buckets per head and 128-query tile, and where there are few
+ * keys float32 parts of dk and dv, up to 16 of them. */
 size_t dsa3d_seq_backward_workspace_size(const dsa3d_seq_desc* desc);
 
 /* Backward for upstream gradient dout, alpha recomputed from lse:

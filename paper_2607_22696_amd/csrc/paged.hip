@@ -161,10 +161,10 @@ __device__ inline void add_bias(float (&s)[16], const PagedGeometry& g, const fl
 
 // ------------------------------------------------------------------------- many rows
 
-// Where the cache rows of the 64 keys from `base` on lie, in bytes, by the first wave.  A key without a place (past the
-// part's keys, or a page number outside the tensors) gets the row of one that has one, so that
-// what is copied is what some query sees, and is left out of the mask; a tile with none has mask 0
-// and rows that are never read.
+// Where the cache rows of the 64 keys from `base` on lie, in bytes, by the first wave.  A key
+// without a place (past the part's keys, or a page number outside the tensors) gets the row of one
+// that has one, so that what is copied is what some query sees, and is left out of the mask; a tile
+// with none has mask 0 and rows that are never read.
 template <typename T>
 __device__ inline void fill_tile(int64_t* tab, uint64_t* mask, const PagedGeometry& g,
                                  const int32_t* pages, const Span1& s, int base, int keys) {
@@ -187,7 +187,8 @@ __device__ inline void fill_tile(int64_t* tab, uint64_t* mask, const PagedGeomet
 // As the forward of seqattn.hip (tiles copied straight to LDS, a tile's second block multiplied
 // beside the first one's softmax), through the page table.
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                        const T* __restrict__ v, const int32_t* __restrict__ pages,
                        const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ cu_q,
@@ -198,7 +199,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
-  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
+  __shared__ __attribute__((aligned(16))) T lds[Tl::kTwo];  // keys and values
   __shared__ int64_t tab[kRing][KT];
   __shared__ uint64_t there[kRing];
   extern __shared__ float bias[];
@@ -234,9 +235,9 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   Softmax sm;
   const T *kp = k + w.u * D, *vp = v + w.u * D;
   auto fetch = [&](int kt, int buf) {
-    Tl::copy(lds + 2 * E * buf, kp, lds + 2 * E * buf + E, vp, tab[kt % kRing]);
+    Tl::copy(lds + Tl::kPlace * buf, kp, lds + Tl::kPlace * buf + E, vp, tab[kt % kRing]);
   };
-  auto products = [&](const T* kc, int b) {
+  auto products = [&](const uint16_t* kc, int b) {
     Frag a[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(kc, b * 32, ks);
@@ -246,7 +247,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     return acc;
   };
   const float scale = BIAS ? 1.0f : g.scale_log2;
-  auto accumulate = [&](const T* vc, int b, const float (&t)[16]) {
+  auto accumulate = [&](const uint16_t* vc, int b, const float (&t)[16]) {
     Frag pf[2];
     to_frags(t, pf);
 #pragma unroll
@@ -266,7 +267,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(m >> 32)) << 32 |
            (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
   };
-  constexpr uint64_t kFull = KT == 64 ? ~0ull : (1ull << KT) - 1;
+  constexpr uint64_t kFull = ~0ull >> (64 - KT);
 
   __syncthreads();
   if (ntiles > 0) fetch(0, 0);
@@ -277,40 +278,42 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
   const int whole = BIAS ? 0 : max(min(s.k_hi, first_sees + 1) - s.k_lo, 0) / KT;
   int kt = 0;
   while (kt < ntiles) {
-    if ((kt & 1) == 0 && kt < whole && mask_of(kt) == kFull) {
-      f32x16_t next = f32x16_t{};
-      if (live) next = products(lds, 0);
-      auto tile = [&](int t, int buf) {
-        const T *kc = lds + 2 * E * buf, *kn = lds + 2 * E * (1 - buf);
-        advance(t, buf);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float y[16];
-          if (live) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = next[i];
-            sm.raise_to(y, scale, o);
+    if constexpr (sizeof(T) == 2) {
+      if ((kt & 1) == 0 && kt < whole && mask_of(kt) == kFull) {
+        f32x16_t next = f32x16_t{};
+        if (live) next = products(lds, 0);
+        auto tile = [&](int t, int buf) {
+          const T *kc = lds + 2 * E * buf, *kn = lds + 2 * E * (1 - buf);
+          advance(t, buf);
+  #pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            float y[16];
+            if (live) {
+  #pragma unroll
+              for (int i = 0; i < 16; ++i) y[i] = next[i];
+              sm.raise_to(y, scale, o);
+            }
+            if (b == NB - 1) {  // the next tile is in LDS
+              wait_copies();
+              __syncthreads();
+            }
+            if (live) {
+              next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
+              sm.weigh(y, scale);
+              accumulate(kc + E, b, y);
+            }
           }
-          if (b == NB - 1) {  // the next tile is in LDS
-            wait_copies();
-            __syncthreads();
-          }
-          if (live) {
-            next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
-            sm.weigh(y, scale);
-            accumulate(kc + E, b, y);
-          }
-        }
-        __syncthreads();
-      };
-      do {
-        tile(kt++, 0);
-        if (kt >= whole || mask_of(kt) != kFull) break;
-        tile(kt++, 1);
-      } while (kt < whole && mask_of(kt) == kFull);
-      continue;
+          __syncthreads();
+        };
+        do {
+          tile(kt++, 0);
+          if (kt >= whole || mask_of(kt) != kFull) break;
+          tile(kt++, 1);
+        } while (kt < whole && mask_of(kt) == kFull);
+        continue;
+      }
     }
-    const T* kc = lds + 2 * E * (kt & 1);
+    const uint16_t *kc = Tl::operands(lds, kt & 1), *vc = kc + Tl::kSecond;
     advance(kt, kt & 1);
     const int kbase = s.k_lo + kt * KT;
     const uint64_t mask = mask_of(kt);
@@ -334,7 +337,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
       }
       sm.raise_to(y, scale, o);
       sm.weigh(y, scale);
-      accumulate(kc + E, b, y);
+      accumulate(vc, b, y);
     }
     wait_copies();
     __syncthreads();
@@ -362,7 +365,8 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
 // ------------------------------------------------------------------------- few rows
 
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
 void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                        const T* __restrict__ v, const int32_t* __restrict__ pages,
                        const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ cu_q,
@@ -427,7 +431,7 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     if (kb < s.k_hi) {
       Frag a[KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(Ks, wave * 32, ks);
+      for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::rows_of(Ks, wave * 32, ks);
       f32x16_t acc = f32x16_t{};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) acc = mfma(a[ks], qf[ks], acc);
@@ -450,7 +454,7 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int p = 0; p < 2; ++p) o[db] = mfma(Tl::a_cols(Vs, db * 32, wave, p), pf[p], o[db]);
+        for (int p = 0; p < 2; ++p) o[db] = mfma(Tl::cols_of(Vs, db * 32, wave, p), pf[p], o[db]);
     }
     __syncthreads();
   }

@@ -4,10 +4,17 @@
 // Products are those of winattn.hip: 32 x 32 blocks with the transposed result (S^T = K Q^T,
 // O^T = V^T P^T), so that a lane owns one query's (or key's) column.  Operand fragments are the
 // same for both storage types: lane l holds row (or column) l % 32 and the 8 consecutive
-// contraction indices 8 (l / 32) .. +7 of a step of 16.  bf16 multiplies them with one
-// v_mfma_f32_32x32x16_bf16; float32 with eight v_mfma_f32_32x32x2_f32, the e-th taking element e
-// of both halves of the wave, which sums the same 16 products in float32.  The result's lane l
-// holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in its element i, for both.
+// contraction indices 8 (l / 32) .. +7 of a step of 16, multiplied by v_mfma_f32_32x32x16_bf16.
+// The result's lane l holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in its element i.
+//
+// float32 operands are split into three bf16 parts, x = h + m + l exactly (8 significant bits
+// each, by truncation, so m < 2^-7 and l < 2^-14 of x), and six of the nine products are summed in
+// float32: the three left out are below 2^-20 of the product together, 2^-23 on average, next to
+// the 2^-24 of each of its roundings.  Six bf16 products take 192 cycles where the eight
+// v_mfma_f32_32x32x2_f32 of the same 16 indices take 512.  Tiles are split once per workgroup, into
+// three bf16 tiles.  4,096 causal tokens, 8 heads x 128, forward: 594 us with float32 products, 467
+// with operands split as they are read, 389 this way (1,035 at two waves per SIMD, with 102 spilled
+// registers).  An infinity has no such parts: it makes NaN of what it reaches.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -23,6 +30,9 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 struct F32x8 {
   float x[8];
 };
+struct Split {
+  bf16x8_t h, m, l;
+};
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -34,24 +44,46 @@ struct Type;
 template <>
 struct Type<uint16_t> {  // bf16 bit patterns
   using Frag = bf16x8_t;
-  using Alpha = _Float16;  // how one wave hands weights to another
   static constexpr int kKeyTile = 64;
 };
 template <>
 struct Type<float> {
-  using Frag = F32x8;
-  using Alpha = float;
+  using Frag = Split;
   static constexpr int kKeyTile = 32;
 };
 
 __device__ inline f32x16_t mfma(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
-__device__ inline f32x16_t mfma(const F32x8& a, const F32x8& b, f32x16_t c) {
+__device__ inline f32x16_t mfma(const Split& a, const Split& b, f32x16_t c) {
+  c = mfma(a.l, b.h, c);
+  c = mfma(a.h, b.l, c);
+  c = mfma(a.m, b.m, c);
+  c = mfma(a.m, b.h, c);
+  c = mfma(a.h, b.m, c);
+  return mfma(a.h, b.h, c);
+}
+// The parts' upper halves are packed two by two by a byte permute.
+__device__ inline Split split(const F32x8& a) {
+  uint32_t h[4], m[4], l[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.x[e], b.x[e], c, 0, 0, 0);
-  return c;
+  for (int i = 0; i < 4; ++i) {
+    uint32_t hu[2], mu[2], lu[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const float x = a.x[2 * i + j];
+      hu[j] = __float_as_uint(x);
+      const float r = x - __uint_as_float(hu[j] & 0xffff0000u);
+      mu[j] = __float_as_uint(r);
+      lu[j] = __float_as_uint(r - __uint_as_float(mu[j] & 0xffff0000u));
+    }
+    h[i] = __builtin_amdgcn_perm(hu[1], hu[0], 0x07060302u);
+    m[i] = __builtin_amdgcn_perm(mu[1], mu[0], 0x07060302u);
+    l[i] = __builtin_amdgcn_perm(lu[1], lu[0], 0x07060302u);
+  }
+  return {__builtin_bit_cast(bf16x8_t, make_uint4(h[0], h[1], h[2], h[3])),
+          __builtin_bit_cast(bf16x8_t, make_uint4(m[0], m[1], m[2], m[3])),
+          __builtin_bit_cast(bf16x8_t, make_uint4(l[0], l[1], l[2], l[3]))};
 }
 
 __device__ inline bf16x8_t as_bf16x8(const uint4& u) { return __builtin_bit_cast(bf16x8_t, u); }
@@ -230,27 +262,60 @@ struct Tile {
     }
   }
 
-  // Operand with tile rows as its rows: row r0 + l % 32, channels 16 ks + 8 (l / 32) .. +7.
-  static __device__ inline Frag a_rows(const T* lds, int r0, int ks) {
-    const int lane = threadIdx.x & 63, row = r0 + (lane & 31), c = ks * 16 + (lane >> 5) * 8;
+  // Room for two tiles that belong together and for the next two, which are being copied: bf16
+  // alternates between two places; float32 has one, which is free again once it is split.
+  static constexpr int kTwo = (kBf16 ? 4 : 5) * ROWS * D, kPlace = kBf16 ? 2 * ROWS * D : 0;
+  // from the first tile's operands to the second's
+  static constexpr int kSecond = (kBf16 ? 1 : 3) * ROWS * D;
+  // What the operands of the two tiles in place `buf` are read from: the tiles themselves, or the
+  // three bf16 tiles that each of them is split into.
+  static __device__ inline const uint16_t* operands(T* lds, int buf) {
     if constexpr (kBf16) {
+      return lds + kPlace * buf;
+    } else {
+      using Part = Tile<uint16_t, D, ROWS, THREADS>;
+      uint16_t* room = reinterpret_cast<uint16_t*>(lds + 2 * ROWS * D);
+#pragma unroll
+      for (int two = 0; two < 2; ++two)
+#pragma unroll
+        for (int i = 0; i < ROWS * D / 8 / THREADS; ++i) {
+          const int at8 = (int)threadIdx.x + i * THREADS;
+          const int row = at8 / (D / 8), c = at8 % (D / 8) * 8;
+          const T* from = lds + two * ROWS * D;
+          F32x8 x;
+          *reinterpret_cast<float4*>(x.x) = *reinterpret_cast<const float4*>(from + at(row, c));
+          *reinterpret_cast<float4*>(x.x + 4) =
+              *reinterpret_cast<const float4*>(from + at(row, c + 4));
+          const Split y = split(x);
+          uint16_t* to = room + two * kSecond + Part::at(row, c);
+          *reinterpret_cast<bf16x8_t*>(to) = y.h;
+          *reinterpret_cast<bf16x8_t*>(to + ROWS * D) = y.m;
+          *reinterpret_cast<bf16x8_t*>(to + 2 * ROWS * D) = y.l;
+        }
+      __syncthreads();
+      return room;
+    }
+  }
+
+  // Operand with tile rows as its rows: row r0 + l % 32, channels 16 ks + 8 (l / 32) .. +7.
+  static __device__ inline Frag a_rows(const uint16_t* lds, int r0, int ks) {
+    if constexpr (kBf16) {
+      const int lane = threadIdx.x & 63, row = r0 + (lane & 31), c = ks * 16 + (lane >> 5) * 8;
       return as_bf16x8(*reinterpret_cast<const uint4*>(lds + at(row, c)));
     } else {
-      F32x8 f;
-      *reinterpret_cast<float4*>(f.x) = *reinterpret_cast<const float4*>(lds + at(row, c));
-      *reinterpret_cast<float4*>(f.x + 4) = *reinterpret_cast<const float4*>(lds + at(row, c + 4));
-      return f;
+      using Part = Tile<uint16_t, D, ROWS, THREADS>;
+      return {Part::a_rows(lds, r0, ks), Part::a_rows(lds + ROWS * D, r0, ks),
+              Part::a_rows(lds + 2 * ROWS * D, r0, ks)};
     }
   }
   // Operand with channels as its rows: channel d0 + l % 32; tile rows 32 kb + 16 p + 4 (l / 32) +
-  // {0..3, 8..11}, the order in which a result's elements 8 p .. 8 p + 7 hold them.  bf16 by
+  // {0..3, 8..11}, the order in which a result's elements 8 p .. 8 p + 7 hold them.  By
   // ds_read_b64_tr_b16 as in winattn.hip.
-  static __device__ inline Frag a_cols(const T* lds, int d0, int kb, int p) {
-    const int lane = threadIdx.x & 63;
+  static __device__ inline Frag a_cols(const uint16_t* lds, int d0, int kb, int p) {
     if constexpr (kBf16) {
       typedef short s4_t __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s4_t lds_s4_t;
-      const int j = lane & 15;
+      const int lane = threadIdx.x & 63, j = lane & 15;
       const int row = kb * 32 + 16 * p + 4 * (lane >> 5) + (j >> 2);
       const int chan = d0 + 16 * ((lane >> 4) & 1) + 4 * (j & 3);
       const s4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + at(row, chan)));
@@ -258,12 +323,34 @@ struct Tile {
       const uint2 ul = __builtin_bit_cast(uint2, lo), uh = __builtin_bit_cast(uint2, hi);
       return as_bf16x8(make_uint4(ul.x, ul.y, uh.x, uh.y));
     } else {
+      using Part = Tile<uint16_t, D, ROWS, THREADS>;
+      return {Part::a_cols(lds, d0, kb, p), Part::a_cols(lds + ROWS * D, d0, kb, p),
+              Part::a_cols(lds + 2 * ROWS * D, d0, kb, p)};
+    }
+  }
+  // The same operands straight from the tile, split as they are read.
+  static __device__ inline Frag rows_of(const T* lds, int r0, int ks) {
+    if constexpr (kBf16) {
+      return a_rows(lds, r0, ks);
+    } else {
+      const int lane = threadIdx.x & 63, row = r0 + (lane & 31), c = ks * 16 + (lane >> 5) * 8;
+      F32x8 f;
+      *reinterpret_cast<float4*>(f.x) = *reinterpret_cast<const float4*>(lds + at(row, c));
+      *reinterpret_cast<float4*>(f.x + 4) = *reinterpret_cast<const float4*>(lds + at(row, c + 4));
+      return split(f);
+    }
+  }
+  static __device__ inline Frag cols_of(const T* lds, int d0, int kb, int p) {
+    if constexpr (kBf16) {
+      return a_cols(lds, d0, kb, p);
+    } else {
+      const int lane = threadIdx.x & 63;
       F32x8 f;
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         f.x[e] = lds[at(kb * 32 + 16 * p + 8 * (e / 4) + 4 * (lane >> 5) + (e % 4),
                         d0 + (lane & 31))];
-      return f;
+      return split(f);
     }
   }
 };
@@ -279,33 +366,39 @@ __device__ inline void load_frag(typename Type<T>::Frag (&f)[D / 16], const T* r
       if (ok) u = *reinterpret_cast<const uint4*>(row + ks * 16 + hh * 8);
       f[ks] = as_bf16x8(u);
     } else {
-      float4 a = make_float4(0, 0, 0, 0), b = a;
+      F32x8 x = {};
       if (ok) {
-        a = *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8);
-        b = *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8 + 4);
+        *reinterpret_cast<float4*>(x.x) =
+            *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8);
+        *reinterpret_cast<float4*>(x.x + 4) =
+            *reinterpret_cast<const float4*>(row + ks * 16 + hh * 8 + 4);
       }
-      *reinterpret_cast<float4*>(f[ks].x) = a;
-      *reinterpret_cast<float4*>(f[ks].x + 4) = b;
+      f[ks] = split(x);
     }
   }
 }
 
 __device__ inline float frag_at(const bf16x8_t& f, int e) { return (float)f[e]; }
-__device__ inline float frag_at(const F32x8& f, int e) { return f.x[e]; }
+__device__ inline float frag_at(const Split& f, int e) {
+  return (float)f.h[e] + ((float)f.m[e] + (float)f.l[e]);
+}
 
 // Sixteen result values as fragments (elements 8 p .. 8 p + 7) of the next product, rounded to
-// the nearest bf16, or as they are.
+// the nearest bf16, or split.
 __device__ inline void to_frags(const float (&x)[16], bf16x8_t (&f)[2]) {
 #pragma unroll
   for (int p = 0; p < 2; ++p)
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[p][e] = (__bf16)x[8 * p + e];
 }
-__device__ inline void to_frags(const float (&x)[16], F32x8 (&f)[2]) {
+__device__ inline void to_frags(const float (&x)[16], Split (&f)[2]) {
 #pragma unroll
-  for (int p = 0; p < 2; ++p)
+  for (int p = 0; p < 2; ++p) {
+    F32x8 y;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[p].x[e] = x[8 * p + e];
+    for (int e = 0; e < 8; ++e) y.x[e] = x[8 * p + e];
+    f[p] = split(y);
+  }
 }
 // x - bf16(x), exact in float32, rounded once: hi + lo carry x to within 2^-17 |x|.
 __device__ inline void to_low_frags(const float (&x)[16], const bf16x8_t (&hi)[2],
@@ -336,23 +429,6 @@ __device__ inline void take_over(const _Float16* from, float (&x)[16]) {
     for (int e = 0; e < 8; ++e) x[8 * p + e] = (float)h[e];
   }
 }
-__device__ inline void hand_over(float* to, const float (&x)[16]) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p)
-    *reinterpret_cast<float4*>(to + 4 * p) =
-        make_float4(x[4 * p], x[4 * p + 1], x[4 * p + 2], x[4 * p + 3]);
-}
-__device__ inline void take_over(const float* from, float (&x)[16]) {
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const float4 y = *reinterpret_cast<const float4*>(from + 4 * p);
-    x[4 * p] = y.x;
-    x[4 * p + 1] = y.y;
-    x[4 * p + 2] = y.z;
-    x[4 * p + 3] = y.w;
-  }
-}
-
 // Stores 16 values of channel block db (channels 32 db + 8 blk + 4 (l / 32) + j) times mul.
 __device__ inline void store_block(float* row, int db, const f32x16_t& acc, float mul) {
   const int hh = (threadIdx.x & 63) >> 5;

@@ -72,7 +72,8 @@ __device__ inline Affine add_bias(float (&s)[16], const SeqGeometry& g, const fl
 
 // W waves of 32 queries each; KT keys per LDS tile, two tiles of keys and of values in LDS.
 template <typename T, int D, int W, bool BIAS, bool RES>
-__global__ __launch_bounds__(W * 64) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__global__ __launch_bounds__(W * 64)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 || D == 64 ? 2 : 1, 2)))
 void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                     const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                     const int32_t* __restrict__ cu_k, const float* __restrict__ table,
@@ -85,8 +86,8 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
   constexpr bool kThroughLds = sizeof(T) == 2;  // queries and results fit a pair of tiles
   static_assert(!kThroughLds || Rows::kElems == 2 * E, "two tiles hold the queries");
-  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
-  extern __shared__ float tab[];                         // the bias by distance
+  __shared__ __attribute__((aligned(16))) T lds[Tl::kTwo];  // keys and values
+  extern __shared__ float tab[];                           // the bias by distance
 
   Work w;
   if (!work_of(g.q_tiles, g.group, w)) return;
@@ -114,8 +115,8 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   Tl::copy_plan(vo, vsb);
   auto fetch = [&](int kt, int buf) {
     const int64_t at = (int64_t)kt * KT;
-    Tl::copy(lds + 2 * E * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
-    Tl::copy(lds + 2 * E * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
+    Tl::copy(lds + Tl::kPlace * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
+    Tl::copy(lds + Tl::kPlace * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
   };
   Frag qf[KS];
   if constexpr (kThroughLds) {
@@ -145,7 +146,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
   float mx_run = -INFINITY, l = 0.0f, base = 0.0f;  // base: mx_run, 0 while there is none
 
-  auto logits = [&](const T* kb, int b) {
+  auto logits = [&](const uint16_t* kb, int b) {
     Frag a[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(kb, b * 32, ks);
@@ -187,7 +188,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
     else
       return Affine{g.scale_log2, 0.0f};
   };
-  auto values = [&](const T* vc, int b, Frag (&av)[DB][2]) {
+  auto values = [&](const uint16_t* vc, int b, Frag (&av)[DB][2]) {
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -211,7 +212,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   // cores while this block's exponentials are on the vector ALU.  Two tiles per turn, so that the
   // LDS buffers' places are constants.
   int kt = 0;
-  {
+  if constexpr (sizeof(T) == 2) {
     const int whole = (g.causal ? min(m, q0 + off + 1) : m) / KT;
     f32x16_t next = f32x16_t{};
     if (whole > 0 && live) next = logits(lds, 0);
@@ -250,7 +251,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
     if (kt < whole) tile(kt++, 0);
   }
   for (; kt < ntiles; ++kt) {
-    const T *kc = lds + 2 * E * (kt & 1), *vc = kc + E;
+    const uint16_t *kc = Tl::operands(lds, kt & 1), *vc = kc + Tl::kSecond;
     if (kt + 1 < ntiles) fetch(kt + 1, (kt + 1) & 1);
     const int kbase = kt * KT;
     const int nb = wave_last < kbase ? 0 : min(NB, (wave_last - kbase) / 32 + 1);
@@ -304,7 +305,8 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
 // the gradient, and takes 78 this way); the other blocks go to a register per lane and side.  The
 // workgroup's sums by bucket go to `partial`.  Every order is fixed.
 template <typename T, int D, bool BIAS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 || D == 64 ? 2 : 1, 2)))
 void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                    const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                    const int32_t* __restrict__ cu_k, const float* __restrict__ table,
@@ -316,7 +318,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
-  __shared__ __attribute__((aligned(16))) T lds[4 * E];  // keys, values of tile 0, of tile 1
+  __shared__ __attribute__((aligned(16))) T lds[Tl::kTwo];  // keys and values
   // for the bias gradient the waves' skewed blocks; the bias by distance; the waves' sums by
   // distance, 8 ends
   extern __shared__ __attribute__((aligned(16))) float room[];
@@ -345,8 +347,8 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   Tl::copy_plan(vo, vsb);
   auto fetch = [&](int kt, int buf) {
     const int64_t at = (int64_t)kt * KT;
-    Tl::copy(lds + 2 * E * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
-    Tl::copy(lds + 2 * E * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
+    Tl::copy(lds + Tl::kPlace * buf, kp + at * g.ks, ko, ksb, m - kt * KT);
+    Tl::copy(lds + Tl::kPlace * buf + E, vp + at * g.vs, vo, vsb, m - kt * KT);
   };
   if (ntiles > 0) fetch(0, 0);
 
@@ -407,16 +409,16 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   float behind = 0.0f, ahead = 0.0f, inside = 0.0f, p_behind = 0.0f, p_ahead = 0.0f;
 
   // S^T = K Q^T and dP^T = V dout^T of a block
-  auto products = [&](const T* kc, int b, f32x16_t& sa, f32x16_t& pa) {
+  auto products = [&](const uint16_t* kc, int b, f32x16_t& sa, f32x16_t& pa) {
     sa = f32x16_t{};
     pa = f32x16_t{};
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       sa = mfma(Tl::a_rows(kc, b * 32, ks), qf[ks], sa);
-      pa = mfma(Tl::a_rows(kc + E, b * 32, ks), gf[ks], pa);
+      pa = mfma(Tl::a_rows(kc + Tl::kSecond, b * 32, ks), gf[ks], pa);
     }
   };
-  auto accumulate = [&](const T* kc, int b, const float (&ds)[16]) {
+  auto accumulate = [&](const uint16_t* kc, int b, const float (&ds)[16]) {
     Frag df[2];
     to_frags(ds, df);
 #pragma unroll
@@ -476,7 +478,8 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
           sum.z += x.z;
           sum.w += x.w;
         }
-        all_sums[wave * stride + kPad + d_lo - g.rel_min + lane] += (sum.x + sum.y) + (sum.z + sum.w);
+        all_sums[wave * stride + kPad + d_lo - g.rel_min + lane] +=
+            (sum.x + sum.y) + (sum.z + sum.w);
       }
     }
   };
@@ -486,7 +489,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   // As in the forward: tiles that every query sees whole, the next block's products beside this
   // block's vector work; then the tiles with a mask or a bias.
   int kt = 0;
-  {
+  if constexpr (sizeof(T) == 2) {
     const int whole = q0 + kSeqTile <= n ? (g.causal ? min(m, max(q0 + off + 1, 0)) : m) / KT : 0;
     f32x16_t sa, pa;
     if (whole > 0) products(lds, 0, sa, pa);
@@ -519,7 +522,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
     if (kt < whole) tile(kt++, 0);
   }
   for (; kt < ntiles; ++kt) {
-    const T* kc = lds + 2 * E * (kt & 1);
+    const uint16_t* kc = Tl::operands(lds, kt & 1);
     if (kt + 1 < ntiles) fetch(kt + 1, (kt + 1) & 1);
     const int kbase = kt * KT;
     const int nb = wave_last < kbase ? 0 : min(NB, (wave_last - kbase) / 32 + 1);
@@ -617,13 +620,15 @@ __global__ __launch_bounds__(256) void seq_table_kernel(int slots, int heads, in
   }
 }
 
-// dk/dv pass at 64 channels: 128 keys of one key head (wave w owns keys 32 w .. +31, lanes l and
-// l ^ 32 share key l % 32) against the queries that see them, head by head of the group:
+// dk/dv pass (float32, and bf16 at 64 channels): 128 keys of one key head (wave w owns keys 32 w ..
+// +31, lanes l and l ^ 32 share key l % 32) against the queries that see them, head by head of the
+// group:
 //   S = Q K^T,  dP = dout V^T,  dv^T += dout^T alpha,  dk^T += Q^T dS.
 // With PARTS the (head, query tile) pairs of a key tile are dealt out to several workgroups,
 // whose float32 sums seq_join_kernel adds.
 template <typename T, int D, bool BIAS, bool PARTS>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 || D == 64 ? 2 : 1, 2)))
 void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
                      const T* __restrict__ v, const int32_t* __restrict__ cu_q,
                      const int32_t* __restrict__ cu_k, const float* __restrict__ table,
@@ -635,7 +640,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   using Tl = Tile<T, D, QT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
-  __shared__ __attribute__((aligned(16))) T lds[4 * E];     // queries, douts of tile 0, of tile 1
+  __shared__ __attribute__((aligned(16))) T lds[Tl::kTwo];       // queries and douts
   __shared__ __attribute__((aligned(16))) float stat[2][2][64];  // lse log2(e), Delta of a tile
   extern __shared__ float tab[];
 
@@ -648,7 +653,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   int qbeg, n;
   key_rows(cu_q, sk.b, g.B, g.nq, qbeg, n);
   const int off = m - n;
-  const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;  // first tile with a query that sees
+  // first tile with a query that sees
+  const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;
   const int per_head = n > q_first ? (n - q_first + QT - 1) / QT : 0;
   const int all = per_head * g.group;
   const int t0 = PARTS ? (int)((int64_t)all * part / g.parts) : 0;
@@ -662,8 +668,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   auto fetch = [&](int it, int buf) {
     const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
     const int64_t row = qbeg + at;
-    Tl::copy(lds + 2 * E * buf, q + row * g.qs + head * D, qo, qsb, n - at);
-    Tl::copy(lds + 2 * E * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
+    Tl::copy(lds + Tl::kPlace * buf, q + row * g.qs + head * D, qo, qsb, n - at);
+    Tl::copy(lds + Tl::kPlace * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
     if (wave < 2)  // the rows' statistics; past the sequence's end the last row's
       copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
              (uint32_t)min(lane, n - at - 1) * 4u, (int64_t)head * g.nq + row);
@@ -682,19 +688,27 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   for (int db = 0; db < DB; ++db) dka[db] = dva[db] = f32x16_t{};
 
   // S = Q K^T and dP = dout V^T of a block: the operands are read together, then multiplied
-  auto products = [&](const T* qc, int b, f32x16_t& sa, f32x16_t& pa) {
-    Frag aq[KS], ag[KS];
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      aq[ks] = Tl::a_rows(qc, b * 32, ks);
-      ag[ks] = Tl::a_rows(qc + E, b * 32, ks);
-    }
+  auto products = [&](const uint16_t* qc, int b, f32x16_t& sa, f32x16_t& pa) {
     sa = f32x16_t{};
     pa = f32x16_t{};
+    if constexpr (sizeof(T) == 2) {
+      Frag aq[KS], ag[KS];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      sa = mfma(aq[ks], kf[ks], sa);
-      pa = mfma(ag[ks], vf[ks], pa);
+      for (int ks = 0; ks < KS; ++ks) {
+        aq[ks] = Tl::a_rows(qc, b * 32, ks);
+        ag[ks] = Tl::a_rows(qc + Tl::kSecond, b * 32, ks);
+      }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sa = mfma(aq[ks], kf[ks], sa);
+        pa = mfma(ag[ks], vf[ks], pa);
+      }
+    } else {  // no room for them all
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        sa = mfma(Tl::a_rows(qc, b * 32, ks), kf[ks], sa);
+        pa = mfma(Tl::a_rows(qc + Tl::kSecond, b * 32, ks), vf[ks], pa);
+      }
     }
   };
   // alpha in place of the logits, and dS
@@ -720,7 +734,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     else
       return Affine{g.scale_log2, 0.0f};
   };
-  auto accumulate = [&](const T* qc, int b, const float (&p)[16], const float (&ds)[16]) {
+  auto accumulate = [&](const uint16_t* qc, int b, const float (&p)[16], const float (&ds)[16]) {
     Frag pf[2], df[2];
     to_frags(p, pf);
     to_frags(ds, df);
@@ -728,7 +742,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        dva[db] = mfma(Tl::a_cols(qc + E, db * 32, b, i), pf[i], dva[db]);
+        dva[db] = mfma(Tl::a_cols(qc + Tl::kSecond, db * 32, b, i), pf[i], dva[db]);
         dka[db] = mfma(Tl::a_cols(qc, db * 32, b, i), df[i], dka[db]);
       }
   };
@@ -748,41 +762,44 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     // block's products beside this block's vector work.
     // (From an even tile on, so that the LDS buffers' places are constants.)
     const int to_end = min(t1 - it, (n - qbase) / QT);  // full tiles up to the head's end
-    if (!BIAS && sizeof(T) == 2 && to_end > 0 && ((it - t0) & 1) == 0 &&
-        (!g.causal || qbase + off >= k0 + kSeqTile - 1)) {
-      f32x16_t sa, pa;
-      auto tile = [&](int t, int buf) {
-        const T *qc = lds + 2 * E * buf, *qn = lds + 2 * E * (1 - buf);
-        if (t + 1 < t1) fetch(t + 1, 1 - buf);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float s[16], ds[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = sa[i];
-          const f32x16_t p0 = pa;
-          const Affine f = biased(s, q_first + t % per_head * QT + b * 32);
-          if (b == NB - 1) {  // the next tile is in LDS
-            wait_copies();
-            __syncthreads();
+    const bool whole = to_end > 0 && ((it - t0) & 1) == 0 &&
+                       (!g.causal || qbase + off >= k0 + kSeqTile - 1);
+    if constexpr (!BIAS && sizeof(T) == 2) {
+      if (whole) {
+        f32x16_t sa, pa;
+        auto tile = [&](int t, int buf) {
+          const T *qc = lds + 2 * E * buf, *qn = lds + 2 * E * (1 - buf);
+          if (t + 1 < t1) fetch(t + 1, 1 - buf);
+  #pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            float s[16], ds[16];
+  #pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = sa[i];
+            const f32x16_t p0 = pa;
+            const Affine f = biased(s, q_first + t % per_head * QT + b * 32);
+            if (b == NB - 1) {  // the next tile is in LDS
+              wait_copies();
+              __syncthreads();
+            }
+            if (b + 1 < NB) products(qc, b + 1, sa, pa);
+            else products(qn, 0, sa, pa);
+            weigh(buf, b, s, f, p0, ds);
+            accumulate(qc, b, s, ds);
           }
-          if (b + 1 < NB) products(qc, b + 1, sa, pa);
-          else products(qn, 0, sa, pa);
-          weigh(buf, b, s, f, p0, ds);
-          accumulate(qc, b, s, ds);
+          __syncthreads();
+        };
+        products(lds, 0, sa, pa);
+        const int end = it + to_end;
+        for (; it + 1 < end; it += 2) {
+          tile(it, 0);
+          tile(it + 1, 1);
         }
-        __syncthreads();
-      };
-      products(lds, 0, sa, pa);
-      const int end = it + to_end;
-      for (; it + 1 < end; it += 2) {
-        tile(it, 0);
-        tile(it + 1, 1);
+        if (it < end) tile(it++, 0);
+        continue;
       }
-      if (it < end) tile(it++, 0);
-      continue;
     }
     const int buf = (it - t0) & 1;
-    const T* qc = lds + 2 * E * buf;
+    const uint16_t* qc = Tl::operands(lds, buf);
     if (it + 1 < t1) fetch(it + 1, 1 - buf);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
@@ -824,7 +841,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   }
 }
 
-// dk/dv pass at 128 channels, where a wave has no room for both sums: two waves share 32 keys (lanes l and l ^ 32 of each share key l % 32):
+// dk/dv pass of bf16 at 128 channels, where a wave has no room for both sums: two waves share 32
+// keys (lanes l and l ^ 32 of each share key l % 32):
 //   waves 0 - 3:  S = Q K^T,  alpha,  dv^T += dout^T alpha
 //   waves 4 - 7:  dP = dout V^T,  dS = alpha (dP - Delta),  dk^T += Q^T dS
 // so that each has one operand and one sum in registers (two waves per SIMD) and two of the four
@@ -835,19 +853,20 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 // 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this 1.18 ms (40% busy).
 constexpr float kAlphaScale = 14.0f;  // base 2
 
-template <typename T, bool BIAS, bool PARTS>
+template <bool BIAS, bool PARTS>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__ k,
-                     const T* __restrict__ v, const int32_t* __restrict__ cu_q,
-                     const int32_t* __restrict__ cu_k, const float* __restrict__ table,
-                     const int32_t* __restrict__ map, const float* __restrict__ delta,
-                     const float* __restrict__ lse2, const T* __restrict__ dout,
-                     T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ part_dk,
-                     float* __restrict__ part_dv) {
+void seq_dkdv_pair_kernel(
+    SeqGeometry g, const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+    const uint16_t* __restrict__ v, const int32_t* __restrict__ cu_q,
+    const int32_t* __restrict__ cu_k, const float* __restrict__ table,
+    const int32_t* __restrict__ map, const float* __restrict__ delta,
+    const float* __restrict__ lse2, const uint16_t* __restrict__ dout, uint16_t* __restrict__ dk,
+    uint16_t* __restrict__ dv, float* __restrict__ part_dk, float* __restrict__ part_dv) {
+  using T = uint16_t;
+  using Alpha = _Float16;
   constexpr int D = 128, QT = Type<T>::kKeyTile;
   using Tl = Tile<T, D, QT, 512>;
   using Frag = typename Type<T>::Frag;
-  using Alpha = typename Type<T>::Alpha;
   constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
   // three tiles of queries and douts: the first waves', the second waves', the next
   __shared__ __attribute__((aligned(16))) T lds[6 * E];
@@ -864,7 +883,8 @@ void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __res
   int qbeg, n;
   key_rows(cu_q, sk.b, g.B, g.nq, qbeg, n);
   const int off = m - n;
-  const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;  // first tile with a query that sees
+  // first tile with a query that sees
+  const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;
   const int per_head = n > q_first ? (n - q_first + QT - 1) / QT : 0;
   const int all = per_head * g.group;
   const int t0 = PARTS ? (int)((int64_t)all * part / g.parts) : 0;
@@ -901,19 +921,11 @@ void seq_dkdv_pair_kernel(SeqGeometry g, const T* __restrict__ q, const T* __res
   // x of a block: S or dP
   auto products = [&](const T* rows, int b) {
     f32x16_t x = f32x16_t{};
-    if constexpr (sizeof(T) == 2) {
-      Frag a[KS];
+    Frag a[KS];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(rows, b * 32, ks);
+    for (int ks = 0; ks < KS; ++ks) a[ks] = Tl::a_rows(rows, b * 32, ks);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) x = mfma(a[ks], wf[ks], x);
-    } else {  // no room for them all
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        x = mfma(Tl::a_rows(rows, b * 32, ks), wf[ks], x);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-    }
+    for (int ks = 0; ks < KS; ++ks) x = mfma(a[ks], wf[ks], x);
     return x;
   };
   // Block b of tile `mine` in LDS buffer `buf`; qb: its first query.
@@ -1072,8 +1084,8 @@ hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
   }
   SeqGeometry h = g;
   h.q_tiles = seq_spread(g.KH, g.nq / (W * 32) + g.B + 1);
-  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64, bias ? padded(g.span) * 4 : 0,
-                s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
+  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64,
+                bias ? padded(g.span) * 4 : 0, s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
                 out, res, lse);
 }
 
@@ -1141,18 +1153,19 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
     const dim3 grid((unsigned)seq_blocks(g.k_tiles, g.parts));
     const bool parts = g.parts > 1;
     const void* fn;
-    if constexpr (D == 64)
+    constexpr bool kPair = sizeof(T) == 2 && D == 128;
+    if constexpr (kPair)
+      fn = parts ? (bias ? (const void*)&seq_dkdv_pair_kernel<true, true>
+                         : (const void*)&seq_dkdv_pair_kernel<false, true>)
+                 : (bias ? (const void*)&seq_dkdv_pair_kernel<true, false>
+                         : (const void*)&seq_dkdv_pair_kernel<false, false>);
+    else
       fn = parts ? (bias ? (const void*)&seq_dkdv_kernel<T, D, true, true>
                          : (const void*)&seq_dkdv_kernel<T, D, false, true>)
                  : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
                          : (const void*)&seq_dkdv_kernel<T, D, false, false>);
-    else
-      fn = parts ? (bias ? (const void*)&seq_dkdv_pair_kernel<T, true, true>
-                         : (const void*)&seq_dkdv_pair_kernel<T, false, true>)
-                 : (bias ? (const void*)&seq_dkdv_pair_kernel<T, true, false>
-                         : (const void*)&seq_dkdv_pair_kernel<T, false, false>);
-    e = launch(fn, grid, D == 64 ? kThreads : 512, bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k,
-               t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
+    e = launch(fn, grid, kPair ? 512 : kThreads, bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k,
+               v, t.cu_q, t.cu_k, t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
                part_dv);
   }
   if (e == hipSuccess && g.nk > 0 && g.parts > 1) {
