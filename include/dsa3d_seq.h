@@ -153,7 +153,7 @@ typedef struct {
 /* Writes rows k, v [total_q][kv_heads][head_dim] (k_stride, v_stride apart) to the new tokens'
  * places in the pages.  Nothing else in the pages is touched; new tokens without a place (a
  * position below 0 or behind the page table, a page number outside the tensors, a row behind the
- * last request) are dropped.  Two tokens with the same place leave either one.
+ * last request) are dropped.  Of two tokens with the same place, each 16 bytes are from either.
  * Errors as for dsa3d_seq_forward. */
 dsa3d_status dsa3d_paged_append(const dsa3d_paged_desc* desc, const void* k, const void* v,
                                 const int32_t* cu_q, const int32_t* kv_lens, const int32_t* pages,

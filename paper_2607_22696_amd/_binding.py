@@ -177,13 +177,13 @@ def make_desc(B, T, H, W, heads, head_dim, kt, kh, kw, dtype="bf16", scale=0.0) 
 
 def _ptr(x):
     """Device pointer of a tensor (or an int address, or None for NULL)."""
-    if x is None or type(x) is int:
+    if x is None or isinstance(x, int):
         return x
     return x.data_ptr()
 
 
 def _stream(stream):
-    if type(stream) is int:
+    if isinstance(stream, int):
         return stream
     if stream is None:
         import torch

@@ -363,11 +363,22 @@ def _rows(chk, name, t, heads, head_dim, dtype, device, rows=None):
     if t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
         chk.problems.append(f"{name}: heads and channels of a row must be contiguous")
         return 0
-    return t.stride(0) if shape[0] > 1 else 0
+    if t.stride(0) < heads * head_dim:  # 0 would select a row's length
+        chk.problems.append(f"{name}: rows overlap (stride {t.stride(0)})")
+        return 0
+    return t.stride(0)
 
 
 def _ints(chk, name, t, shape, device):
     chk.tensor(name, t, shape, torch.int32, device)
+
+
+def _int32(chk, name, x):
+    """An int of the descriptor (ctypes would drop the bits above)."""
+    x = int(x)
+    if not -2 ** 31 <= x < 2 ** 31:
+        chk.problems.append(f"{name}: {x} does not fit 32 bits")
+    return x
 
 
 def _cu(chk, name, t, device):
@@ -395,7 +406,7 @@ def _relative(chk, rel_table, rel_buckets, rel_min, heads, device):
     _ints(chk, "rel_buckets", rel_buckets, tuple(rel_buckets.shape), device)
     if rel_table.shape[0] < 1 or rel_buckets.numel() < 1:
         chk.problems.append("rel_table, rel_buckets: empty")
-    return int(rel_min), rel_buckets.numel(), rel_table.shape[0]
+    return _int32(chk, "rel_min", rel_min), rel_buckets.numel(), rel_table.shape[0]
 
 
 def _lead_rows(chk, q):
@@ -439,7 +450,11 @@ def relative_buckets(num_buckets=32, max_distance=128, both=True, device="cuda")
     buckets hold one distance each, the others widen with the logarithm up to max_distance, from
     where on all distances share the last one.  With `both` keys ahead of the query have buckets
     of their own.  Returns (rel_buckets, rel_min) as the calls below take them."""
-    values, rel_min = dsa3d_relative_buckets(int(num_buckets), int(max_distance), both)
+    chk = _Checks("relative_buckets")
+    num_buckets = _int32(chk, "num_buckets", num_buckets)
+    max_distance = _int32(chk, "max_distance", max_distance)
+    chk.done()
+    values, rel_min = dsa3d_relative_buckets(num_buckets, max_distance, both)
     return torch.tensor(values, dtype=torch.int32, device=device), rel_min
 
 
@@ -603,8 +618,9 @@ def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=
     if need_lse:
         chk.optional("lse", lse, q.shape[:2], torch.float32, dev)
     chk.workspace(workspace, dev)
+    max_kv = _int32(chk, "max_kv", max_kv)
     chk.done()
-    desc = make_paged_desc(batch, nq, heads, kv_heads, D, num, size, columns, int(max_kv), causal,
+    desc = make_paged_desc(batch, nq, heads, kv_heads, D, num, size, columns, max_kv, causal,
                            _IO_DTYPES[q.dtype], scale, lo, span, buckets, qs)
     if out is None:
         out = _like(q, dev)

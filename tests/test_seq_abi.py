@@ -247,3 +247,29 @@ def test_cache_checks():
     raises(ops.paged_append, "v: expected", **dict(k, v=bf(8, 2, 64)))
     raises(ops.paged_append, "k: expected", **dict(k, k=bf(9, 4, 64)))
     raises(ops.paged_append, "k: unsupported dtype", **dict(k, k=bf(9, 2, 64).half()))
+
+
+def test_rows_that_overlap():
+    """A row stride of 0 in a descriptor selects the row itself, so a broadcast tensor is refused
+    before it gets there, as is every stride below a row."""
+    wide = torch.zeros(4096, dtype=torch.bfloat16)
+    a = dict(q=bf(9, 4, 64), k=bf(9, 2, 64), v=bf(9, 2, 64), cu_q=ints(3))
+    for name, heads in (("q", 4), ("k", 2), ("v", 2)):
+        for t in (bf(1, heads, 64).expand(9, heads, 64),
+                  wide.as_strided((9, heads, 64), (64, 64, 1))):
+            raises(ops.seq_forward, f"{name}: rows overlap", **dict(a, **{name: t}))
+    c = dict(k_pages=bf(5, 16, 2, 64), v_pages=bf(5, 16, 2, 64), pages=ints(2, 3), kv_lens=ints(2),
+             cu_q=ints(3))
+    raises(ops.paged_forward, "q: rows overlap", q=bf(1, 4, 64).expand(9, 4, 64), **c)
+    raises(ops.paged_append, "v: rows overlap", k=bf(9, 2, 64), v=bf(1, 2, 64).expand(9, 2, 64),
+           **c)
+
+
+def test_numbers_past_32_bits():
+    c = dict(k_pages=bf(5, 16, 2, 64), v_pages=bf(5, 16, 2, 64), pages=ints(2, 3), kv_lens=ints(2),
+             cu_q=ints(3), q=bf(9, 4, 64))
+    raises(ops.paged_forward, "max_kv: 4294967296 does not fit", max_kv=2 ** 32, **c)
+    a = dict(q=bf(9, 4, 64), k=bf(9, 2, 64), v=bf(9, 2, 64), cu_q=ints(3))
+    raises(ops.seq_forward, "rel_min: -4294967296 does not fit", rel_min=-2 ** 32,
+           rel_table=torch.zeros(6, 4), rel_buckets=ints(5), **a)
+    raises(ops.relative_buckets, "max_distance: 4294967424", max_distance=2 ** 32 + 128)
