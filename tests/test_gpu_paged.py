@@ -259,3 +259,65 @@ def test_a_prompt_read_in_chunks_and_written_on():
     for a, b in ((whole, lse), (got, got_l)):
         near("out", a, o, bd.out(o, mag))
         near("lse", b, l, bd.lse(l))
+
+
+@pytest.mark.parametrize("new", ([1, 2], [100, 1]))
+def test_pages_past_32_bits(new):
+    """Pages that lie 5 GB and more into their tensors: the write finds them, and attention gives
+    the bits that it gives for the same pages in small tensors."""
+    H, KH, D, page, far = 4, 2, 128, 16, 660_000
+    c = Case(140, new, [700, 90], H=H, KH=KH, D=D, page=page)
+    want = c.run()
+    kp, vp = (torch.empty(far + c.kp.shape[0], page, KH, D, dtype=torch.bfloat16, device="cuda")
+              for _ in range(2))
+    assert kp.numel() > 2 ** 31 and kp[:far].numel() * 2 > 5 << 30
+    kp[far:], vp[far:] = c.kp, c.vp
+    small, c.kp, c.vp = (c.kp, c.vp), kp, vp
+    near_pages = c.pages
+    c.pages = np.where(near_pages >= 0, near_pages + far, -1)
+    got = c.run()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    k, v = (torch.randn(sum(new), KH, D, device="cuda").bfloat16() for _ in range(2))
+    rest = (ints(c.held), ints(ref.starts(new)))
+    dsa.paged_append(k, v, *small, ints(near_pages), *rest)
+    dsa.paged_append(k, v, kp, vp, ints(c.pages), *rest)
+    assert torch.equal(kp[far:], small[0]) and torch.equal(vp[far:], small[1])
+
+
+def test_two_graphs_with_one_workspace():
+    cases = [Case(150 + i, new, held, H=8, KH=2, D=128)
+             for i, (new, held) in enumerate((([1, 1, 1], [3000, 40, 900]),
+                                              ([60, 1], [2100, 4000])))]
+    room = torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for c in cases:
+        args = (c.q, c.kp, c.vp, ints(c.pages), ints(c.held), ints(ref.starts(c.new)))
+        want = dsa.paged_forward(*args, need_lse=True)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = dsa.paged_forward(*args, need_lse=True, workspace=room)
+        graphs.append((graph, held, want, args))
+    for i in (0, 1, 1, 0, 0, 1):
+        graph, held, want, _ = graphs[i]
+        for x in held:
+            x.fill_(float("nan"))
+        room.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want))
+
+
+def test_a_padded_batch():
+    """Requests of no new tokens and rows behind the last request, as a batch of fixed size has
+    them: the rows get 0 and -inf, the others what they get without the padding, and the write
+    leaves the pages of requests without new tokens as they were."""
+    c = Case(160, [1, 1, 0, 0], [200, 33, 50, 0], tail=2)
+    out, lse = c.check()
+    assert (out[2:] == 0).all() and torch.isneginf(lse[2:]).all()
+    before = c.kp.clone()
+    k = torch.randn(4, 2, 64, device="cuda").bfloat16()
+    dsa.paged_append(k, k, c.kp, c.vp, ints(c.pages), ints(c.held), ints(ref.starts(c.new)))
+    changed = (c.kp != before).flatten(2).any(-1).nonzero().tolist()
+    assert sorted(changed) == sorted([[int(c.pages[0, 199 // 16]), 199 % 16],
+                                      [int(c.pages[1, 32 // 16]), 32 % 16]])

@@ -238,3 +238,107 @@ def test_wrong_offsets_stay_inside_the_tensors():
         c.backward(out, None, lse)
         torch.cuda.synchronize()
         assert (guard[:32] == 7).all() and (guard[182:] == 7).all()
+
+
+LONG = {
+    "long_128": dict(lengths=[700, 270], H=4, KH=2, D=128),
+    "long_64": dict(lengths=[700, 270], H=3, KH=1),
+    "long_biased": dict(lengths=[700, 270], H=4, KH=2, D=128, bias=(32, 128, True)),
+    "long_other_keys": dict(lengths=[300, 520], keys=[650, 400], H=2, KH=2, D=128),
+}
+
+
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+@pytest.mark.parametrize("causal", (False, True))
+@pytest.mark.parametrize("name", LONG)
+def test_runs_of_whole_tiles(name, causal, dtype):
+    """Sequences of many tiles, most of them seen whole."""
+    Case(100 + len(name), causal=causal, dtype=dtype, **LONG[name]).check(residual=True)
+
+
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_the_widest_bias(dtype, D):
+    """The most distances a bias can tell apart, forward and backward."""
+    c = Case(110, [150, 40], H=2, KH=1, D=D, dtype=dtype, bias=(256, 1023, True))
+    assert len(c.bucket) == dsa.DSA3D_SEQ_MAX_SPAN - 1
+    c.check(residual=True)
+
+
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("how", ("plain", "causal", "bias", "residual"))
+def test_many_queries_of_long_sequences(how, D):
+    """8,320 and 40 tokens of 16 heads, where the forward takes more queries at a time; some of
+    the rows are compared."""
+    lengths, H, KH = [8320, 40], 16, 4
+    nq = sum(lengths)
+    g = torch.Generator().manual_seed(D)
+    q, k, v = (torch.randn(nq, n, D, generator=g).bfloat16().cuda() for n in (H, KH, KH))
+    cu = torch.tensor(ref.starts(lengths), dtype=torch.int32).cuda()
+    causal, kw, table, bucket, rel_min = how != "plain", {}, None, None, 0
+    if how == "bias":
+        bucket, rel_min = dsa.dsa3d_relative_buckets(32, 128, False)
+        table = torch.randn(32, H, generator=g)
+        kw = dict(rel_table=table.cuda(), rel_min=rel_min,
+                  rel_buckets=torch.tensor(bucket, dtype=torch.int32).cuda())
+        table = table.double().numpy()
+    out, lse, res = dsa.seq_forward(q, k, v, cu, causal=causal, need_residual=how == "residual",
+                                    **kw)
+    torch.cuda.synchronize()
+    k64, v64 = (x.double().cpu().numpy() for x in (k, v))
+    rows = [0, 1, 31, 32, 255, 256, 4000, 4127, 8191, 8192, 8300, 8319, 8320, 8359]
+    q64 = q[rows].double().cpu().numpy()
+    for i, row in enumerate(rows):  # a row alone, at the end of the keys that it sees
+        first = 0 if row < 8320 else 8320
+        last = row + 1 if causal else (8320 if row < 8320 else nq)
+        args = ([1], [last - first])
+        o, l, mag = ref.forward(q64[i:i + 1], k64[first:last], v64[first:last], *args, True
+                                if how == "bias" else False, None, table, bucket, rel_min)
+        bd = Bounds("bf16", how == "residual", q64[i:i + 1], k64[first:last], *args, 0.0, table)
+        near("out", out[row:row + 1], o, bd.out(o, mag))
+        near("lse", lse[row:row + 1], l, bd.lse(l))
+        if res is not None:
+            near("out + out_res", out[row:row + 1].double() + res[row:row + 1].double(), o,
+                 bd.read_out(o, mag))
+
+
+def test_rows_far_apart():
+    """q, k and v as columns of one tensor whose rows lie 8 MB apart, 4.8 GB in all, give the bits
+    of contiguous ones."""
+    c = Case(120, [500, 100], H=2, KH=1, causal=True)
+    wide = torch.empty(600, 1 << 22, dtype=torch.bfloat16, device="cuda")
+    out, lse, _ = c.forward()
+    grads = c.backward(out, None, lse)
+    at = 0
+    for name in ("q", "k", "v"):
+        x = getattr(c, name)
+        to = wide[:, at:at + x[0].numel()].unflatten(1, x.shape[1:])
+        to.copy_(x)
+        setattr(c, name, to)
+        at += 1 << 20
+    out2, lse2, _ = c.forward()
+    for a, b in zip((out, lse, *grads), (out2, lse2, *c.backward(out2, None, lse2))):
+        assert torch.equal(a, b)
+
+
+def test_two_graphs_with_one_workspace():
+    """Two captured backward passes that were given the same workspace, replayed in turn."""
+    cases = [Case(130 + i, n, H=4, KH=2, D=128, causal=True, bias=(32, 128, False))
+             for i, n in enumerate(([300, 64], [40, 290, 7]))]
+    room = torch.empty(1 << 23, dtype=torch.uint8, device="cuda")
+    held, want, graphs = [], [], []
+    for c in cases:
+        out, lse, res = c.forward(need_residual=True)
+        want.append(c.backward(out, res, lse))
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held.append(c.backward(out, res, lse, workspace=room))
+        graphs.append((graph, out, lse, res))
+    for i in (0, 1, 1, 0, 0, 1):
+        for x in held[i]:
+            x.fill_(float("nan"))
+        room.fill_(255)
+        graphs[i][0].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held[i], want[i]))
