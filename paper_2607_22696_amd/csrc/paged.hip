@@ -195,7 +195,7 @@ void paged_rows_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
                        const float* __restrict__ table, const int32_t* __restrict__ map,
                        T* __restrict__ out, float* __restrict__ lse, float* __restrict__ part_o,
                        float* __restrict__ part_l) {
-  constexpr int KT = Type<T>::kKeyTile;
+  constexpr int KT = kKeyTile<T, D>;
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
@@ -488,8 +488,8 @@ void paged_keys_kernel(PagedGeometry g, const T* __restrict__ q, const T* __rest
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float f = tops[i][r] == -INFINITY ? totals[i][r]
-                                              : totals[i][r] * __builtin_amdgcn_exp2f(tops[i][r] - tr);
+      float f = totals[i][r];
+      if (tops[i][r] != -INFINITY) f *= __builtin_amdgcn_exp2f(tops[i][r] - tr);
       total += f;
       const float4 y = *reinterpret_cast<const float4*>(
           reinterpret_cast<const float*>(KV) + (i * kFewRows + r) * D + ((chunk ^ (r & 15)) << 2));
@@ -573,9 +573,10 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(int64_t rows, int 
       *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, h);
     }
   }
-  if (lane == 0 && lse != nullptr)
-    lse[row] = total == 0.0f ? -INFINITY
-                             : ((top == -INFINITY ? 0.0f : top) + __builtin_amdgcn_logf(total)) * kLn2;
+  if (lane == 0 && lse != nullptr) {
+    const float base = top == -INFINITY ? 0.0f : top;
+    lse[row] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+  }
 }
 
 // ------------------------------------------------------------------------- append
@@ -641,8 +642,8 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
 
 }  // namespace
 
-// Rows per workgroup: 32 where the requests have no more on average.  Parts of the keys (`splits` at
-// most, of `part` keys at least; a tile whose keys fit one part has no join):
+// Rows per workgroup: 32 where the requests have no more on average.  Parts of the keys (`splits`
+// at most, of `part` keys at least; a tile whose keys fit one part has no join):
 //  - few rows: reading is all, so the key heads, requests and parts make up to 2,048 workgroups,
 //    which also evens out requests of different lengths, in parts of 1,024 keys, or of 512 where
 //    that leaves the card half empty.  64 requests of 200 to 8,000 tokens, 32 / 8 heads x 128:

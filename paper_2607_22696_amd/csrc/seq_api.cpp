@@ -102,7 +102,7 @@ dsa3d_status check_seq(const dsa3d_seq_desc* d, bool own_keys, dsa3d::SeqGeometr
   g->scale_log2 = g->scale * kLog2e;
   g->q_tiles = dsa3d::seq_spread(g->KH, g->nq / dsa3d::kSeqTile + g->B + 1);
   g->k_tiles = dsa3d::seq_spread(g->KH, g->nk / dsa3d::kSeqTile + g->B + 1);
-  g->parts = dsa3d::seq_backward_parts(*g);
+  g->parts = dsa3d::seq_backward_parts(*g, d->dtype == DSA3D_BF16);
   if (dsa3d::seq_blocks(g->q_tiles, g->group) >= kIndexLimit ||
       dsa3d::seq_blocks(g->k_tiles, g->parts) >= kIndexLimit)
     return DSA3D_ERR_INVALID_SHAPE;

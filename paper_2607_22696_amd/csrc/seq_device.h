@@ -44,13 +44,14 @@ struct Type;
 template <>
 struct Type<uint16_t> {  // bf16 bit patterns
   using Frag = bf16x8_t;
-  static constexpr int kKeyTile = 64;
 };
 template <>
 struct Type<float> {
   using Frag = Split;
-  static constexpr int kKeyTile = 32;
 };
+// Rows of a tile of four waves: 64, or 32 where they would be 160 KB in float32.
+template <typename T, int D>
+constexpr int kKeyTile = sizeof(T) * D == 512 ? 32 : 64;
 
 __device__ inline f32x16_t mfma(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
@@ -450,7 +451,7 @@ __device__ inline void store_block(uint16_t* row, int db, const f32x16_t& acc, f
   }
 }
 
-// A wave's 32 results (lane l's column is row l % 32) times mul to rows `first` .. of `to`, `stride`
+// A wave's 32 results (lane l's column is row l % 32) times mul to the rows at `to`, `stride`
 // elements apart, as far as there are `rows`.  bf16 rows pass through LDS, in the wave's own 32
 // rows of `lds`, so that they are written whole, 16 bytes per lane; RES writes what the rounding
 // to bf16 leaves instead.

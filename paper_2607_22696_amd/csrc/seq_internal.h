@@ -42,7 +42,7 @@ struct SeqTensors {
 
 hipError_t launch_seq_forward(const SeqGeometry& g, bool bf16, const SeqTensors& t, void* out,
                               void* out_res, float* lse, hipStream_t stream);
-int seq_backward_parts(const SeqGeometry& g);
+int seq_backward_parts(const SeqGeometry& g, bool bf16);
 size_t seq_backward_workspace(const SeqGeometry& g, bool want_table);
 hipError_t launch_seq_backward(const SeqGeometry& g, bool bf16, const SeqTensors& t,
                                const void* out, const void* out_res, const float* lse,

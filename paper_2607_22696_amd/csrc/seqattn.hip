@@ -79,7 +79,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
                     const int32_t* __restrict__ cu_k, const float* __restrict__ table,
                     const int32_t* __restrict__ map, T* __restrict__ out,
                     T* __restrict__ out_res, float* __restrict__ lse) {
-  constexpr int QT = W * 32, KT = W * (sizeof(T) == 2 ? 16 : 8);
+  constexpr int QT = W * 32, KT = W / 4 * kKeyTile<T, D>;
   using Tl = Tile<T, D, KT, W * 64>;
   using Rows = Tile<T, D, QT, W * 64>;  // a tile of queries, or of results
   using Frag = typename Type<T>::Frag;
@@ -314,7 +314,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
                    const T* __restrict__ out_res, const float* __restrict__ lse,
                    const T* __restrict__ dout, T* __restrict__ dq, float* __restrict__ delta,
                    float* __restrict__ lse2_out, float* __restrict__ partial) {
-  constexpr int KT = Type<T>::kKeyTile;
+  constexpr int KT = kKeyTile<T, D>;
   using Tl = Tile<T, D, KT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
@@ -636,7 +636,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
                      const float* __restrict__ lse2, const T* __restrict__ dout,
                      T* __restrict__ dk, T* __restrict__ dv, float* __restrict__ part_dk,
                      float* __restrict__ part_dv) {
-  constexpr int QT = Type<T>::kKeyTile;
+  constexpr int QT = sizeof(T) == 2 ? 64 : 32;  // float32: room for two workgroups at 64 channels
   using Tl = Tile<T, D, QT>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
@@ -864,7 +864,7 @@ void seq_dkdv_pair_kernel(
     uint16_t* __restrict__ dv, float* __restrict__ part_dk, float* __restrict__ part_dv) {
   using T = uint16_t;
   using Alpha = _Float16;
-  constexpr int D = 128, QT = Type<T>::kKeyTile;
+  constexpr int D = 128, QT = 64;
   using Tl = Tile<T, D, QT, 512>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
@@ -1085,8 +1085,8 @@ hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
   SeqGeometry h = g;
   h.q_tiles = seq_spread(g.KH, g.nq / (W * 32) + g.B + 1);
   return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64,
-                bias ? padded(g.span) * 4 : 0, s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
-                out, res, lse);
+                bias ? padded(g.span) * 4 : 0, s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v,
+                t.cu_q, t.cu_k, t.table, t.map, out, res, lse);
 }
 
 template <typename T, int D>
@@ -1165,8 +1165,8 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
                  : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
                          : (const void*)&seq_dkdv_kernel<T, D, false, false>);
     e = launch(fn, grid, kPair ? 512 : kThreads, bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k,
-               v, t.cu_q, t.cu_k, t.table, t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk,
-               part_dv);
+               v, t.cu_q, t.cu_k, t.table, t.map, (const float*)delta, (const float*)lse2, dout,
+               dk, dv, part_dk, part_dv);
   }
   if (e == hipSuccess && g.nk > 0 && g.parts > 1) {
     const int64_t count = (int64_t)g.nk * g.KH * D / 4;
@@ -1202,10 +1202,14 @@ hipError_t launch_seq_forward(const SeqGeometry& g, bool bf16, const SeqTensors&
 // Parts of the dk/dv pass.  Key heads x key tiles workgroups do the work of all heads of a group;
 // where they are fewer than two per compute unit (four under a causal mask, where the first tiles
 // have twice the average work), the (head, query tile) pairs are dealt out to up to 16 parts.  Key
-// tiles are estimated from the rows and sequences.
-int seq_backward_parts(const SeqGeometry& g) {
+// tiles are estimated from the rows and sequences.  A part has at least 256 queries of a head on
+// average (1,900 tokens, 8 heads x 128, bf16: step of 99 us, 109 with parts of 128), in float32,
+// whose tiles take longer than the join, 64 (1,721 tokens, 6 heads x 64: 234 us with parts of 256,
+// 191 of 128, 170 of 64).
+int seq_backward_parts(const SeqGeometry& g, bool bf16) {
   const int64_t blocks = (int64_t)g.KH * std::max<int64_t>(1, g.nk / kSeqTile);
-  const int64_t most = std::min<int64_t>(16, (int64_t)g.group * std::max(1, g.nq / g.B / 256));
+  const int least = bf16 ? 256 : 64;
+  const int64_t most = std::min<int64_t>(16, (int64_t)g.group * std::max(1, g.nq / g.B / least));
   return (int)std::max<int64_t>(1, std::min<int64_t>((g.causal ? 1024 : 512) / blocks, most));
 }
 
