@@ -542,6 +542,84 @@ __device__ inline void key_rows(const int32_t* cu, int b, int B, int total, int&
   n = __builtin_amdgcn_readfirstlane(max(cu_at(cu, b + 1, total) - begin, 0));
 }
 
+// The sums (largest) of x >= 0 over the wave's lanes up to each: by 1, 2, 4 and 8 lanes within rows
+// of 16, then the first and third row's last lane to the next row, the second's to the two behind.
+template <typename Join>
+__device__ inline int prefix(int x, const Join& join) {
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = join(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  return join(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+}
+__device__ inline int prefix_sum(int x) {
+  return prefix(x, [](int a, int b) { return a + b; });
+}
+__device__ inline int prefix_max(int x) {
+  return prefix(x, [](int a, int b) { return max(a, b); });
+}
+
+// A tile of one side's rows (queries, or keys where KEYS) and the sequence's rows of the other.
+struct Place {
+  int begin, n, tile;   // the sequence's rows on this side, the tile's number among them
+  int other, m;         // and on the other side
+};
+
+// The tile of slot number `slot`.  Up to 63 sequences are held by a lane each, and slots number the
+// tiles from the longest work to the shortest, so that what is dealt out last is short: the work of
+// a tile, in tiles of the other side, is all of them, or under a causal mask one less with every
+// tile from the last query's (first key's) on.  The slot's work is the largest that more than
+// `slot` tiles reach.  More sequences: as they lie, late queries (early keys) first.  Texts of
+// 1,024, 700, 2,048, 311 and 13 tokens, 16 heads x 64, biased step: 202 us as they lie, 191 so; 16
+// causal ones of 1,024, 16 / 4 heads x 128, forward 95 and 89 us, eight of them, step 290 and 278;
+// 32 of 512, 8 heads x 128, all keys, where there is nothing to order, 80 and 86.
+template <int TILE, bool KEYS>
+__device__ inline Place place_of(const int32_t* cu, int total, const int32_t* cu2, int total2,
+                                 int B, int causal, int slots, int slot) {
+  Place p = {};
+  if (B >= 64) {
+    const Slot s = find_slot<TILE>(cu, B, total, 1, KEYS ? slot : slots - 1 - slot);
+    p.begin = s.begin;
+    p.n = s.end - s.begin;
+    p.tile = s.tile;
+    key_rows(cu2, s.b, B, total2, p.other, p.m);
+    return p;
+  }
+  const int lane = threadIdx.x & 63, b = min(lane, B);
+  const int next = min(b + 1, B);  // four loads at once, none behind a branch
+  const int raw0 = cu[b], raw1 = cu[next], raw2 = cu2[b], raw3 = cu2[next];
+  const int begin = b == 0 ? 0 : min(max(raw0, 0), total);
+  const int end = b < B ? min(max(raw1, 0), total) : total;
+  const int other = b == 0 ? 0 : min(max(raw2, 0), total2);
+  const int n = lane > B ? 0 : max(end - begin, 0);
+  const int m = b < B ? max(min(raw3, total2) - other, 0) : 0;
+  const int tiles = n / TILE + (n % TILE != 0), most = m / TILE + (m % TILE != 0);
+  const int from = !causal ? tiles + most : KEYS ? tiles : most;
+  const auto reach = [&](int c) {  // this sequence's tiles of work c and more
+    return c <= 0 ? tiles : c > most ? 0 : min(max(from - c + 1, 0), tiles);
+  };
+  const auto all = [](int x) { return __builtin_amdgcn_readlane(prefix_sum(x), 63); };
+  int lo = 0, hi = __builtin_amdgcn_readlane(prefix_max(most), 63);
+  while (lo < hi) {
+    const int c = (lo + hi + 1) / 2;
+    if (all(reach(c)) > slot) lo = c;
+    else hi = c - 1;
+  }
+  const int above = reach(lo + 1), here = reach(lo) - above;
+  const int i = slot - all(above), before = prefix_sum(here) - here;
+  const uint64_t who = __ballot(i >= before && i < before + here);
+  if (who == 0) return p;  // behind the last tile
+  const int l = __builtin_ctzll(who);
+  const int rank = __builtin_amdgcn_readlane(above - before, l) + i;
+  p.begin = __builtin_amdgcn_readlane(begin, l);
+  p.n = __builtin_amdgcn_readlane(n, l);
+  p.tile = KEYS ? rank : __builtin_amdgcn_readlane(tiles, l) - 1 - rank;
+  p.other = __builtin_amdgcn_readlane(other, l);
+  p.m = __builtin_amdgcn_readlane(m, l);
+  return p;
+}
+
 // The bias by distance of one head, in base-2 units: -inf where it hides, 0 where it has no
 // bucket.
 __device__ inline float bias_of(const float* table, const int32_t* map, int heads, int buckets,

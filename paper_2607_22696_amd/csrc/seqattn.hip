@@ -90,12 +90,11 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
   extern __shared__ float tab[];                           // the bias by distance
 
   Work w;
-  if (!work_of(g.q_tiles, g.group, w)) return;
-  const Slot sq = find_slot<QT>(cu_q, g.B, g.nq, 1, w.slot);
-  const int q0 = sq.tile * QT, n = sq.end - sq.begin;
+  if (!work_of<false>(g.q_tiles, g.group, w)) return;
+  const Place sq = place_of<QT, false>(cu_q, g.nq, cu_k, g.nk, g.B, g.causal, g.q_tiles.slots,
+                                       w.slot);
+  const int q0 = sq.tile * QT, n = sq.n, k0 = sq.other, m = sq.m;
   if (q0 >= n) return;
-  int k0, m;
-  key_rows(cu_k, sq.b, g.B, g.nk, k0, m);
   const int off = m - n;  // position of query 0
   const int nkeys = g.causal ? min(m, min(q0 + QT, n) + off) : m;
   const int ntiles = nkeys > 0 ? (nkeys + KT - 1) / KT : 0;
@@ -324,17 +323,16 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   extern __shared__ __attribute__((aligned(16))) float room[];
 
   Work w;
-  if (!work_of(g.q_tiles, g.group, w)) return;
-  const Slot sq = find_slot<kSeqTile>(cu_q, g.B, g.nq, 1, w.slot);
-  const int q0 = sq.tile * kSeqTile, n = sq.end - sq.begin;
+  if (!work_of<false>(g.q_tiles, g.group, w)) return;
+  const Place sq = place_of<kSeqTile, false>(cu_q, g.nq, cu_k, g.nk, g.B, g.causal,
+                                             g.q_tiles.slots, w.slot);
+  const int q0 = sq.tile * kSeqTile, n = sq.n, k0 = sq.other, m = sq.m;
   if (q0 >= n) {
     if (BIAS && partial != nullptr)
       for (int c = threadIdx.x; c < g.nb; c += kThreads)
         partial[((int64_t)w.slot * g.H + w.head) * g.nb + c] = 0.0f;
     return;
   }
-  int k0, m;
-  key_rows(cu_k, sq.b, g.B, g.nk, k0, m);
   const int off = m - n;
   const int nkeys = g.causal ? min(m, min(q0 + kSeqTile, n) + off) : m;
   const int ntiles = nkeys > 0 ? (nkeys + KT - 1) / KT : 0;
@@ -647,11 +645,10 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   Work w;
   if (!work_of<false>(g.k_tiles, PARTS ? g.parts : 1, w)) return;
   const int part = PARTS ? w.head - w.u * g.parts : 0;
-  const Slot sk = find_slot<kSeqTile>(cu_k, g.B, g.nk, 1, w.slot);
-  const int k0 = sk.tile * kSeqTile, m = sk.end - sk.begin;
+  const Place sk = place_of<kSeqTile, true>(cu_k, g.nk, cu_q, g.nq, g.B, g.causal, g.k_tiles.slots,
+                                            w.slot);
+  const int k0 = sk.tile * kSeqTile, m = sk.n, qbeg = sk.other, n = sk.m;
   if (k0 >= m) return;
-  int qbeg, n;
-  key_rows(cu_q, sk.b, g.B, g.nq, qbeg, n);
   const int off = m - n;
   // first tile with a query that sees
   const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;
@@ -877,11 +874,10 @@ void seq_dkdv_pair_kernel(
   Work w;
   if (!work_of<false>(g.k_tiles, PARTS ? g.parts : 1, w)) return;
   const int part = PARTS ? w.head - w.u * g.parts : 0;
-  const Slot sk = find_slot<kSeqTile>(cu_k, g.B, g.nk, 1, w.slot);
-  const int k0 = sk.tile * kSeqTile, m = sk.end - sk.begin;
+  const Place sk = place_of<kSeqTile, true>(cu_k, g.nk, cu_q, g.nq, g.B, g.causal, g.k_tiles.slots,
+                                            w.slot);
+  const int k0 = sk.tile * kSeqTile, m = sk.n, qbeg = sk.other, n = sk.m;
   if (k0 >= m) return;
-  int qbeg, n;
-  key_rows(cu_q, sk.b, g.B, g.nq, qbeg, n);
   const int off = m - n;
   // first tile with a query that sees
   const int q_first = g.causal ? max(k0 - off, 0) / QT * QT : 0;

@@ -342,3 +342,15 @@ def test_two_graphs_with_one_workspace():
         graphs[i][0].replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held[i], want[i]))
+
+
+@pytest.mark.parametrize("causal", (False, True))
+@pytest.mark.parametrize("count", (1, 2, 62, 63, 64, 65))
+def test_numbers_of_sequences(count, causal):
+    """Around the number of sequences that a wave holds, with lengths that rise, fall and repeat,
+    empty ones among them, other keys than queries and rows behind the last sequence."""
+    lengths = [(37 * i) % 301 if i % 5 else (0, 128, 300)[i // 5 % 3] for i in range(count)]
+    keys = [(53 * i + 40) % 280 if i % 7 else 0 for i in range(count)]
+    c = Case(170 + count, lengths, keys=keys, H=2, KH=1, causal=causal, tail=140,
+             bias=(8, 20, True))
+    c.check(residual=True)
