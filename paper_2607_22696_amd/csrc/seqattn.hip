@@ -662,8 +662,15 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
   uint32_t qo[Tl::NC], go[Tl::NC];
   Tl::copy_plan(qo, qsb);
   Tl::copy_plan(go, gsb);
-  auto fetch = [&](int it, int buf) {
-    const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
+  // Tiles are fetched in their order: the next one's head and number in it are counted on.
+  int next_head = w.u * g.group + (t0 < t1 ? t0 / per_head : 0);
+  int next_at = t0 < t1 ? t0 % per_head : 0;
+  auto fetch = [&](int buf) {
+    const int head = next_head, at = q_first + next_at * QT;
+    if (++next_at == per_head) {
+      next_at = 0;
+      ++next_head;
+    }
     const int64_t row = qbeg + at;
     Tl::copy(lds + Tl::kPlace * buf, q + row * g.qs + head * D, qo, qsb, n - at);
     Tl::copy(lds + Tl::kPlace * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
@@ -671,7 +678,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
       copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
              (uint32_t)min(lane, n - at - 1) * 4u, (int64_t)head * g.nq + row);
   };
-  if (t0 < t1) fetch(t0, 0);
+  int in_head = next_at, head = next_head;  // of tile `it`
+  if (t0 < t1) fetch(0);
 
   const int j0 = k0 + wave * 32, jk = j0 + (lane & 31);
   const bool kok = jk < m, live = j0 < m;
@@ -747,11 +755,11 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 
   int it = t0;
   while (it < t1) {
-    const int in_head = it % per_head, qbase = q_first + in_head * QT;
+    const int qbase = q_first + in_head * QT;
     if constexpr (BIAS) {
       if (it == t0 || in_head == 0) {
         __syncthreads();  // the previous head's table is no longer read
-        fill_bias(tab, g, table, map, w.u * g.group + it / per_head);
+        fill_bias(tab, g, table, map, head);
       }
     }
     __syncthreads();
@@ -766,14 +774,14 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
         f32x16_t sa, pa;
         auto tile = [&](int t, int buf) {
           const T *qc = lds + 2 * E * buf, *qn = lds + 2 * E * (1 - buf);
-          if (t + 1 < t1) fetch(t + 1, 1 - buf);
+          if (t + 1 < t1) fetch(1 - buf);
   #pragma unroll
           for (int b = 0; b < NB; ++b) {
             float s[16], ds[16];
   #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = sa[i];
             const f32x16_t p0 = pa;
-            const Affine f = biased(s, q_first + t % per_head * QT + b * 32);
+            const Affine f = biased(s, 0);  // without a bias no place counts
             if (b == NB - 1) {  // the next tile is in LDS
               wait_copies();
               __syncthreads();
@@ -787,6 +795,11 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
         };
         products(lds, 0, sa, pa);
         const int end = it + to_end;
+        in_head += to_end;
+        if (in_head == per_head) {
+          in_head = 0;
+          ++head;
+        }
         for (; it + 1 < end; it += 2) {
           tile(it, 0);
           tile(it + 1, 1);
@@ -797,7 +810,7 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     }
     const int buf = (it - t0) & 1;
     const uint16_t* qc = Tl::operands(lds, buf);
-    if (it + 1 < t1) fetch(it + 1, 1 - buf);
+    if (it + 1 < t1) fetch(1 - buf);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int qb = qbase + b * 32;
@@ -820,6 +833,10 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
     }
     wait_copies();
     ++it;
+    if (++in_head == per_head) {
+      in_head = 0;
+      ++head;
+    }
   }
   __syncthreads();
   if (!live) return;
@@ -891,8 +908,12 @@ void seq_dkdv_pair_kernel(
   uint32_t qo[Tl::NC], go[Tl::NC];
   Tl::copy_plan(qo, qsb);
   Tl::copy_plan(go, gsb);
-  auto fetch = [&](int it, int buf) {
-    const int head = w.u * g.group + it / per_head, at = q_first + it % per_head * QT;
+  // The tile fetched next, its head and its number in it; the number of the one before it, and of
+  // the one before that.
+  int head = w.u * g.group + (t0 < t1 ? t0 / per_head : 0);
+  int next_at = t0 < t1 ? t0 % per_head : 0, first_at = 0, second_at = 0;
+  auto fetch = [&](int buf) {
+    const int at = q_first + next_at * QT;
     const int64_t row = qbeg + at;
     Tl::copy(lds + 2 * E * buf, q + row * g.qs + head * D, qo, qsb, n - at);
     Tl::copy(lds + 2 * E * buf + E, dout + (row * g.H + head) * D, go, gsb, n - at);
@@ -900,7 +921,17 @@ void seq_dkdv_pair_kernel(
       copy_4(lds_offset(&stat[buf][wave][0]), wave == 0 ? lse2 : delta,
              (uint32_t)min(lane, n - at - 1) * 4u, (int64_t)head * g.nq + row);
   };
-  if (t0 < t1) fetch(t0, 0);
+  auto count_on = [&] {
+    second_at = first_at;
+    first_at = next_at;
+    if (++next_at == per_head) {
+      next_at = 0;
+      ++head;
+    }
+  };
+  if (t0 < t1) fetch(0);
+  const int head0 = head;
+  count_on();
 
   const int pair = wave & 3;
   const bool second = wave >= 4;
@@ -980,14 +1011,14 @@ void seq_dkdv_pair_kernel(
   auto run = [&](int step, int in, int out, int next) {
     __syncthreads();
     if constexpr (BIAS) {
-      if (step < steps && (step == 0 || (t0 + step) % per_head == 0)) {
-        fill_bias<512>(tab, g, table, map, w.u * g.group + (t0 + step) / per_head);
+      if (step < steps && (step == 0 || first_at == 0)) {
+        fill_bias<512>(tab, g, table, map, step == 0 ? head0 : next_at == 0 ? head - 1 : head);
         __syncthreads();
       }
     }
-    if (step + 1 < steps) fetch(t0 + step + 1, next);
-    auto tile = [&](int mine, int buf) {
-      const int qb = q_first + (t0 + mine) % per_head * QT;
+    if (step + 1 < steps) fetch(next);
+    auto tile = [&](int at, int buf) {
+      const int qb = q_first + at * QT;
       if (g.causal && qb + QT - 1 + off < j0) return;  // the same for both waves
       const T* rows = lds + 2 * E * buf + (second ? E : 0);
       f32x16_t x = products(rows, 0);
@@ -1001,11 +1032,12 @@ void seq_dkdv_pair_kernel(
     };
     if (live) {
       if (!second) {
-        if (step < steps) tile(step, in);
+        if (step < steps) tile(first_at, in);
       } else if (step > 0) {
-        tile(step - 1, out);
+        tile(second_at, out);
       }
     }
+    count_on();
     wait_copies();
   };
   for (int step = 0; step <= steps; step += 3) {
