@@ -321,3 +321,16 @@ def test_a_padded_batch():
     changed = (c.kp != before).flatten(2).any(-1).nonzero().tolist()
     assert sorted(changed) == sorted([[int(c.pages[0, 199 // 16]), 199 % 16],
                                       [int(c.pages[1, 32 // 16]), 32 % 16]])
+
+
+@pytest.mark.parametrize("new", ([1, 2], [100, 1]))
+def test_no_pages_and_no_columns(new):
+    c = Case(180, new, [50, 60])
+    args = (ints(c.held), ints(ref.starts(new)))
+    k = c.q[:, :2].contiguous()
+    for kp, vp, pages in ((c.kp[:0], c.vp[:0], ints(c.pages)),
+                          (c.kp, c.vp, ints(np.zeros((2, 0))))):
+        out, lse = dsa.paged_forward(c.q, kp, vp, pages, *args, need_lse=True)
+        before = kp.clone()
+        dsa.paged_append(k, k, kp, vp, pages, *args)
+        assert (out == 0).all() and torch.isneginf(lse).all() and torch.equal(kp, before)
