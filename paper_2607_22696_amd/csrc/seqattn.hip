@@ -301,7 +301,7 @@ void seq_fwd_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict_
 // bias gradient sums dS by distance: a block that reaches into the table is written to LDS with
 // its diagonals as rows, whose sums, one per lane, are added to the wave's sums by distance (with
 // LDS atomics, 140 cycles each, the pass took 153 us for 4,096 tokens of 16 heads x 64, 66 without
-// the gradient, and takes 78 this way); the other blocks go to a register per lane and side.  The
+// the gradient, and takes 76 this way); the other blocks go to a register per lane and side.  The
 // workgroup's sums by bucket go to `partial`.  Every order is fixed.
 template <typename T, int D, bool BIAS>
 __global__ __launch_bounds__(kThreads)
