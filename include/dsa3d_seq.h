@@ -99,10 +99,13 @@ size_t dsa3d_seq_backward_workspace_size(const dsa3d_seq_desc* desc);
  *   dq = scale sum_j dS k_j,   dk_j = scale sum dS q,   dv_j = sum alpha dout
  *   d_table[c][h] = sum of dS over the pairs whose distance has bucket c
  * The sums of dk and dv run over the queries of every head that reads the key's head.  O is out
- * + out_res, or out alone when out_res is NULL.  dq, dk, dv are in the descriptor's dtype, the
- * table's gradient is float32 and may be NULL (then it is not formed).  Every element is written
- * once and sums have a fixed order: repeated calls give the same bits.  The workspace (256-byte
- * aligned) must not overlap any argument.
+ * + out_res, or out alone when out_res is NULL.  lse, out and out_res may be those of more keys
+ * than the call has (a sequence's keys in several calls, their statistics joined): the gradients
+ * are then sums over the call's keys.  dq, dk, dv are in the descriptor's dtype, the table's
+ * gradient is float32 and may be NULL (then it is not formed); in it a query's sum of dS that is
+ * no larger than the rounding of its Delta (2^-16 of the root of <dout^2, O^2>, with out_res or in
+ * float32) counts as 0.  Every element is written once and sums have a fixed order: repeated calls
+ * give the same bits.  The workspace (256-byte aligned) must not overlap any argument.
  * Errors as for the forward, plus: lse, dout or a gradient NULL -> DSA3D_ERR_NULL_POINTER; a
  * workspace missing or too small -> DSA3D_ERR_WORKSPACE. */
 dsa3d_status dsa3d_seq_backward(const dsa3d_seq_desc* desc, const void* q, const void* k,

@@ -1,0 +1,88 @@
+"""What the bounds of tests/seq_util.py cannot see of the packed-sequence kernels: the table
+gradient in float32 accuracy, from the call's own statistics and from those of more keys than the
+call has."""
+import numpy as np
+import pytest
+import torch
+
+from tests import seq_table
+from tests.seq_util import TYPES, rounded
+
+import paper_2607_22696_amd as dsa
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    dsa.load()
+    yield
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x), dtype=torch.int32).cuda()
+
+
+def of_the_bound(name, got, want, limit):
+    worst = float((np.abs(got.double().cpu().numpy() - want) / limit).max())
+    print(f"  {name}: {worst:.3f} of the bound", flush=True)
+    assert worst <= 1.0, (name, worst)
+
+
+class Biased:
+    """One sequence whose values share an offset, so that Delta and its rounding are large beside
+    dS, and a bias of few distances, beyond which most pairs are."""
+
+    def __init__(self, seed, n, dtype, D, causal, H=4, KH=2):
+        r = np.random.default_rng(seed)
+        self.dtype, self.causal, self.n = dtype, causal, n
+        (self.q, self.q64), (self.k, self.k64), (self.g, self.g64) = (
+            rounded(r, (n, heads, D), dtype, std) for heads, std in ((H, 1.5), (KH, 1.0), (H, 1.0)))
+        v = r.standard_normal((n, KH, D)) + 6.0
+        self.v = torch.tensor(v).to(TYPES[dtype])
+        self.v64 = self.v.double().numpy()
+        self.bucket, self.rel_min = dsa.dsa3d_relative_buckets(6, 5, not causal)
+        self.table = r.standard_normal((6, H)).astype(np.float32)
+        self.bias = dict(rel_table=torch.tensor(self.table).cuda(), rel_buckets=ints(self.bucket))
+        self.table = self.table.astype(np.float64)
+        self.place = (self.table, self.bucket, self.rel_min)
+        self.q, self.k, self.v, self.g = (x.cuda() for x in (self.q, self.k, self.v, self.g))
+
+
+@pytest.mark.parametrize("causal", (False, True))
+@pytest.mark.parametrize("dtype,D", (("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)))
+def test_the_table_gradient_in_float32_accuracy(dtype, D, causal):
+    c = Biased(200 + D, 1100, dtype, D, causal)
+    how = dict(causal=causal, rel_min=c.rel_min, **c.bias)
+    out, lse, res = dsa.seq_forward(c.q, c.k, c.v, ints([0, c.n]), need_residual=True, **how)
+    got = dsa.seq_backward(c.q, c.k, c.v, out, res, lse, c.g, ints([0, c.n]), **how)[3]
+    o, l = seq_table.statistics(c.q64, c.k64, c.v64, *c.place, causal)
+    of_the_bound("d_rel_table", got, *seq_table.table_gradient(
+        c.q64, c.k64, c.v64, c.g64, o, l, *c.place, causal,
+        carried=2.0 ** (-18 if dtype == "bf16" else -23)))
+
+
+@pytest.mark.parametrize("residual", (True, False))
+@pytest.mark.parametrize("dtype,D", (("bf16", 64), ("bf16", 128), ("f32", 64), ("f32", 128)))
+def test_the_table_gradient_from_statistics_of_more_keys(dtype, D, residual):
+    """Keys in two calls with the joined out and lse, as ranks that share a sequence's keys have
+    them: dS = alpha (dP - Delta) of either call's keys, which do not add up to zero."""
+    c = Biased(210 + D, 700, dtype, D, False)
+    o, l = seq_table.statistics(c.q64, c.k64, c.v64, *c.place)
+    out = torch.tensor(o).to(TYPES[dtype])
+    res = (torch.tensor(o) - out.double()).bfloat16() if dtype == "bf16" and residual else None
+    given = out.double().numpy() + (0.0 if res is None else res.double().numpy())
+    lse = torch.tensor(l).float()
+    half = c.n // 2
+    for first, last in ((0, half), (half, c.n)):
+        # key j of the call is key first + j of all, whose distance is less by what lies behind
+        shift = last - c.n
+        got = dsa.seq_backward(c.q, c.k[first:last], c.v[first:last], out.cuda(),
+                               None if res is None else res.cuda(), lse.cuda(), c.g,
+                               ints([0, c.n]), ints([0, last - first]), rel_min=c.rel_min - shift,
+                               **c.bias)[3]
+        of_the_bound("d_rel_table", got, *seq_table.table_gradient(
+            c.q64, c.k64[first:last], c.v64[first:last], c.g64, given, lse.double().numpy(),
+            *c.place, shift=shift))
