@@ -410,25 +410,30 @@ __device__ inline void to_low_frags(const float (&x)[16], const bf16x8_t (&hi)[2
     for (int e = 0; e < 8; ++e) lo[p][e] = (__bf16)(x[8 * p + e] - (float)hi[p][e]);
 }
 
-// Sixteen values of a lane to LDS and back.
-__device__ inline void hand_over(_Float16* to, const float (&x)[16]) {
-  typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+// Sixteen values x >= 0 of a lane to LDS and back, 24 bits each: a float's upper half and the byte
+// below it (16 significant bits, rounded to nearest, and float32's range).  The wave's lanes are 16
+// bytes apart, its three pieces 64 lanes.
+__device__ inline void hand_over(uint4* to, const float (&x)[16]) {
+  uint32_t u[16], hi[8], lo[4];
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    f16x8_t h;
+  for (int i = 0; i < 16; ++i) u[i] = __float_as_uint(x[i]) + 0x80u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = (_Float16)x[8 * p + e];
-    *reinterpret_cast<f16x8_t*>(to + 8 * p) = h;
-  }
+  for (int i = 0; i < 8; ++i) hi[i] = __builtin_amdgcn_perm(u[2 * i + 1], u[2 * i], 0x07060302u);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    lo[i] = __builtin_amdgcn_perm(u[4 * i + 1], u[4 * i], 0x0c0c0501u) |
+            __builtin_amdgcn_perm(u[4 * i + 3], u[4 * i + 2], 0x05010c0cu);
+  to[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  to[64] = make_uint4(hi[4], hi[5], hi[6], hi[7]);
+  to[128] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
 }
-__device__ inline void take_over(const _Float16* from, float (&x)[16]) {
-  typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+__device__ inline void take_over(const uint4* from, float (&x)[16]) {
+  const uint4 a = from[0], b = from[64], c = from[128];
+  const uint32_t hi[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}, lo[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
-  for (int p = 0; p < 2; ++p) {
-    const f16x8_t h = *reinterpret_cast<const f16x8_t*>(from + 8 * p);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[8 * p + e] = (float)h[e];
-  }
+  for (int i = 0; i < 16; ++i)
+    x[i] = __uint_as_float(__builtin_amdgcn_perm(
+        hi[i / 2], lo[i / 4], (i % 2 ? 0x0706000cu : 0x0504000cu) | (uint32_t)(i % 4) << 8));
 }
 // Stores 16 values of channel block db (channels 32 db + 8 blk + 4 (l / 32) + j) times mul.
 __device__ inline void store_block(float* row, int db, const f32x16_t& acc, float mul) {

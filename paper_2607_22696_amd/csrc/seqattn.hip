@@ -875,13 +875,12 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 //   waves 0 - 3:  S = Q K^T,  alpha,  dv^T += dout^T alpha
 //   waves 4 - 7:  dP = dout V^T,  dS = alpha (dP - Delta),  dk^T += Q^T dS
 // so that each has one operand and one sum in registers (two waves per SIMD) and two of the four
-// products.  The second takes alpha from the first through LDS, one query tile later: float16 of
-// 2^14 alpha (11 bits down to 2^-28), which is what its lanes hold of the same block.  Measured
-// for 8,192 tokens, 16 heads x 128, all keys: both sums in one wave, one wave per SIMD, 1.44 ms
-// (matrix cores 30% busy); in one wave at two waves per SIMD, operands read as they are used,
-// 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this 1.18 ms (40% busy).
-constexpr float kAlphaScale = 14.0f;  // base 2
-
+// products.  The second takes alpha from the first through LDS, one query tile later, in 24 bits
+// (16 significant ones, next to the 8 that dS is rounded to), which is what its lanes hold of the
+// same block.  Measured for 8,192 tokens, 16 heads x 128, all keys: both sums in one wave, one wave
+// per SIMD, 1.44 ms (matrix cores 30% busy); in one wave at two waves per SIMD, operands read as
+// they are used, 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this 1.20 ms (40%
+// busy; 1.18 with alpha in float16, whose range loses weights below 2^-28).
 template <bool BIAS, bool PARTS>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void seq_dkdv_pair_kernel(
@@ -892,14 +891,13 @@ void seq_dkdv_pair_kernel(
     const float* __restrict__ lse2, const uint16_t* __restrict__ dout, uint16_t* __restrict__ dk,
     uint16_t* __restrict__ dv, float* __restrict__ part_dk, float* __restrict__ part_dv) {
   using T = uint16_t;
-  using Alpha = _Float16;
   constexpr int D = 128, QT = 64;
   using Tl = Tile<T, D, QT, 512>;
   using Frag = typename Type<T>::Frag;
   constexpr int KS = D / 16, DB = D / 32, NB = QT / 32, E = Tl::kElems;
   // three tiles of queries and douts: the first waves', the second waves', the next
   __shared__ __attribute__((aligned(16))) T lds[6 * E];
-  __shared__ __attribute__((aligned(16))) Alpha alpha[3][NB][4][64][16];
+  __shared__ uint4 alpha[2][NB][4][3 * 64];  // by step
   __shared__ __attribute__((aligned(16))) float stat[3][2][64];  // lse log2(e), Delta of a tile
   extern __shared__ float tab[];
 
@@ -970,12 +968,12 @@ void seq_dkdv_pair_kernel(
     for (int ks = 0; ks < KS; ++ks) x = mfma(a[ks], wf[ks], x);
     return x;
   };
-  // Block b of tile `mine` in LDS buffer `buf`; qb: its first query.
-  auto block = [&](int buf, int b, int qb, const f32x16_t& x) {
+  // Block b of the tile in LDS buffer `buf`, its alpha in place `half`; qb: its first query.
+  auto block = [&](int buf, int half, int b, int qb, const f32x16_t& x) {
     const T* cols = lds + 2 * E * buf + (second ? 0 : E);
     float y[16];
     const float* st = &stat[buf][second ? 1 : 0][b * 32 + 4 * hh];
-    Alpha* al = alpha[buf][b][pair][lane];
+    uint4* al = &alpha[half][b][pair][lane];
     if (!second) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) y[i] = x[i];
@@ -989,7 +987,7 @@ void seq_dkdv_pair_kernel(
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           const int i = 4 * blk + j;
-          y[i] = __builtin_amdgcn_exp2f(fmaf(y[i], f.mul, f.add + kAlphaScale - lv[j]));
+          y[i] = __builtin_amdgcn_exp2f(fmaf(y[i], f.mul, f.add - lv[j]));
         }
       }
       if (qb + 31 >= n || (g.causal && qb + off < j0 + 31)) {
@@ -1032,6 +1030,7 @@ void seq_dkdv_pair_kernel(
       }
     }
     if (step + 1 < steps) fetch(next);
+    const int half = (step & 1) ^ (second ? 1 : 0);  // the second waves: the step before
     auto tile = [&](int at, int buf) {
       const int qb = q_first + at * QT;
       if (g.causal && qb + QT - 1 + off < j0) return;  // the same for both waves
@@ -1041,7 +1040,7 @@ void seq_dkdv_pair_kernel(
       for (int b = 0; b < NB; ++b) {
         f32x16_t y = f32x16_t{};
         if (b + 1 < NB) y = products(rows, b + 1);
-        block(buf, b, qb + b * 32, x);
+        block(buf, half, b, qb + b * 32, x);
         x = y;
       }
     };
@@ -1062,7 +1061,7 @@ void seq_dkdv_pair_kernel(
   }
   __syncthreads();
   if (!live) return;
-  const float mul = (second ? g.scale : 1.0f) * 0x1p-14f;
+  const float mul = second ? g.scale : 1.0f;
   if constexpr (PARTS) {
     if (!kok) return;
     float* to = (second ? part_dk : part_dv) + (((int64_t)part * g.nk + krow) * g.KH + w.u) * D;

@@ -1,12 +1,13 @@
 """What the bounds of tests/seq_util.py cannot see of the packed-sequence kernels: the table
 gradient in float32 accuracy, from the call's own statistics and from those of more keys than the
-call has."""
+call has; gradients of keys whose weights are small."""
 import numpy as np
 import pytest
 import torch
 
 from tests import seq_table
 from tests.seq_util import TYPES, rounded
+from tests.test_gpu_seq import Case
 
 import paper_2607_22696_amd as dsa
 
@@ -86,3 +87,16 @@ def test_the_table_gradient_from_statistics_of_more_keys(dtype, D, residual):
         of_the_bound("d_rel_table", got, *seq_table.table_gradient(
             c.q64, c.k64[first:last], c.v64[first:last], c.g64, given, lse.double().numpy(),
             *c.place, shift=shift))
+
+
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("dtype", ("bf16", "f32"))
+def test_keys_of_small_weights(dtype, D):
+    """Weights down to e^-60 of a row's largest: dk and dv of their keys are as exact, relative
+    to their own terms, as any."""
+    c = Case(220, [200, 33], H=4, KH=2, D=D, dtype=dtype, scale=1.0)
+    c.q[..., 0] = 1
+    c.k[:] = 0
+    c.k[..., 0] = -4.0 * (torch.arange(233) % 16)[:, None]
+    c.q64, c.k64 = (x.double().cpu().numpy() for x in (c.q, c.k))
+    c.check()
