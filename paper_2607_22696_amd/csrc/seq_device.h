@@ -7,14 +7,16 @@
 // contraction indices 8 (l / 32) .. +7 of a step of 16, multiplied by v_mfma_f32_32x32x16_bf16.
 // The result's lane l holds column l % 32, rows 8 (i / 4) + 4 (l / 32) + i % 4 in its element i.
 //
-// float32 operands are split into three bf16 parts, x = h + m + l exactly (8 significant bits
-// each, by truncation, so m < 2^-7 and l < 2^-14 of x), and six of the nine products are summed in
-// float32: the three left out are below 2^-20 of the product together, 2^-23 on average, next to
-// the 2^-24 of each of its roundings.  Six bf16 products take 192 cycles where the eight
-// v_mfma_f32_32x32x2_f32 of the same 16 indices take 512.  Tiles are split once per workgroup, into
-// three bf16 tiles.  4,096 causal tokens, 8 heads x 128, forward: 594 us with float32 products, 467
-// with operands split as they are read, 389 this way (1,035 at two waves per SIMD, with 102 spilled
-// registers).  An infinity has no such parts: it makes NaN of what it reaches.
+// float32 operands are split into three bf16 parts, x = h + m + l exactly (each the nearest bf16 of
+// what is left, so m <= 2^-8 and l <= 2^-17 of x's leading bit), and six of the nine products are
+// summed in float32: the three left out are at most 2^-24 of the product together, of either sign,
+// as much as one of its roundings.  (Parts cut off instead of rounded cost the same instructions
+// and leave out up to 2^-21, always towards zero.)  Six bf16 products take 192 cycles where the
+// eight v_mfma_f32_32x32x2_f32 of the same 16 indices take 512.  Tiles are split once per
+// workgroup, into three bf16 tiles.  4,096 causal tokens, 8 heads x 128, forward: 594 us with
+// float32 products, 467 with operands split as they are read, 389 this way (1,035 at two waves per
+// SIMD, with 102 spilled registers).  Infinities, and values that round to one as a bf16 (3.39e38
+// and more), have no such parts: they make NaN of what they reach.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -64,23 +66,24 @@ __device__ inline f32x16_t mfma(const Split& a, const Split& b, f32x16_t c) {
   c = mfma(a.h, b.m, c);
   return mfma(a.h, b.h, c);
 }
-// The parts' upper halves are packed two by two by a byte permute.
+// Two floats as bf16, and what that leaves of them.
+__device__ inline uint32_t take_part(float (&x)[2]) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+  const f32x2_t y = {x[0], x[1]};
+  const uint32_t u = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2_t));
+  x[0] -= __uint_as_float(u << 16);
+  x[1] -= __uint_as_float(u & 0xffff0000u);
+  return u;
+}
 __device__ inline Split split(const F32x8& a) {
   uint32_t h[4], m[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    uint32_t hu[2], mu[2], lu[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float x = a.x[2 * i + j];
-      hu[j] = __float_as_uint(x);
-      const float r = x - __uint_as_float(hu[j] & 0xffff0000u);
-      mu[j] = __float_as_uint(r);
-      lu[j] = __float_as_uint(r - __uint_as_float(mu[j] & 0xffff0000u));
-    }
-    h[i] = __builtin_amdgcn_perm(hu[1], hu[0], 0x07060302u);
-    m[i] = __builtin_amdgcn_perm(mu[1], mu[0], 0x07060302u);
-    l[i] = __builtin_amdgcn_perm(lu[1], lu[0], 0x07060302u);
+    float x[2] = {a.x[2 * i], a.x[2 * i + 1]};
+    h[i] = take_part(x);
+    m[i] = take_part(x);
+    l[i] = take_part(x);
   }
   return {__builtin_bit_cast(bf16x8_t, make_uint4(h[0], h[1], h[2], h[3])),
           __builtin_bit_cast(bf16x8_t, make_uint4(m[0], m[1], m[2], m[3])),

@@ -1,6 +1,6 @@
 """What the bounds of tests/seq_util.py cannot see of the packed-sequence kernels: the table
 gradient in float32 accuracy, from the call's own statistics and from those of more keys than the
-call has; gradients of keys whose weights are small."""
+call has; gradients of keys whose weights are small; the parts of float32 operands."""
 import numpy as np
 import pytest
 import torch
@@ -100,3 +100,19 @@ def test_keys_of_small_weights(dtype, D):
     c.k[..., 0] = -4.0 * (torch.arange(233) % 16)[:, None]
     c.q64, c.k64 = (x.double().cpu().numpy() for x in (c.q, c.k))
     c.check()
+
+
+@pytest.mark.parametrize("D", (64, 128))
+def test_the_parts_of_float32_operands(D):
+    """x x - z, z being x x rounded: what a product loses stands alone.  Each operand is three
+    bf16 parts to half a step, so that beside the products that are left out, at most 2^-24, the
+    sum of two products and a third addend near 1 can lose 2^-24 for each; parts that are cut off
+    would lose 2^-21 of these x."""
+    x = 1 + 2.0 ** -7 - np.arange(1, 17) * 2.0 ** -23
+    z = (x * x).astype(np.float32).astype(np.float64)
+    q, k = torch.zeros(2, 16, 1, D, dtype=torch.float32)
+    q[:, 0, 0], q[:, 0, 1] = torch.tensor(x), torch.tensor(-z)
+    k[:, 0, 0], k[:, 0, 1] = torch.tensor(x), 1.0
+    lse = dsa.seq_forward(q.cuda(), k.cuda(), k.cuda(), ints(range(17)), scale=1024.0)[1][:, 0]
+    want = 1024 * (x * x - z)
+    of_the_bound("lse", lse, want, 1024 * 4.25 * 2.0 ** -24 + np.abs(want) * 2.0 ** -21)
