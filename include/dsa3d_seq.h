@@ -59,7 +59,10 @@ extern "C" {
 #define DSA3D_SEQ_MAX_SPAN 2048
 #define DSA3D_SEQ_MAX_BUCKETS 256
 
-/* Index range: total_q * heads and total_k * kv_heads below 2^31, batch below 2^24. */
+/* Index range: total_q * heads and total_k * kv_heads below 2^31, batch below 2^24, and the
+ * workgroups of a launch, heads * (total_q / 128 + batch + 1) of queries and kv_heads *
+ * (total_k / 128 + batch + 1) of keys, at most 2^31 - 2^22 (up to 16 times as many of keys where
+ * kv_heads * total_k is below 2^17). */
 typedef struct {
   int32_t batch;                       /* sequences, at least 1                               */
   int32_t total_q, total_k;            /* rows of q and of k, v (0 is allowed)                */
@@ -91,8 +94,8 @@ dsa3d_status dsa3d_seq_forward(const dsa3d_seq_desc* desc, const void* q, const 
                                void* out_res, float* lse, hipStream_t stream);
 
 /* Workspace bytes dsa3d_seq_backward needs (0 for a descriptor it would reject): 8 per query
- * row and head, with a bias 4 rel_buckets per head and 128-query tile, and where there are few
- * keys float32 parts of dk and dv, up to 16 of them. */
+ * row and head, with a bias 4 rel_buckets per head and tile of 128 queries (total_q / 128 +
+ * batch + 1 tiles), and where there are few keys float32 parts of dk and dv, up to 16 of them. */
 size_t dsa3d_seq_backward_workspace_size(const dsa3d_seq_desc* desc);
 
 /* Backward for upstream gradient dout, alpha recomputed from lse:
@@ -139,13 +142,16 @@ dsa3d_status dsa3d_relative_buckets(int32_t buckets, int32_t max_distance, int32
  * token i stands at position m - n + i.  A page number outside [0, num_pages) holds no tokens: it
  * is neither read nor written, and its tokens are hidden from every query. */
 typedef struct {
-  int32_t batch, total_q;              /* requests and new tokens of all of them              */
+  int32_t batch, total_q;              /* requests and new tokens of all of them; workgroups as
+                                          above, kv_heads * (total_q * heads / kv_heads / 32 +
+                                          batch + 1) of queries (times the parts)             */
   int32_t heads, kv_heads, head_dim;   /* as dsa3d_seq_desc (heads is not used by the append) */
   int32_t num_pages, page_size;        /* num_pages * page_size below 2^31                    */
   int32_t max_pages;                   /* columns of the page table                           */
   int32_t max_kv;                      /* no request holds more tokens than this; 0 selects
                                           max_pages * page_size.  Tokens from max_kv on are not
-                                          attended to.                                        */
+                                          attended to.  The smaller of the two is at most 2^30
+                                          for dsa3d_paged_forward.                            */
   int32_t causal;
   int32_t rel_min, rel_span, rel_buckets;
   float scale;

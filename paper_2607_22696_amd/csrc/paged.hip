@@ -530,7 +530,7 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(int64_t rows, int 
                                                               T* __restrict__ out,
                                                               float* __restrict__ lse) {
   constexpr int LANES = D / 4, SIDES = 64 / LANES;  // lanes per part, parts at a time
-  const int64_t row = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  const int64_t row = (int64_t)block_number() * (kThreads / 64) + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63, side = lane / LANES, c = lane % LANES * 4;
   if (row >= rows) return;
   // lane s holds part s's log-sum-exp (at most 64 parts)
@@ -586,8 +586,9 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(
     PagedGeometry g, int chunks, const uint4* __restrict__ k, const uint4* __restrict__ v,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ kv_lens,
     const int32_t* __restrict__ pages, uint4* __restrict__ k_pages, uint4* __restrict__ v_pages) {
-  const int tok = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-  if (tok >= g.nq) return;
+  const int64_t at_row = (int64_t)block_number() * (kThreads / 64) + (threadIdx.x >> 6);
+  if (at_row >= g.nq) return;
+  const int tok = (int)at_row, lane = threadIdx.x & 63;
   const int b = search(g.B, tok, [&](int i) { return cu_at(cu_q, i, g.nq); });
   if (b >= g.B) return;
   const int begin = cu_at(cu_q, b, g.nq), n = max(cu_at(cu_q, b + 1, g.nq), begin) - begin;
@@ -605,14 +606,6 @@ __global__ __launch_bounds__(kThreads) void paged_append_kernel(
   }
 }
 
-template <typename... A>
-hipError_t launch(const void* fn, dim3 grid, size_t lds, hipStream_t s, A... args) {
-  void* a[] = {(void*)&args...};
-  return hipLaunchKernel(fn, grid, dim3(kThreads), a, lds, s);
-}
-
-size_t round_256(size_t x) { return (x + 255) & ~size_t(255); }
-
 template <typename T, int D>
 hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
                      const int32_t* pages, const int32_t* kv_lens, const int32_t* cu_q,
@@ -629,13 +622,13 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
                   : (const void*)&paged_keys_kernel<T, D, false>)
           : (bias ? (const void*)&paged_rows_kernel<T, D, true>
                   : (const void*)&paged_rows_kernel<T, D, false>);
-  hipError_t e = launch(fn, dim3((unsigned)seq_blocks(g.tiles, g.splits)),
-                        bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, k, v, pages, kv_lens,
-                        cu_q, table, map, out, lse, part_o, part_l);
+  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, g.splits), kThreads,
+                            bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, k, v, pages, kv_lens,
+                            cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1) {
     constexpr int per = kThreads / 64;
-    e = launch((const void*)&paged_join_kernel<T, D>, dim3((unsigned)((rows + per - 1) / per)), 0,
-               s, rows, g.splits, (const float*)part_o, (const float*)part_l, out, lse);
+    e = seq_launch((const void*)&paged_join_kernel<T, D>, (rows + per - 1) / per, kThreads, 0,
+                   s, rows, g.splits, (const float*)part_o, (const float*)part_l, out, lse);
   }
   return e;
 }
@@ -710,9 +703,10 @@ hipError_t launch_paged_append(const PagedGeometry& g0, bool bf16, const void* k
   g.ks /= per16;
   g.vs /= per16;
   constexpr int per = kThreads / 64;
-  return launch((const void*)&paged_append_kernel, dim3((unsigned)((g.nq + per - 1) / per)), 0, s,
-                g, g.KH * g.D / per16, (const uint4*)k, (const uint4*)v, cu_q, kv_lens, pages,
-                (uint4*)k_pages, (uint4*)v_pages);
+  const int64_t blocks = ((int64_t)g.nq + per - 1) / per;
+  return seq_launch((const void*)&paged_append_kernel, blocks, kThreads, 0, s, g,
+                    g.KH * g.D / per16, (const uint4*)k, (const uint4*)v, cu_q, kv_lens, pages,
+                    (uint4*)k_pages, (uint4*)v_pages);
 }
 
 }  // namespace dsa3d

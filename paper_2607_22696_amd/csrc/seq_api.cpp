@@ -103,8 +103,8 @@ dsa3d_status check_seq(const dsa3d_seq_desc* d, bool own_keys, dsa3d::SeqGeometr
   g->q_tiles = dsa3d::seq_spread(g->KH, g->nq / dsa3d::kSeqTile + g->B + 1);
   g->k_tiles = dsa3d::seq_spread(g->KH, g->nk / dsa3d::kSeqTile + g->B + 1);
   g->parts = dsa3d::seq_backward_parts(*g, d->dtype == DSA3D_BF16);
-  if (dsa3d::seq_blocks(g->q_tiles, g->group) >= kIndexLimit ||
-      dsa3d::seq_blocks(g->k_tiles, g->parts) >= kIndexLimit)
+  if (dsa3d::seq_blocks(g->q_tiles, g->group) > dsa3d::kMostBlocks ||
+      dsa3d::seq_blocks(g->k_tiles, g->parts) > dsa3d::kMostBlocks)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->k = strided_bytes(d->total_k, g->ks, krow, s->item);
@@ -307,7 +307,8 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
   dsa3d::paged_plan(*g);
-  if (dsa3d::seq_blocks(g->tiles, g->splits) >= kIndexLimit) return DSA3D_ERR_INVALID_SHAPE;
+  if (!append && dsa3d::seq_blocks(g->tiles, g->splits) > dsa3d::kMostBlocks)
+    return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->out = (uint64_t)d->total_q * qrow * s->item;
   s->pages = (uint64_t)d->batch * d->max_pages * 4;

@@ -638,6 +638,8 @@ __device__ inline float bias_of(const float* table, const int32_t* map, int head
   return x <= kHidden ? -INFINITY : x * kLog2e;
 }
 
+__device__ inline int block_number() { return (int)(blockIdx.x + blockIdx.y * kGridX); }
+
 // Block -> (key head, slot, head within the group).  Blocks go to XCD x % 8, so the blocks of a
 // key head stay on one XCD, whose L2 then serves its keys and values; with key heads that the 8
 // XCDs do not share evenly, each head's tiles are dealt out over `parts` of them, so that early
@@ -648,12 +650,13 @@ struct Work {
 };
 template <bool LATE_FIRST = true>
 __device__ inline bool work_of(const Spread& sp, int per, Work& w) {
-  const int x = blockIdx.x % 8;
-  int r = blockIdx.x / 8;
+  const int x = block_number() % 8;
+  int r = block_number() / 8;
   const int j = r % per;
   r /= per;
-  const int su = (r % sp.local) * 8 + x;
-  const int rank = LATE_FIRST ? sp.ranks - 1 - r / sp.local : r / sp.local;
+  const int su = (r % sp.local) * 8 + x, nth = r / sp.local;
+  if (nth >= sp.ranks) return false;  // behind the grid's last workgroup
+  const int rank = LATE_FIRST ? sp.ranks - 1 - nth : nth;
   w.u = su % sp.units;
   w.slot = rank * sp.parts + su / sp.units;
   w.head = w.u * per + j;

@@ -33,6 +33,23 @@ inline int64_t seq_blocks(const Spread& s, int per) {
   return 8ll * s.local * s.ranks * per;
 }
 
+// A launch has fewer than 2^32 threads in x, so more workgroups than kGridX lie in rows of that
+// many (a multiple of 8: block n stays on XCD n % 8), the last of which may be wider than needed:
+// workgroup blockIdx.x + blockIdx.y kGridX, which must not reach 2^31.
+constexpr int kGridX = 1 << 22;
+constexpr int64_t kMostBlocks = (1ll << 31) - kGridX;
+
+template <typename... A>
+hipError_t seq_launch(const void* fn, int64_t blocks, int threads, size_t lds, hipStream_t s,
+                      A... args) {
+  void* a[] = {(void*)&args...};
+  const int64_t rows = (blocks + kGridX - 1) / kGridX;
+  const dim3 grid((uint32_t)(rows > 1 ? kGridX : blocks), (uint32_t)rows);
+  return hipLaunchKernel(fn, grid, dim3(threads), a, lds, s);
+}
+
+inline size_t round_256(size_t x) { return (x + 255) & ~size_t(255); }
+
 struct SeqTensors {
   const void *q, *k, *v;
   const int32_t *cu_q, *cu_k;

@@ -1082,10 +1082,10 @@ __global__ __launch_bounds__(kThreads) void seq_join_kernel(int64_t count, int p
                                                             const float4* __restrict__ part_dv,
                                                             T* __restrict__ dk,
                                                             T* __restrict__ dv) {
-  const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  const int64_t i = (int64_t)(blockIdx.x / 2) * kThreads + threadIdx.x;
   if (i >= count) return;
-  const float4* from = blockIdx.y == 0 ? part_dk : part_dv;
-  T* to = (blockIdx.y == 0 ? dk : dv) + i * 4;
+  const float4* from = blockIdx.x % 2 == 0 ? part_dk : part_dv;
+  T* to = (blockIdx.x % 2 == 0 ? dk : dv) + i * 4;
   float4 sum = from[i];
   for (int p = 1; p < parts; ++p) {
     const float4 x = from[p * count + i];
@@ -1104,12 +1104,6 @@ __global__ __launch_bounds__(kThreads) void seq_join_kernel(int64_t count, int p
 
 // ---------------------------------------------------------------------------- launches
 
-template <typename... A>
-hipError_t launch(const void* fn, dim3 grid, int threads, size_t lds, hipStream_t s, A... args) {
-  void* a[] = {(void*)&args...};
-  return hipLaunchKernel(fn, grid, dim3(threads), a, lds, s);
-}
-
 template <typename T, int D, int W>
 hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, float* lse,
                      hipStream_t s) {
@@ -1126,9 +1120,9 @@ hipError_t forward_w(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
   }
   SeqGeometry h = g;
   h.q_tiles = seq_spread(g.KH, g.nq / (W * 32) + g.B + 1);
-  return launch(fn, dim3((unsigned)seq_blocks(h.q_tiles, g.group)), W * 64,
-                bias ? padded(g.span) * 4 : 0, s, h, (const T*)t.q, (const T*)t.k, (const T*)t.v,
-                t.cu_q, t.cu_k, t.table, t.map, out, res, lse);
+  return seq_launch(fn, seq_blocks(h.q_tiles, g.group), W * 64, bias ? padded(g.span) * 4 : 0, s, h,
+                    (const T*)t.q, (const T*)t.k, (const T*)t.v, t.cu_q, t.cu_k, t.table, t.map,
+                    out, res, lse);
 }
 
 template <typename T, int D>
@@ -1144,8 +1138,6 @@ hipError_t forward_d(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, 
   }
   return forward_w<T, D, 4>(g, t, out, res, lse, s);
 }
-
-size_t round_256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // The backward's workspace: Delta and lse log2(e) [heads][rows], the bias gradient's bucket sums,
 // and the parts of dk and dv.
@@ -1185,14 +1177,13 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
     const size_t lds = !bias     ? 0
                        : partial ? 4 * (5 * (size_t)padded(g.span) + 8 + 4 * kSkewed)
                                  : 4 * (size_t)padded(g.span);
-    e = launch(fn, dim3((unsigned)seq_blocks(g.q_tiles, g.group)), kThreads, lds, s, g, q, k, v,
-               t.cu_q, t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, lse2, partial);
+    e = seq_launch(fn, seq_blocks(g.q_tiles, g.group), kThreads, lds, s, g, q, k, v, t.cu_q,
+                   t.cu_k, t.table, t.map, out, res, lse, dout, dq, delta, lse2, partial);
   }
   if (e == hipSuccess && want_table)
-    e = launch((const void*)&seq_table_kernel, dim3(g.H), kThreads, 0, s,
-               g.nq > 0 ? g.q_tiles.slots : 0, g.H, g.nb, (const float*)partial, d_table);
+    e = seq_launch((const void*)&seq_table_kernel, g.H, kThreads, 0, s,
+                   g.nq > 0 ? g.q_tiles.slots : 0, g.H, g.nb, (const float*)partial, d_table);
   if (e == hipSuccess && g.nk > 0) {
-    const dim3 grid((unsigned)seq_blocks(g.k_tiles, g.parts));
     const bool parts = g.parts > 1;
     const void* fn;
     constexpr bool kPair = sizeof(T) == 2 && D == 128;
@@ -1206,15 +1197,15 @@ hipError_t backward_d(const SeqGeometry& g, const SeqTensors& t, const T* out, c
                          : (const void*)&seq_dkdv_kernel<T, D, false, true>)
                  : (bias ? (const void*)&seq_dkdv_kernel<T, D, true, false>
                          : (const void*)&seq_dkdv_kernel<T, D, false, false>);
-    e = launch(fn, grid, kPair ? 512 : kThreads, bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k,
-               v, t.cu_q, t.cu_k, t.table, t.map, (const float*)delta, (const float*)lse2, dout,
-               dk, dv, part_dk, part_dv);
+    e = seq_launch(fn, seq_blocks(g.k_tiles, g.parts), kPair ? 512 : kThreads,
+                   bias ? (size_t)padded(g.span) * 4 : 0, s, g, q, k, v, t.cu_q, t.cu_k, t.table,
+                   t.map, (const float*)delta, (const float*)lse2, dout, dk, dv, part_dk, part_dv);
   }
   if (e == hipSuccess && g.nk > 0 && g.parts > 1) {
     const int64_t count = (int64_t)g.nk * g.KH * D / 4;
-    e = launch((const void*)&seq_join_kernel<T>,
-               dim3((unsigned)((count + kThreads - 1) / kThreads), 2), kThreads, 0, s, count,
-               g.parts, (const float4*)part_dk, (const float4*)part_dv, dk, dv);
+    const int64_t blocks = (count + kThreads - 1) / kThreads;
+    e = seq_launch((const void*)&seq_join_kernel<T>, 2 * blocks, kThreads, 0, s, count, g.parts,
+                   (const float4*)part_dk, (const float4*)part_dv, dk, dv);
   }
   return e;
 }
