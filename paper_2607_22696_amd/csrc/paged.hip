@@ -10,8 +10,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
-
+#include "paged_rules.h"
 #include "seq_device.h"
 #include "seq_internal.h"
 
@@ -21,8 +20,6 @@ namespace {
 using namespace seq;
 
 constexpr int kThreads = 256;
-constexpr int kFewRows = 32, kManyRows = 128;
-constexpr int kFewKeys = 128;  // keys per tile of the form with few rows: 32 per wave
 constexpr int kRing = 4;       // row tables of tiles in flight
 
 __device__ inline int div_by(uint32_t x, uint32_t mul, uint32_t shift) {
@@ -635,38 +632,12 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
 
 }  // namespace
 
-// Rows per workgroup: 32 where the requests have no more on average.  Parts of the keys (`splits`
-// at most, of `part` keys at least; a tile whose keys fit one part has no join):
-//  - few rows: reading is all, so the key heads, requests and parts make up to 2,048 workgroups,
-//    which also evens out requests of different lengths, in parts of 1,024 keys, or of 512 where
-//    that leaves the card half empty.  64 requests of 200 to 8,000 tokens, 32 / 8 heads x 128:
-//    238 us in parts of 2,048 keys, 219 of 1,024, 215 of 512; one of 4,000: 63, 28, 19 us; four of
-//    30,000: 105, 110, 113 us.
-//  - many rows: a part's float32 results are written and read again, which weighs more than uneven
-//    ends: parts of 4,096 keys, or as many as fill the card (512 workgroups).  1,024 new of 16,384
-//    tokens: 340 us in parts of 2,048, 312 of 4,096; chunks of 512, 801, 300 and single tokens:
-//    265 and 236 us.
-void paged_plan(PagedGeometry& g) {
-  constexpr int kMost = 64;
-  const int64_t rows = (int64_t)g.nq * g.group;
-  g.tile = rows <= (int64_t)kFewRows * g.B ? kFewRows : kManyRows;
-  const int64_t tiles = std::max<int64_t>((rows + g.tile - 1) / g.tile, std::min(g.B, g.nq));
-  const int64_t units = std::max<int64_t>(1, tiles * g.KH);
-  int64_t splits;
-  if (g.tile == kFewRows) {
-    g.part = units * g.max_kv >= 512 * 1024 ? 1024 : 512;
-    splits = std::min<int64_t>(2048 / units, g.max_kv / g.part);
-  } else {
-    const int64_t fill = (512 + units - 1) / units;
-    splits = std::min<int64_t>(2048 / units, g.max_kv / 4096);
-    g.part = 4096;
-    if (splits < fill) {
-      g.part = (int)std::max<int64_t>(512, g.max_kv / fill);
-      splits = std::min<int64_t>(fill, g.max_kv / g.part);
-    }
-  }
-  g.splits = (int)std::max<int64_t>(1, std::min<int64_t>(splits, kMost));
-  g.tiles = seq_spread(g.KH, (int)(rows / g.tile) + g.B + 1);
+void set_plan(PagedGeometry& g) {
+  const PagedPlan p = paged_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
+  g.tile = p.tile;
+  g.splits = p.splits;
+  g.part = p.part;
+  g.tiles = seq_spread(g.KH, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
 }
 
 size_t paged_workspace(const PagedGeometry& g) {

@@ -306,7 +306,7 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     return DSA3D_ERR_UNSUPPORTED;
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
-  dsa3d::paged_plan(*g);
+  dsa3d::set_plan(*g);
   if (!append && dsa3d::seq_blocks(g->tiles, g->splits) > dsa3d::kMostBlocks)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);

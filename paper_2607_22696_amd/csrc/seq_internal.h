@@ -82,7 +82,7 @@ struct PagedGeometry {
   Spread tiles;
 };
 
-void paged_plan(PagedGeometry& g);
+void set_plan(PagedGeometry& g);  // tile, splits, part and tiles
 size_t paged_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,
                                 const void* k_pages, const void* v_pages, const int32_t* pages,
