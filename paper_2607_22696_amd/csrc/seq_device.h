@@ -93,7 +93,6 @@ __device__ inline Split split(const F32x8& a) {
 __device__ inline bf16x8_t as_bf16x8(const uint4& u) { return __builtin_bit_cast(bf16x8_t, u); }
 
 __device__ inline uint16_t to_bf16(float x) { return __builtin_bit_cast(uint16_t, (__bf16)x); }
-__device__ inline float from_bf16(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 
 // x combined with the value of lane l ^ 32 (v_permlane32_swap: no LDS traffic).
 __device__ inline float pair_max(float x) {
@@ -173,28 +172,6 @@ struct Tile {
   static __device__ inline int row_of_thread(int i) { return (int)threadIdx.x / KCH + i * kStep; }
   static __device__ inline int chan_of_thread() { return ((int)threadIdx.x % KCH) * CH; }
 
-  // This thread's first chunk of a tile whose row 0 is at src.
-  static __device__ inline const T* first_chunk(const T* src, int64_t stride) {
-    return src + row_of_thread(0) * stride + chan_of_thread();
-  }
-  // The thread's chunks of a tile, `first` being its first one's address; rows from `valid` on
-  // read as zero (their loads go to the last valid row).  valid >= 1, uniform.
-  static __device__ inline void load(uint4 (&r)[NL], const T* first, int64_t stride, int valid) {
-    if (valid >= ROWS) {
-#pragma unroll
-      for (int i = 0; i < NL; ++i)
-        r[i] = *reinterpret_cast<const uint4*>(first + i * (kStep * stride));
-    } else {
-      asm volatile("");  // a branch: full tiles do not pay for this
-#pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int row = row_of_thread(i);
-        r[i] = *reinterpret_cast<const uint4*>(
-            first + (int64_t)(min(row, valid - 1) - row_of_thread(0)) * stride);
-        if (row >= valid) r[i] = make_uint4(0, 0, 0, 0);
-      }
-    }
-  }
   // Tile rows through a table of tensor rows (negative: no such row, reads as zero).
   static __device__ inline void load(uint4 (&r)[NL], const T* src, int64_t stride,
                                      const int* tab) {
