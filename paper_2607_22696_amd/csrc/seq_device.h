@@ -122,14 +122,14 @@ __device__ inline void copy_16(uint32_t to, const void* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :
                : "s"(to), "v"(off), "s"(base)
-               : "memory", "m0");
+               : "memory");
 }
 // The same from an address per lane.
 __device__ inline void copy_16(uint32_t to, const void* from) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                :
                : "s"(to), "v"(from)
-               : "memory", "m0");
+               : "memory");
 }
 // The same with 4 bytes per lane, from base + first floats + off bytes.
 __device__ inline void copy_4(uint32_t to, const float* base, uint32_t off, int64_t first) {
@@ -137,7 +137,7 @@ __device__ inline void copy_4(uint32_t to, const float* base, uint32_t off, int6
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2"
                :
                : "s"(to), "v"(off), "s"(base)
-               : "memory", "m0");
+               : "memory");
 }
 __device__ inline void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
