@@ -27,10 +27,11 @@
  * softmax statistics and sums are float32.  With bf16, alpha and dS enter their second products
  * rounded to bf16 (half a unit in the last place each, as the output's own rounding), unless
  * out_res is asked for.  float32 products are made of bf16 parts to 2^-24 of a product, and an
- * infinity (or 3.39e38 and more) in a float32 tensor becomes NaN.  What is hidden has weight 0: a
- * NaN or an infinity among the keys or values of a sequence can make NaN of queries of that
- * sequence that do not see it, but never of another sequence's, and what lies behind a sequence's
- * end is never used.
+ * infinity (or 3.39e38 and more) in a float32 tensor becomes NaN.  What is hidden has weight 0,
+ * and 0 times what is not finite is NaN: a NaN or an infinity among the keys or values of a
+ * sequence, in the backward also among its queries or upstream gradients (those of a query that
+ * sees no key among them), can make NaN of rows of that sequence that it is hidden from, but never
+ * of another sequence's, and what lies behind a sequence's end is never used.
  *
  * Values in device memory cannot be checked on the host.  cu must not decrease; entries outside
  * [0, rows] are clamped to it, so that a wrong one gives wrong results but no access outside the

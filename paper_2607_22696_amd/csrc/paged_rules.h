@@ -15,8 +15,12 @@ struct PagedPlan {
   int splits, part;  // most parts of a tile's keys, and least keys of a part
 };
 
-// Rows per workgroup: 32 where the requests have no more on average.  Parts of the keys (`splits`
-// at most, of `part` keys at least, whole tiles; a tile whose keys fit one part has no join):
+// Rows per workgroup: 32 where the requests have no more on average, in which form single tokens
+// are read fastest, else 128, which multiply each copied key with four times the rows.  Tiles of
+// 32 / 128, us, 16 requests of 4,000 keys with n new tokens each: 32 / 8 heads x 128, n = 2 51/46,
+// 8 60/50, 12 74/55, 64 211/111; 16 / 16 x 64, n = 2 53/56, 16 59/62, 64 87/73; one with 300 beside
+// 15 of one 105/89, beside 63 261/314.  Parts of the keys (`splits` at most, of `part` keys at
+// least, whole tiles; a tile whose keys fit one part has no join):
 //  - few rows: reading is all, so the key heads, requests and parts make up to 2,048 workgroups,
 //    which also evens out requests of different lengths, in parts of 1,024 keys, or of 512 where
 //    that leaves the card half empty.  64 requests of 200 to 8,000 tokens, 32 / 8 heads x 128:

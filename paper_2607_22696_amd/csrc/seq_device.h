@@ -117,7 +117,8 @@ __device__ inline uint32_t lds_offset(const void* p) {
 }
 // 16 bytes per lane from base + off to LDS at `to` + 16 lane, without a register in between.  The
 // compiler does not count it among the loads it waits for: the reader waits with wait_copies().
-// (Its builtin has the compiler wait for every copy in flight before any LDS read.)
+// (Its builtin has the compiler wait for every copy in flight before any LDS read.  m0 is reserved:
+// the compiler keeps nothing in it, and nothing else in these kernels writes it.)
 __device__ inline void copy_16(uint32_t to, const void* base, uint32_t off) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
                :

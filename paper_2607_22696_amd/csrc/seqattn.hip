@@ -455,7 +455,7 @@ void seq_dq_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict__
   // every place has alpha's share; the outer places, where alpha is largest, take theirs back at
   // the end.  With statistics of more keys than these the sum is no rounding, exceeds `trust` and
   // stays.  One text of 4,000 tokens, 4 heads x 64, the outer buckets' error: bf16 8e-7 (2.5e-6
-  // without this), float32 1.1e-6 (1.3e-5).
+  // without this), float32 7e-7 (1.4e-5).
   auto count = [&](const float (&p)[16], const float (&ds)[16], int kb) {
     if (!want_table) return;
     const int d_lo = kb - (i0 + 31 + off);
@@ -1129,9 +1129,15 @@ template <typename T, int D>
 hipError_t forward_d(const SeqGeometry& g, const SeqTensors& t, T* out, T* res, float* lse,
                      hipStream_t s) {
   // Eight waves halve the copies per product but leave half the workgroups: they pay where the
-  // sequences are long and the workgroups many.  16 heads x 128, 4 / 8 waves: one causal sequence
-  // of 16,384 tokens 1.025 / 1.001 ms, of 8,192 (all keys) 515 / 491 us; 32 sequences of 512
-  // 77 / 81 us, four of 1,000 with 8 heads 27 / 31 us.
+  // sequences are long and the workgroups many.  16 heads, 4 / 8 waves, us:
+  //                            64 channels                      128 channels
+  //   tokens              plain    bias   residual        plain    bias   residual
+  //   one of 8,192      330/313  350/335  237/233 causal  513/495  529/516  377/363 causal
+  //   two of 4,096      169/162  180/173  124/122 causal  261/253  270/262  196/188 causal
+  //   four of 2,048      90/87    96/93    69/70  causal  138/138  141/142  111/110 causal
+  //   32 of 512          55/60    61/64    52/63  causal   84/96    89/100   78/94  causal
+  //   one of 4,096 x 8   59/75    71/84    75/102 causal   81/106   89/116  101/140 causal
+  // One causal sequence of 16,384 at 64 channels is slower by 1% (residual 4%) with eight.
   const bool wide = g.nk >= 4096 * (int64_t)g.B && (int64_t)g.nq * g.H >= 256 * 512;
   if constexpr (sizeof(T) == 2) {
     if (wide) return forward_w<T, D, 8>(g, t, out, res, lse, s);
