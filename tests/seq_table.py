@@ -65,3 +65,35 @@ def table_gradient(q, k, v, dout, out, lse, table, bucket, rel_min, causal=False
 def statistics(q, k, v, table, bucket, rel_min, causal=False):
     """out and lse of one sequence in float64."""
     return ref.forward(q, k, v, [len(q)], [len(k)], causal, None, table, bucket, rel_min)[:2]
+
+
+def spreads(q, k, v, dout, causal=False):
+    """out, dq, dk, dv of one sequence in float64 and the standard deviations that float32
+    roundings give their elements: each pair's weight by e_row and e_pair, its dS by |dP| +
+    |Delta| times these."""
+    n, m, H, D = len(q), len(k), q.shape[1], q.shape[2]
+    out, lse, _ = ref.forward(q, k, v, [n], [m], causal)
+    grads = ref.backward(q, k, v, dout, [n], [m], causal)[0][:3]
+    values = (out, *grads)
+    var = [np.zeros(x.shape) for x in values]
+    for h in range(H):
+        u = h // (H // k.shape[1])
+        t = q[:, h] @ k[:, u].T / np.sqrt(D)
+        alpha = np.exp(t - lse[:, h, None])
+        if causal:
+            alpha = np.where(np.arange(m)[None, :] > np.arange(n)[:, None] + (m - n), 0.0, alpha)
+        e2 = ((3 * np.abs(lse[:, h, None]) + 4) * 2.0 ** -25) ** 2 + \
+            ((np.abs(t - lse[:, h, None]) + 2 * (np.abs(t) + 1) * np.sqrt(D / 16) + 4)
+             * 2.0 ** -25) ** 2
+        size = alpha * (np.abs(dout[:, h] @ v[:, u].T) +
+                        np.abs((dout[:, h] * out[:, h]).sum(1, keepdims=True)))
+        a2, s2 = alpha ** 2 * e2, size ** 2 * e2 / D
+        var[0][:, h] += a2 @ v[:, u] ** 2
+        var[1][:, h] += s2 @ k[:, u] ** 2
+        var[2][:, u] += s2.T @ q[:, h] ** 2
+        var[3][:, u] += a2.T @ dout[:, h] ** 2
+    return values, [np.sqrt(x) for x in var]
+
+
+def rms(x):
+    return float(np.sqrt((x ** 2).mean()))

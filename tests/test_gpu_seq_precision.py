@@ -1,6 +1,7 @@
 """What the bounds of tests/seq_util.py cannot see of the packed-sequence kernels: the table
 gradient in float32 accuracy, from the call's own statistics and from those of more keys than the
-call has; gradients of keys whose weights are small; the parts of float32 operands."""
+call has; gradients of keys whose weights are small; float32 results and the parts of their
+operands."""
 import numpy as np
 import pytest
 import torch
@@ -116,3 +117,28 @@ def test_the_parts_of_float32_operands(D):
     lse = dsa.seq_forward(q.cuda(), k.cuda(), k.cuda(), ints(range(17)), scale=1024.0)[1][:, 0]
     want = 1024 * (x * x - z)
     of_the_bound("lse", lse, want, 1024 * 4.25 * 2.0 ** -24 + np.abs(want) * 2.0 ** -21)
+
+
+@pytest.mark.parametrize("D", (64, 128))
+@pytest.mark.parametrize("causal", (False, True))
+def test_float32_results(D, causal):
+    """Root mean square errors against the spread that float32 roundings give (operands of two
+    parts would be at 2.8 to 5.5 of it, see test_seq_table_bound.py); paged results too."""
+    r = np.random.default_rng(230 + D)
+    (q, q64), (k, k64), (v, v64), (g, g64) = (rounded(r, (300, 2, D), "f32", s)
+                                              for s in (1.5, 1.0, 1.0, 1.0))
+    q, k, v, g = (x.cuda() for x in (q, k, v, g))
+    cu = ints([0, 300])
+    out, lse, _ = dsa.seq_forward(q, k, v, cu, causal=causal)
+    got = [out, *dsa.seq_backward(q, k, v, out, None, lse, g, cu, causal=causal)]
+    want, spread = seq_table.spreads(q64, k64, v64, g64, causal)
+    paged = [x.new_zeros(10, 32, 2, D) for x in (k, v)]
+    table = ints(np.random.default_rng(1).permutation(10)[None])
+    dsa.paged_append(k, v, *paged, table, ints([300]), cu)
+    got.append(dsa.paged_forward(q, *paged, table, ints([300]), cu, causal=causal)[0])
+    got.append(torch.cat([dsa.paged_forward(q[i:i + 1], *paged, table, ints([i + 1 if causal else
+                          300]), ints([0, 1]), causal=causal)[0] for i in range(300)]))
+    for name, a, i in zip(("out", "dq", "dk", "dv", "chunk", "tokens"), got, (0, 1, 2, 3, 0, 0)):
+        ratio = seq_table.rms(a.double().cpu().numpy() - want[i]) / seq_table.rms(spread[i])
+        print(f"  {name}: {ratio:.3f} of the spread", flush=True)
+        assert ratio <= 2.0, (name, ratio)

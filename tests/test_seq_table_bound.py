@@ -68,3 +68,23 @@ def test_the_meant_roundings_pass(case):
                                  dict(compensated=False)))
 def test_losses_of_precision_do_not(case, how):
     assert worst(case, **how) > 1.0
+
+
+@pytest.mark.parametrize("causal", (False, True))
+def test_operands_without_their_last_part(causal):
+    """The spread of float32 gradients against operands of 16 bits (two bf16 parts): each result's
+    root mean square error exceeds twice the root mean square of the spread, which what float32
+    rounds the operands to does not."""
+    r = np.random.default_rng(6)
+    q, k, v, g = (r.standard_normal((300, 2, D)).astype(np.float32).astype(np.float64) * s
+                  for s in (1.5, 1, 1, 1))
+    want, spread = seq_table.spreads(q, k, v, g, causal)
+
+    def short(x):
+        return bf16(x) + bf16(x - bf16(x))
+
+    for f, fits in ((short, False),
+                    (lambda x: (x * (1 + 2.0 ** -24 * r.uniform(-1, 1, x.shape))), True)):
+        got, _ = seq_table.spreads(*(f(x) for x in (q, k, v, g)), causal)
+        for a, b, s in zip(got, want, spread):
+            assert (seq_table.rms(a - b) <= 2 * seq_table.rms(s)) == fits
