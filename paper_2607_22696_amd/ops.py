@@ -490,7 +490,7 @@ def seq_forward(q, k, v, cu_q, cu_k=None, causal=False, scale=0.0, rel_table=Non
     `rel_table` (float32 [buckets, heads]) adds rel_table[rel_buckets[distance - rel_min]] to the
     logits, distances clamped to the ends of rel_buckets (see relative_buckets).
     Returns (out, lse, out_res).  out_res, the bf16 rounding residual of out, is what a bias
-    gradient in float32 accuracy needs; it is None unless need_residual is set, and for float32
+    gradient to some 2^-17 needs; it is None unless need_residual is set, and for float32
     tensors, which have none (as lse is None when need_lse is False)."""
     chk = _Checks("seq_forward")
     dev, desc = _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, rel_min)
@@ -521,7 +521,9 @@ def seq_backward(q, k, v, out, out_res, lse, dout, cu_q, cu_k=None, causal=False
                  workspace=None):
     """Returns (dq, dk, dv) in the type of q, and with rel_table also its gradient (float32; None
     where need_table is False).  `grads`: tensors to write into, in this order.  out_res may be
-    None (Delta from the rounded out alone)."""
+    None (Delta from the rounded out alone).  out, out_res and lse may be those of more keys than
+    the call has (the keys of a sequence in several calls, joined): the gradients are sums over the
+    call's keys."""
     chk = _Checks("seq_backward")
     dev, desc = _seq_desc(chk, q, k, v, cu_q, cu_k, causal, scale, rel_table, rel_buckets, rel_min)
     for name, t in (("out", out), ("dout", dout)):
