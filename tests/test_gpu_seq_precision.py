@@ -142,3 +142,19 @@ def test_float32_results(D, causal):
         ratio = seq_table.rms(a.double().cpu().numpy() - want[i]) / seq_table.rms(spread[i])
         print(f"  {name}: {ratio:.3f} of the spread", flush=True)
         assert ratio <= 2.0, (name, ratio)
+
+
+@pytest.mark.parametrize("bits", (0x7fffffff, -1, 0x7f800001))
+@pytest.mark.parametrize("D", (64, 128))
+def test_a_nan_among_the_statistics_stays(D, bits):
+    """lse of one query a NaN of any bits: its dq, and dk and dv of every key that it sees, are NaN
+    in its head and its key head alone."""
+    c = Case(280, [70], H=2, KH=2, D=D)
+    out, lse, _ = c.forward()
+    want = c.backward(out, None, lse)
+    lse.view(torch.int32)[9, 1] = bits
+    dq, dk, dv = c.backward(out, None, lse)
+    assert dq[9, 1].isnan().all() and dk[:, 1].isnan().all() and dv[:, 1].isnan().all()
+    dq[9, 1] = want[0][9, 1]
+    for a, b in zip((dq, dk[:, :1], dv[:, :1]), (want[0], want[1][:, :1], want[2][:, :1])):
+        assert torch.equal(a, b)
