@@ -391,9 +391,9 @@ __device__ inline void to_low_frags(const float (&x)[16], const bf16x8_t (&hi)[2
     for (int e = 0; e < 8; ++e) lo[p][e] = (__bf16)(x[8 * p + e] - (float)hi[p][e]);
 }
 
-// Sixteen values of a lane to LDS and back, 24 bits each: a float's upper three bytes (16 significant
-// bits, the rest cut off, and float32's range; a NaN stays one).  The wave's lanes are 16 bytes
-// apart, its three pieces 64 lanes.
+// Sixteen values of a lane to LDS and back, 24 bits each: a float's upper three bytes (16
+// significant bits, the rest cut off, and float32's range; a NaN stays one).  The wave's lanes are
+// 16 bytes apart, its three pieces 64 lanes.
 __device__ inline void hand_over(uint4* to, const float (&x)[16]) {
   uint32_t u[16], hi[8], lo[4];
 #pragma unroll

@@ -879,8 +879,8 @@ void seq_dkdv_kernel(SeqGeometry g, const T* __restrict__ q, const T* __restrict
 // (16 significant ones, cut off, next to the 8 that dS is rounded to), which is what its lanes hold
 // of the same block.  Measured for 8,192 tokens, 16 heads x 128, all keys: both sums in one wave,
 // one wave per SIMD, 1.44 ms (matrix cores 30% busy); in one wave at two waves per SIMD, operands
-// read as they are used, 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this 1.17 ms
-// (41% busy; no less with alpha in float16, whose range loses weights below 2^-28).
+// read as they are used, 1.5 ms; dv and dk as two launches with S formed twice 1.32 ms; this
+// 1.17 ms (41% busy; no less with alpha in float16, whose range loses weights below 2^-28).
 template <bool BIAS, bool PARTS>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void seq_dkdv_pair_kernel(
