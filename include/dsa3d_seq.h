@@ -81,7 +81,8 @@ typedef struct {
 /* out and, when not NULL, lse and out_res.  out_res (bf16 only, else it must be NULL) is the
  * rounding residual bf16(O - out), with alpha carried to 16 significant bits in its product:
  * out + out_res then has O to about 16 bits, which the backward needs for a bias gradient
- * that is off by no more than some 2^-17 of its size.  cu_k NULL: the keys' sequences are the queries' (total_k = total_q).
+ * that is off by no more than some 2^-17 of its size.  cu_k NULL: the keys' sequences are the
+ * queries' (total_k = total_q).
  * bias_table and bias_map may be NULL when rel_buckets is 0.
  * Errors: NULL desc, cu_q, or a tensor with rows -> DSA3D_ERR_NULL_POINTER; a size outside the
  * ranges above, heads not a multiple of kv_heads, total_k != total_q without cu_k, a negative or
