@@ -89,6 +89,9 @@ hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q
                                 const int32_t* kv_lens, const int32_t* cu_q, const float* table,
                                 const int32_t* map, void* out, float* lse, void* workspace,
                                 hipStream_t stream);
+// Joins the parts of each row that the workspace holds (log-sum-exps, then results).
+hipError_t launch_paged_join(const PagedGeometry& g, bool bf16, const float* part_o,
+                             const float* part_l, void* out, float* lse, hipStream_t stream);
 hipError_t launch_paged_append(const PagedGeometry& g, bool bf16, const void* k, const void* v,
                                const int32_t* cu_q, const int32_t* kv_lens, const int32_t* pages,
                                void* k_pages, void* v_pages, hipStream_t stream);
