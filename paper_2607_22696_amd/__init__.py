@@ -15,7 +15,10 @@ from ._binding import (  # noqa: F401
     make_desc, make_win_desc, status_string,
     dsa3d_paged_append, dsa3d_paged_desc, dsa3d_paged_forward, dsa3d_paged_forward_workspace_size,
     dsa3d_relative_buckets, dsa3d_seq_backward, dsa3d_seq_backward_workspace_size, dsa3d_seq_desc,
-    dsa3d_seq_forward, make_paged_desc, make_seq_desc)
+    dsa3d_seq_forward, make_paged_desc, make_seq_desc,
+    dsa3d_mx_cache, dsa3d_paged_append_mx, dsa3d_paged_forward_mx,
+    dsa3d_paged_forward_mx_workspace_size, dsa3d_paged_read_mx, make_mx_cache)
 from .ops import (backward, dwconv3d_backward, dwconv3d_forward, forward, paged_append,  # noqa: F401
-                  paged_forward, pw_backward, pw_forward, relative_buckets, seq_backward,
+                  paged_append_mx, paged_cache_mx, paged_forward, paged_forward_mx,
+                  paged_read_mx, pw_backward, pw_forward, relative_buckets, seq_backward,
                   seq_forward, win_backward, win_forward)

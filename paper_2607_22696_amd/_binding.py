@@ -40,7 +40,9 @@ EXPORTED = ("dsa3d_forward", "dsa3d_backward", "dsa3d_backward_timed", "dsa3d_ba
             "dsa3d_pw_backward", "dsa3d_win_forward", "dsa3d_win_backward_workspace_size",
             "dsa3d_win_backward", "dsa3d_seq_forward", "dsa3d_seq_backward_workspace_size",
             "dsa3d_seq_backward", "dsa3d_relative_buckets", "dsa3d_paged_append",
-            "dsa3d_paged_forward_workspace_size", "dsa3d_paged_forward")
+            "dsa3d_paged_forward_workspace_size", "dsa3d_paged_forward", "dsa3d_paged_append_mx",
+            "dsa3d_paged_read_mx", "dsa3d_paged_forward_mx_workspace_size",
+            "dsa3d_paged_forward_mx")
 
 DSA3D_WIN_MAX_TOKENS = 65536
 DSA3D_WIN_BACKWARD_PHASES = 2
@@ -92,6 +94,11 @@ class dsa3d_paged_desc(ctypes.Structure):
                 ("rel_buckets", ctypes.c_int32), ("scale", ctypes.c_float),
                 ("dtype", ctypes.c_int32), ("q_stride", ctypes.c_int64),
                 ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
+
+
+class dsa3d_mx_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scales", ctypes.c_void_p),
+                ("v_scales", ctypes.c_void_p), ("bits", ctypes.c_int32)]
 
 
 class Dsa3dError(RuntimeError):
@@ -160,6 +167,15 @@ def load():
         lib.dsa3d_paged_forward_workspace_size.restype = ctypes.c_size_t
         lib.dsa3d_paged_forward.argtypes = [gd] + [vp] * 11 + [ctypes.c_size_t, vp]
         lib.dsa3d_paged_forward.restype = ctypes.c_int
+        md = ctypes.POINTER(dsa3d_mx_cache)
+        lib.dsa3d_paged_append_mx.argtypes = [gd] + [vp] * 5 + [md, vp]
+        lib.dsa3d_paged_append_mx.restype = ctypes.c_int
+        lib.dsa3d_paged_read_mx.argtypes = [gd, md] + [vp] * 6
+        lib.dsa3d_paged_read_mx.restype = ctypes.c_int
+        lib.dsa3d_paged_forward_mx_workspace_size.argtypes = [gd, ctypes.c_int32]
+        lib.dsa3d_paged_forward_mx_workspace_size.restype = ctypes.c_size_t
+        lib.dsa3d_paged_forward_mx.argtypes = [gd, vp, md] + [vp] * 8 + [ctypes.c_size_t, vp]
+        lib.dsa3d_paged_forward_mx.restype = ctypes.c_int
         lib.dsa3d_backward_workspace_size.argtypes = [pd]
         lib.dsa3d_backward_workspace_size.restype = ctypes.c_size_t
         lib.dsa3d_status_string.argtypes = [ctypes.c_int]
@@ -431,6 +447,48 @@ def dsa3d_paged_forward(desc, q, k_pages, v_pages, pages, kv_lens, cu_q, bias_ta
                                     _stream(stream))
     if check and st != DSA3D_OK:
         raise Dsa3dError(st, "dsa3d_paged_forward")
+    return st
+
+
+def make_mx_cache(k, v, k_scales, v_scales, bits) -> dsa3d_mx_cache:
+    """The four arrays (tensors or addresses) as the library takes them."""
+    return dsa3d_mx_cache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), bits)
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def dsa3d_paged_append_mx(desc, k, v, cu_q, kv_lens, pages, cache, stream=None,
+                          check=True) -> int:
+    st = load().dsa3d_paged_append_mx(_ref(desc), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(kv_lens),
+                                      _ptr(pages), _ref(cache), _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_paged_append_mx")
+    return st
+
+
+def dsa3d_paged_read_mx(desc, cache, pages, kv_lens, cu_q, k, v, stream=None, check=True) -> int:
+    st = load().dsa3d_paged_read_mx(_ref(desc), _ref(cache), _ptr(pages), _ptr(kv_lens),
+                                    _ptr(cu_q), _ptr(k), _ptr(v), _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_paged_read_mx")
+    return st
+
+
+def dsa3d_paged_forward_mx_workspace_size(desc, bits) -> int:
+    return load().dsa3d_paged_forward_mx_workspace_size(ctypes.byref(desc), bits)
+
+
+def dsa3d_paged_forward_mx(desc, q, cache, pages, kv_lens, cu_q, bias_table, bias_map, out,
+                           lse=None, workspace=None, workspace_bytes=0, stream=None,
+                           check=True) -> int:
+    st = load().dsa3d_paged_forward_mx(_ref(desc), _ptr(q), _ref(cache), _ptr(pages),
+                                       _ptr(kv_lens), _ptr(cu_q), _ptr(bias_table),
+                                       _ptr(bias_map), _ptr(out), _ptr(lse), _ptr(workspace),
+                                       workspace_bytes, _stream(stream))
+    if check and st != DSA3D_OK:
+        raise Dsa3dError(st, "dsa3d_paged_forward_mx")
     return st
 
 

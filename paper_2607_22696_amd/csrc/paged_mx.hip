@@ -1,0 +1,709 @@
+// A paged cache held in 8 or 4 bits: the write of new tokens, their reading back, and the newest
+// tokens' attention over the pages (include/dsa3d_mx.h), gfx950 kernels.
+//
+// A token's key or value of one head is D / 32 blocks of 32 elements (e4m3 or e2m1 floats) and a
+// power of two each.  Elements are rounded and read by gfx950's scaled conversions.  Every value is
+// a bf16 number exactly, and the products are those of paged.hip on bf16 operands.  (The scaled 8-bit
+// products, v_mfma_scale_f32_32x32x64_f8f6f4, take the elements as they are, but not with a
+// float32 sum: 64 terms of up to 1,024 came out up to 0.07 off, 2^-14 of the largest.)
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "paged_device.h"
+
+namespace dsa3d {
+namespace {
+
+using namespace paged;
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// The cache as the kernels take it: addresses of the first page.
+struct MxPages {
+  uint8_t *k, *v, *ks, *vs;
+};
+
+__device__ inline float power_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Elements as bf16: 8 channels of 8 bits from two words, or of 4 bits from one, times a power.
+__device__ inline uint32_t two_of_8(uint32_t u, float power, bool upper) {
+  return __builtin_bit_cast(uint32_t,
+                            upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, power, true)
+                                  : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(u, power, false));
+}
+__device__ inline uint4 eight(uint32_t lo, uint32_t hi, float power) {
+  return make_uint4(two_of_8(lo, power, false), two_of_8(lo, power, true),
+                    two_of_8(hi, power, false), two_of_8(hi, power, true));
+}
+__device__ inline uint4 eight(uint32_t u, float power) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, power, 0),
+                 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, power, 1),
+                 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, power, 2),
+                 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(u, power, 3);
+  return make_uint4(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                    __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
+}
+
+// W words of elements of one key: CH = W 32 / BITS channels from a block's border on, or half a
+// block, with a byte of scales per block.
+template <int BITS, int W>
+struct Piece {
+  static constexpr int kEights = W * 4 / BITS;  // chunks of 8 channels
+  static constexpr int kBlocks = (kEights + 3) / 4;
+  uint32_t w[W];
+  uint32_t scales;
+
+  __device__ inline void load(const uint8_t* at, const uint8_t* scale_at) {
+    if constexpr (W >= 4) {
+#pragma unroll
+      for (int i = 0; i < W / 4; ++i)
+        *reinterpret_cast<uint4*>(w + 4 * i) = *reinterpret_cast<const uint4*>(at + 16 * i);
+    } else {
+      *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
+    }
+    if constexpr (kBlocks == 2)
+      scales = *reinterpret_cast<const uint16_t*>(scale_at);
+    else
+      scales = *scale_at;
+  }
+  __device__ inline void clear(bool none) {  // zeros where there is no such key
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = none ? 0u : w[i];
+    scales = none ? 0x7f7fu : scales;
+  }
+  __device__ inline float power(int chunk) const {
+    return power_of(scales >> (8 * (chunk / 4)) & 255u);
+  }
+  __device__ inline uint4 eight_at(int chunk) const {
+    if constexpr (BITS == 8)
+      return eight(w[2 * chunk], w[2 * chunk + 1], power(chunk));
+    else
+      return eight(w[chunk], power(chunk));
+  }
+};
+
+// The products of exact bf16 keys and values with queries and alpha, float32 ones in three parts.
+__device__ inline f32x16_t times(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) {
+  return mfma(a, b, c);
+}
+__device__ inline f32x16_t times(const bf16x8_t& a, const Split& b, f32x16_t c) {
+  c = mfma(a, b.l, c);
+  c = mfma(a, b.m, c);
+  return mfma(a, b.h, c);
+}
+
+// A row's results to the output or, where its keys are in several parts, to the workspace.
+template <typename T>
+__device__ inline void store_4(T* to, const float4& y) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(to) = y;
+  } else {
+    const uint16_t h[4] = {to_bf16(y.x), to_bf16(y.y), to_bf16(y.z), to_bf16(y.w)};
+    *reinterpret_cast<uint2*>(to) = __builtin_bit_cast(uint2, h);
+  }
+}
+
+// Keeps a wave's own LDS accesses in their order (the LDS serves a wave in order).
+__device__ inline void fence_wave() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// Place of key j of the span's request among the rows of all pages of one head: -1 if none.
+__device__ inline int64_t place_of_key(const PagedGeometry& g, const int32_t* pages, int b, int u,
+                                       int j) {
+  const int page = div_by((uint32_t)j, g.page_mul, g.page_shift);
+  const int p = pages[(int64_t)b * g.max_pages + page];
+  if (p < 0 || p >= g.num_pages) return -1;
+  return ((int64_t)p * g.KH + u) * g.page_size + (j - page * g.page_size);
+}
+
+// ------------------------------------------------------------------------- many rows
+
+// 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
+// elements are loaded while the one before it is multiplied, converted once for all four waves.
+template <typename T, int D, int BITS, bool BIAS>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
+                    const int32_t* __restrict__ pages, const int32_t* __restrict__ kv_lens,
+                    const int32_t* __restrict__ cu_q, const float* __restrict__ table,
+                    const int32_t* __restrict__ map, T* __restrict__ out,
+                    float* __restrict__ lse, float* __restrict__ part_o,
+                    float* __restrict__ part_l) {
+  constexpr int KT = 64, RB = D * BITS / 8, SB = D / 32;
+  using Tl = Tile<uint16_t, D, KT>;
+  using Frag = typename Type<T>::Frag;
+  using Quarter = Piece<BITS, RB / 16>;  // four threads share a key
+  constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
+  __shared__ __attribute__((aligned(16))) uint16_t lds[4 * E];  // keys, values; twice
+  __shared__ __attribute__((aligned(8))) uint16_t there[2][4];
+  extern __shared__ float bias[];
+
+  Work w;
+  if (!work_of(g.tiles, g.splits, w)) return;
+  const int split = w.head - w.u * g.splits;
+  Span1 s;
+  if (!locate<kManyRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
+  const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
+  const int key = threadIdx.x / 4, part = threadIdx.x % 4;
+  // the place of this thread's key of a tile; keys past the last repeat it, to be masked
+  auto place = [&](int kt) {
+    return place_of_key(g, pages, s.b, w.u, min(s.k_lo + kt * KT + key, s.k_hi - 1));
+  };
+  Quarter kq, vq;
+  auto load = [&](int64_t row) {
+    const int64_t r = max(row, (int64_t)0), at = r * RB + part * (RB / 4),
+                  sc = r * SB + part * SB / 4;
+    kq.load(c.k + at, c.ks + sc);
+    vq.load(c.v + at, c.vs + sc);
+  };
+  auto put = [&](int64_t row, int buf) {
+    if (__any(row < 0)) vq.clear(row < 0);
+    uint16_t* to = lds + 2 * E * buf;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      const int at = Tl::at(key, part * (D / 4) + 8 * i);
+      *reinterpret_cast<uint4*>(to + at) = kq.eight_at(i);
+      *reinterpret_cast<uint4*>(to + E + at) = vq.eight_at(i);
+    }
+    const uint64_t ok = __ballot(row >= 0);  // the same four times for each key
+    if ((threadIdx.x & 63) == 0) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) bits |= (uint32_t)(ok >> (4 * i) & 1) << i;
+      there[buf][wave_id()] = (uint16_t)bits;
+    }
+  };
+  int64_t row0 = 0, row1 = 0;
+  if (ntiles > 0) {
+    row0 = place(0);
+    load(row0);
+    if (ntiles > 1) row1 = place(1);
+  }
+  if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
+
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
+  const int rw = s.r0 + wave * 32;
+  const bool live = rw < s.rows;
+  const Row x = row_of(g, s, w.u, rw + (lane & 31));
+  Frag qf[KS];
+  load_frag<T, D>(qf, q + x.q_at, x.ok);
+  const int pos = s.off + x.i;
+  const int last = g.causal ? min(s.seen - 1, pos) : s.seen - 1;
+  int wave_last = live ? s.seen - 1 : -1, all_see = s.seen - 1;
+  if (live && g.causal) {
+    all_see = min(all_see, s.off + div_by(rw, g.group_mul, g.group_shift));
+    wave_last = min(wave_last, s.off + div_by(min(rw + 31, s.rows - 1), g.group_mul,
+                                              g.group_shift));
+  }
+
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
+  Softmax sm;
+  const float scale = BIAS ? 1.0f : g.scale_log2;
+  if (ntiles > 0) put(row0, 0);
+  if (ntiles > 1) load(row1);
+  __syncthreads();
+  for (int kt = 0; kt < ntiles; ++kt) {
+    const int buf = kt & 1;
+    const int64_t row2 = kt + 2 < ntiles ? place(kt + 2) : 0;
+    const uint16_t *kc = lds + 2 * E * buf, *vc = kc + E;
+    const int kbase = s.k_lo + kt * KT;
+    const uint2 m = *reinterpret_cast<const uint2*>(there[buf]);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const int kb = kbase + b * 32;
+      const uint32_t bits = __builtin_amdgcn_readfirstlane(b == 0 ? m.x : m.y);
+      if (bits == 0 || min(wave_last, s.k_hi - 1) < kb) continue;
+      f32x16_t acc = f32x16_t{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) acc = times(Tl::a_rows(kc, b * 32, ks), qf[ks], acc);
+      float y[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) y[i] = acc[i];
+      if constexpr (BIAS) add_bias(y, g, bias, x.head - w.u * g.group, kb, pos);
+      if (bits != ~0u || kb + 31 > min(all_see, s.k_hi - 1)) {
+        asm volatile("");  // a branch: blocks that every row sees do not pay for it
+        const int seen = min(last, s.k_hi - 1) - kb - 4 * hh;
+        const uint32_t mine = bits >> (4 * hh);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (c_row(i, 0) > seen || (mine >> c_row(i, 0) & 1) == 0) y[i] = -INFINITY;
+      }
+      sm.raise_to(y, scale, o);
+      sm.weigh(y, scale);
+      Frag pf[2];
+      to_frags(y, pf);
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          o[db] = times(Tl::a_cols(vc, db * 32, b, p), pf[p], o[db]);
+    }
+    if (kt + 1 < ntiles) {
+      put(row1, 1 - buf);
+      row1 = row2;
+      if (kt + 2 < ntiles) load(row1);
+    }
+    __syncthreads();
+  }
+  const float ltot = pair_sum(sm.l);
+  const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;
+  const float l2 = ltot == 0.0f ? -INFINITY : sm.base + __builtin_amdgcn_logf(ltot);
+  if (!x.ok) return;
+  if (s.only) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db) store_block(out + x.out_at * D, db, o[db], inv);
+    if (hh == 0 && lse != nullptr) lse[x.out_at] = l2 * kLn2;
+    if (hh == 0 && g.splits > 1) part_l[x.out_at * g.splits] = kDone;
+  } else {
+    const int64_t at = x.out_at * g.splits + split;
+    if (ltot != 0.0f) {  // the join skips the parts of a row without keys
+#pragma unroll
+      for (int db = 0; db < DB; ++db) store_block(part_o + at * D, db, o[db], inv);
+    }
+    if (hh == 0) part_l[at] = part_lse(l2);
+  }
+}
+
+// ------------------------------------------------------------------------- few rows
+
+// 32 rows per workgroup; its waves share out the keys in blocks of 32 and read them each for itself,
+// without a barrier until the end: lane l has half the channels of key l % 32, which is the keys'
+// operand (the contraction's order is free as long as the queries have it too).  Values pass
+// through 32 rows of LDS that are the wave's own, to be read transposed.
+template <typename T, int D, int BITS, bool BIAS>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
+                    const int32_t* __restrict__ pages, const int32_t* __restrict__ kv_lens,
+                    const int32_t* __restrict__ cu_q, const float* __restrict__ table,
+                    const int32_t* __restrict__ map, T* __restrict__ out,
+                    float* __restrict__ lse, float* __restrict__ part_o,
+                    float* __restrict__ part_l) {
+  constexpr int RB = D * BITS / 8, SB = D / 32, KB = 32, WAVES = kThreads / 64;
+  using Tl = Tile<uint16_t, D, KB, 64>;
+  using Frag = typename Type<T>::Frag;
+  using Half = Piece<BITS, RB / 8>;
+  constexpr int KS = D / 16, DB = D / 32, E = Tl::kElems;
+  // each wave's block of values; at the end the waves' results, half of the channels at a time
+  __shared__ __attribute__((aligned(16))) uint16_t lds[WAVES * E];
+  __shared__ float tops[WAVES][kFewRows], totals[WAVES][kFewRows];
+  extern __shared__ float bias[];
+
+  Work w;
+  if (!work_of(g.tiles, g.splits, w)) return;
+  const int split = w.head - w.u * g.splits;
+  Span1 s;
+  if (!locate<kFewRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
+  const int first = s.k_lo + wave * KB;  // this wave's blocks: first, first + 128, ...
+  const int nblocks = s.k_hi > first ? (s.k_hi - first + WAVES * KB - 1) / (WAVES * KB) : 0;
+  auto place = [&](int i) {
+    return place_of_key(g, pages, s.b, w.u,
+                        min(first + i * (WAVES * KB) + (lane & 31), s.k_hi - 1));
+  };
+  auto load = [&](Half& kh, Half& vh, int64_t row) {
+    const int64_t r = max(row, (int64_t)0), at = r * RB + hh * (RB / 2), sc = r * SB + hh * SB / 2;
+    kh.load(c.k + at, c.ks + sc);
+    vh.load(c.v + at, c.vs + sc);
+  };
+  Half k0, v0, k1, v1;
+  int64_t row0 = 0, row1 = 0;
+  if (nblocks > 0) row0 = place(0);
+  if (nblocks > 1) row1 = place(1);
+  if (nblocks > 0) load(k0, v0, row0);
+  if (nblocks > 1) load(k1, v1, row1);
+  if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
+
+  const Row x = row_of(g, s, w.u, s.r0 + (lane & 31));
+  Frag qf[KS];
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {  // channels hh D / 2 + 8 ks .. + 7
+    const T* from = q + x.q_at + hh * (D / 2) + 8 * ks;
+    if constexpr (sizeof(T) == 2) {
+      uint4 y = make_uint4(0, 0, 0, 0);
+      if (x.ok) y = *reinterpret_cast<const uint4*>(from);
+      qf[ks] = as_bf16x8(y);
+    } else {
+      F32x8 y = {};
+      if (x.ok) {
+        *reinterpret_cast<float4*>(y.x) = *reinterpret_cast<const float4*>(from);
+        *reinterpret_cast<float4*>(y.x + 4) = *reinterpret_cast<const float4*>(from + 4);
+      }
+      qf[ks] = seq::split(y);
+    }
+  }
+  const int pos = s.off + x.i;
+  const int last = min(g.causal ? min(s.seen - 1, pos) : s.seen - 1, s.k_hi - 1);
+  const int all_see =
+      min(g.causal ? min(s.seen - 1, s.off + div_by(s.r0, g.group_mul, g.group_shift))
+                   : s.seen - 1, s.k_hi - 1);
+  f32x16_t o[DB];
+#pragma unroll
+  for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
+  Softmax sm;
+  const float scale = BIAS ? 1.0f : g.scale_log2;
+  uint16_t* mine = lds + wave * E;
+  if constexpr (BIAS) __syncthreads();
+
+  // Block i, whose elements are in kh and vh: these are free for block i + 2 once they are converted.
+  auto block = [&](int i, Half& kh, Half& vh, int64_t& row) {
+    const int kb = first + i * (WAVES * KB);
+    const uint32_t bits = (uint32_t)__ballot(row >= 0);
+    if (bits != ~0u) vh.clear(row < 0);
+    f32x16_t acc = f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) acc = times(as_bf16x8(kh.eight_at(ks)), qf[ks], acc);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks)
+      *reinterpret_cast<uint4*>(mine + Tl::at(lane & 31, hh * (D / 2) + 8 * ks)) = vh.eight_at(ks);
+    if (i + 2 < nblocks) {
+      row = place(i + 2);
+      load(kh, vh, row);
+    }
+    float t[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t[e] = acc[e];
+    if constexpr (BIAS) add_bias(t, g, bias, x.head - w.u * g.group, kb, pos);
+    if (bits != ~0u || kb + 31 > all_see) {
+      asm volatile("");  // a branch: blocks that every row sees do not pay for it
+      const int seen = last - kb - 4 * hh;
+      const uint32_t have = bits >> (4 * hh);
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (c_row(e, 0) > seen || (have >> c_row(e, 0) & 1) == 0) t[e] = -INFINITY;
+    }
+    sm.raise_to(t, scale, o);
+    sm.weigh(t, scale);
+    Frag pf[2];
+    to_frags(t, pf);
+    fence_wave();
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int p = 0; p < 2; ++p) o[db] = times(Tl::a_cols(mine, db * 32, 0, p), pf[p], o[db]);
+    fence_wave();
+  };
+  for (int i = 0; i < nblocks; i += 2) {
+    block(i, k0, v0, row0);
+    if (i + 1 < nblocks) block(i + 1, k1, v1, row1);
+  }
+
+  // The waves' sums join over a common maximum, D / 2 channels at a time.
+  const float lw = pair_sum(sm.l);
+  if (hh == 0) {
+    tops[wave][lane] = sm.top;
+    totals[wave][lane] = lw;
+  }
+  __syncthreads();
+  const int col = lane & 31;
+  const auto most = [&](int r) {
+    return fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+  };
+  const float own = sm.top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm.top - most(col));
+  const int count = min(s.rows - s.r0, kFewRows);
+  constexpr int CH = D / 8;  // chunks of four channels in a half
+  float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {
+    if (half) __syncthreads();
+#pragma unroll
+    for (int d = 0; d < DB / 2; ++d)
+#pragma unroll
+      for (int blk = 0; blk < 4; ++blk) {
+        const int chunk = d * 8 + 2 * blk + hh;  // permuted against bank conflicts
+        const f32x16_t& y = o[half * (DB / 2) + d];
+        *reinterpret_cast<float4*>(sums + (wave * kFewRows + col) * (D / 2) +
+                                   ((chunk ^ (col & (CH - 1))) << 2)) =
+            make_float4(y[4 * blk] * own, y[4 * blk + 1] * own, y[4 * blk + 2] * own,
+                        y[4 * blk + 3] * own);
+      }
+    __syncthreads();
+    for (int e = threadIdx.x; e < count * CH; e += kThreads) {
+      const int r = e / CH, chunk = e % CH;
+      const float tr = most(r);
+      float total = 0.0f;
+      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int i = 0; i < WAVES; ++i) {
+        float f = totals[i][r];
+        if (tops[i][r] != -INFINITY) f *= __builtin_amdgcn_exp2f(tops[i][r] - tr);
+        total += f;
+        const float4 y = *reinterpret_cast<const float4*>(
+            sums + (i * kFewRows + r) * (D / 2) + ((chunk ^ (r & (CH - 1))) << 2));
+        sum.x += y.x;
+        sum.y += y.y;
+        sum.z += y.z;
+        sum.w += y.w;
+      }
+      const float inv = total > 0.0f ? 1.0f / total : total;
+      const float l2 = total == 0.0f
+                           ? -INFINITY
+                           : (tr == -INFINITY ? 0.0f : tr) + __builtin_amdgcn_logf(total);
+      const float4 y = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
+      const Row z = row_of(g, s, w.u, s.r0 + r);
+      const int at_chan = half * (D / 2) + chunk * 4;
+      const bool lead = half == 0 && chunk == 0;
+      if (s.only) {
+        store_4(out + z.out_at * D + at_chan, y);
+        if (lead && lse != nullptr) lse[z.out_at] = l2 * kLn2;
+        if (lead && g.splits > 1) part_l[z.out_at * g.splits] = kDone;
+      } else {
+        const int64_t at = z.out_at * g.splits + split;
+        if (total != 0.0f) store_4(part_o + at * D + at_chan, y);
+        if (lead) part_l[at] = part_lse(l2);
+      }
+    }
+  }
+}
+
+// ------------------------------------------------------------------------- write and read
+
+// Rows of k and v as chunks of 8 channels, k's first: a wave takes 64 chunks of one token, or, where
+// tokens have 32 or fewer, as many tokens as it has room for.
+struct Rows {
+  int per;     // chunks of a token's key and value together
+  int waves;   // waves per token
+  int tokens;  // tokens per wave
+};
+
+inline Rows rows_of(const PagedGeometry& g) {
+  const int per = 2 * g.KH * (g.D / 8);
+  return {per, (per + 63) / 64, per <= 32 ? 64 / per : 1};
+}
+
+// This lane's chunk: token, half (0: key, 1: value), head, first channel; and the token's place.
+struct Chunk {
+  int token, which, head, chan;
+  bool ok;        // there is such a chunk
+  int64_t place;  // row among all pages' rows of head 0's layout: page and row within it
+  int page, row;
+};
+
+__device__ inline Chunk chunk_of(const PagedGeometry& g, const Rows& r, const int32_t* cu_q,
+                                 const int32_t* kv_lens, const int32_t* pages) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t wid = (uint32_t)block_number() * (kThreads / 64) + wave_id();
+  const uint32_t group = wid / r.waves;
+  const int base = (int)min((uint64_t)group * r.tokens, (uint64_t)g.nq);
+  const int nth = r.tokens == 1 ? 0 : lane / r.per;
+  const int c = r.tokens == 1 ? (int)(wid - group * r.waves) * 64 + lane : lane - nth * r.per;
+  Chunk x;
+  x.token = base + nth;
+  x.ok = c < r.per && nth < r.tokens && nth < g.nq - base;
+  x.which = c >= r.per / 2;
+  const int chan = (c - x.which * (r.per / 2)) * 8;
+  x.head = chan / g.D;
+  x.chan = chan - x.head * g.D;
+  x.page = -1;
+  x.row = 0;
+  for (int i = 0; i < min(r.tokens, g.nq - base); ++i) {  // the same for all lanes
+    const int tok = base + i;
+    const int b = search(g.B, tok, [&](int k) { return cu_at(cu_q, k, g.nq); });
+    if (b >= g.B) continue;
+    const int begin = cu_at(cu_q, b, g.nq), n = max(cu_at(cu_q, b + 1, g.nq), begin) - begin;
+    const int64_t at = (int64_t)kv_lens[b] - n + (tok - begin);
+    if (tok < begin || tok - begin >= n || at < 0 || at >= (int64_t)g.max_pages * g.page_size)
+      continue;
+    const int page = div_by((uint32_t)at, g.page_mul, g.page_shift);
+    const int p = pages[(int64_t)b * g.max_pages + page];
+    if (p < 0 || p >= g.num_pages || i != nth) continue;
+    x.page = p;
+    x.row = (int)(at - (int64_t)page * g.page_size);
+  }
+  x.place = x.page < 0 ? -1 : ((int64_t)x.page * g.KH + x.head) * g.page_size + x.row;
+  return x;
+}
+
+template <typename T>
+__device__ inline void load_8(float (&x)[8], const T* at) {
+  if constexpr (sizeof(T) == 2) {
+    const uint4 u = *reinterpret_cast<const uint4*>(at);
+    const uint32_t h[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(h[i] << 16);
+      x[2 * i + 1] = __uint_as_float(h[i] & 0xffff0000u);
+    }
+  } else {
+    *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(at);
+    *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(at + 4);
+  }
+}
+
+// The largest magnitude's bits -> the block's scale byte.  With M 1.75 2^8 or 1.5 2^2, the least e
+// with a <= M 2^e is a's exponent less 8 or 2, and one more where its mantissa is larger than M's:
+// adding what M's mantissa leaves to a whole one carries then.  255 where the largest would round
+// to 2^128 (a NaN's and an infinity's bits are larger still).
+template <int BITS>
+__device__ inline uint32_t scale_byte(uint32_t a) {
+  constexpr uint32_t kUp = BITS == 8 ? 0x1fffffu : 0x3fffffu, kLess = BITS == 8 ? 8 : 2;
+  constexpr uint32_t kOver = BITS == 8 ? 0x7f780000u : 0x7f600000u;
+  const uint32_t e = (a + kUp) >> 23;
+  return a >= kOver ? 255u : max(e, 10u + kLess) - kLess;
+}
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(kThreads) void mx_append_kernel(
+    PagedGeometry g, Rows r, const T* __restrict__ k, const T* __restrict__ v,
+    const int32_t* __restrict__ cu_q, const int32_t* __restrict__ kv_lens,
+    const int32_t* __restrict__ pages, MxPages to) {
+  const Chunk c = chunk_of(g, r, cu_q, kv_lens, pages);
+  const bool ok = c.ok && c.place >= 0;
+  float x[8] = {};
+  if (ok)
+    load_8(x, (c.which ? v + c.token * g.vs : k + c.token * g.ks) + c.head * g.D + c.chan);
+  uint32_t a = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(x[i]) & 0x7fffffffu);
+  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, true));  // lane ^ 1
+  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true));  // lane ^ 2
+  const uint32_t byte = scale_byte<BITS>(a);
+  if (!ok) return;
+  const bool none = byte == 255u;
+  const float power = power_of(none ? 127u : byte);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = none ? 0.0f : x[i];
+  uint8_t* codes = c.which ? to.v : to.k;
+  uint8_t* scales = c.which ? to.vs : to.ks;
+  if constexpr (BITS == 8) {
+    typedef short s2_t __attribute__((ext_vector_type(2)));
+    uint32_t u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      s2_t y = {0, 0};
+      y = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(y, x[4 * i], x[4 * i + 1], power, false);
+      y = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(y, x[4 * i + 2], x[4 * i + 3], power, true);
+      u[i] = __builtin_bit_cast(uint32_t, y);
+    }
+    *reinterpret_cast<uint2*>(codes + c.place * g.D + c.chan) = make_uint2(u[0], u[1]);
+  } else {
+    uint32_t u = 0;
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[0], x[1], power, 0);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[2], x[3], power, 1);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[4], x[5], power, 2);
+    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[6], x[7], power, 3);
+    *reinterpret_cast<uint32_t*>(codes + (c.place * g.D + c.chan) / 2) = u;
+  }
+  if (c.chan % 32 == 0) scales[(c.place * g.D + c.chan) / 32] = (uint8_t)byte;
+}
+
+template <typename T, int BITS>
+__global__ __launch_bounds__(kThreads) void mx_read_kernel(
+    PagedGeometry g, Rows r, MxPages from, const int32_t* __restrict__ pages,
+    const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ cu_q, T* __restrict__ k,
+    T* __restrict__ v) {
+  const Chunk c = chunk_of(g, r, cu_q, kv_lens, pages);
+  if (!c.ok) return;
+  uint4 y = make_uint4(0, 0, 0, 0);
+  if (c.place >= 0) {
+    const uint8_t* codes = c.which ? from.v : from.k;
+    const int64_t at = c.place * g.D + c.chan;
+    const float power = power_of((c.which ? from.vs : from.ks)[at / 32]);
+    if constexpr (BITS == 8) {
+      const uint2 u = *reinterpret_cast<const uint2*>(codes + at);
+      y = eight(u.x, u.y, power);
+    } else {
+      y = eight(*reinterpret_cast<const uint32_t*>(codes + at / 2), power);
+    }
+  }
+  T* to = (c.which ? v + c.token * g.vs : k + c.token * g.ks) + c.head * g.D + c.chan;
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(to) = y;
+  } else {  // a bf16 number is a float32 number's upper half
+    *reinterpret_cast<uint4*>(to) =
+        make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
+    *reinterpret_cast<uint4*>(to + 4) =
+        make_uint4(y.z << 16, y.z & 0xffff0000u, y.w << 16, y.w & 0xffff0000u);
+  }
+}
+
+int64_t row_blocks(const PagedGeometry& g, const Rows& r) {
+  const int64_t waves = ((int64_t)g.nq + r.tokens - 1) / r.tokens * r.waves;
+  return (waves + kThreads / 64 - 1) / (kThreads / 64);
+}
+
+MxPages pages_of(const dsa3d_mx_cache& c) { return {c.k, c.v, c.k_scales, c.v_scales}; }
+
+template <typename T, int D, int BITS>
+hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const int32_t* pages,
+                     const int32_t* kv_lens, const int32_t* cu_q, const float* table,
+                     const int32_t* map, T* out, float* lse, void* ws, hipStream_t s) {
+  const bool bias = g.nb > 0;
+  const int64_t rows = (int64_t)g.nq * g.H;
+  float* part_l = g.splits > 1 ? (float*)ws : nullptr;
+  float* part_o = g.splits > 1 ? (float*)((char*)ws + round_256((size_t)g.splits * rows * 4))
+                               : nullptr;
+  const void* fn = g.tile == kFewRows
+                       ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true>
+                               : (const void*)&mx_keys_kernel<T, D, BITS, false>)
+                       : (bias ? (const void*)&mx_rows_kernel<T, D, BITS, true>
+                               : (const void*)&mx_rows_kernel<T, D, BITS, false>);
+  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, g.splits), kThreads,
+                            bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
+                            cu_q, table, map, out, lse, part_o, part_l);
+  if (e == hipSuccess && g.splits > 1)
+    e = launch_paged_join(g, sizeof(T) == 2, part_o, part_l, out, lse, s);
+  return e;
+}
+
+template <typename T>
+hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache& cache,
+                     const int32_t* pages, const int32_t* kv_lens, const int32_t* cu_q,
+                     const float* table, const int32_t* map, void* out, float* lse, void* ws,
+                     hipStream_t s) {
+  const MxPages c = pages_of(cache);
+  const T* x = (const T*)q;
+  T* y = (T*)out;
+  if (cache.bits == 8)
+    return g.D == 64
+               ? forward_d<T, 64, 8>(g, x, c, pages, kv_lens, cu_q, table, map, y, lse, ws, s)
+               : forward_d<T, 128, 8>(g, x, c, pages, kv_lens, cu_q, table, map, y, lse, ws, s);
+  return g.D == 64
+             ? forward_d<T, 64, 4>(g, x, c, pages, kv_lens, cu_q, table, map, y, lse, ws, s)
+             : forward_d<T, 128, 4>(g, x, c, pages, kv_lens, cu_q, table, map, y, lse, ws, s);
+}
+
+}  // namespace
+
+hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,
+                                   const dsa3d_mx_cache& cache, const int32_t* pages,
+                                   const int32_t* kv_lens, const int32_t* cu_q,
+                                   const float* table, const int32_t* map, void* out, float* lse,
+                                   void* ws, hipStream_t s) {
+  if (g.nq == 0) return hipSuccess;
+  return bf16 ? forward_t<uint16_t>(g, q, cache, pages, kv_lens, cu_q, table, map, out, lse, ws, s)
+              : forward_t<float>(g, q, cache, pages, kv_lens, cu_q, table, map, out, lse, ws, s);
+}
+
+hipError_t launch_paged_append_mx(const PagedGeometry& g, bool bf16, const void* k, const void* v,
+                                  const int32_t* cu_q, const int32_t* kv_lens,
+                                  const int32_t* pages, const dsa3d_mx_cache& cache,
+                                  hipStream_t s) {
+  if (g.nq == 0) return hipSuccess;
+  const Rows r = rows_of(g);
+  const MxPages c = pages_of(cache);
+  const void* fn = bf16 ? (cache.bits == 8 ? (const void*)&mx_append_kernel<uint16_t, 8>
+                                           : (const void*)&mx_append_kernel<uint16_t, 4>)
+                        : (cache.bits == 8 ? (const void*)&mx_append_kernel<float, 8>
+                                           : (const void*)&mx_append_kernel<float, 4>);
+  return seq_launch(fn, row_blocks(g, r), kThreads, 0, s, g, r, k, v, cu_q, kv_lens, pages, c);
+}
+
+hipError_t launch_paged_read_mx(const PagedGeometry& g, bool bf16, const dsa3d_mx_cache& cache,
+                                const int32_t* pages, const int32_t* kv_lens, const int32_t* cu_q,
+                                void* k, void* v, hipStream_t s) {
+  if (g.nq == 0) return hipSuccess;
+  const Rows r = rows_of(g);
+  const MxPages c = pages_of(cache);
+  const void* fn = bf16 ? (cache.bits == 8 ? (const void*)&mx_read_kernel<uint16_t, 8>
+                                           : (const void*)&mx_read_kernel<uint16_t, 4>)
+                        : (cache.bits == 8 ? (const void*)&mx_read_kernel<float, 8>
+                                           : (const void*)&mx_read_kernel<float, 4>);
+  return seq_launch(fn, row_blocks(g, r), kThreads, 0, s, g, r, c, pages, kv_lens, cu_q, k, v);
+}
+
+}  // namespace dsa3d

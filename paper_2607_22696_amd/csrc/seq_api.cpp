@@ -1,6 +1,8 @@
 // C-ABI entry points of the packed-sequence and paged attention: argument validation and dispatch.
-// The operations and the conventions are described in include/dsa3d_seq.h.
+// The operations and the conventions are described in include/dsa3d_seq.h and dsa3d_mx.h.
 #include "dsa3d_seq.h"
+
+#include "dsa3d_mx.h"
 
 #include <hip/hip_runtime.h>
 
@@ -394,6 +396,152 @@ dsa3d_status dsa3d_paged_forward(const dsa3d_paged_desc* desc, const void* q, co
   const hipError_t e = dsa3d::launch_paged_forward(
       g, desc->dtype == DSA3D_BF16, q, k_pages, v_pages, pages, kv_lens, cu_q, bias_table,
       bias_map, out, lse, workspace, stream);
+  return e == hipSuccess ? DSA3D_OK : DSA3D_ERR_DEVICE;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------- paged, 8 or 4 bits
+
+namespace {
+
+// The cache's sizes in bytes instead of those of bf16 or float32 pages.
+struct MxSizes {
+  uint64_t codes, scales;
+};
+
+dsa3d_status check_bits(int32_t bits) {
+  return bits == 8 || bits == 4 ? DSA3D_OK : DSA3D_ERR_UNSUPPORTED;
+}
+
+dsa3d_status check_cache(const dsa3d_paged_desc* d, const dsa3d_mx_cache* c, bool rows,
+                         dsa3d::PagedGeometry* g, PagedSizes* s, MxSizes* m) {
+  if (c == nullptr) return DSA3D_ERR_NULL_POINTER;
+  dsa3d_status st = check_paged(d, rows, g, s);
+  if (st == DSA3D_OK) st = check_bits(c->bits);
+  if (st != DSA3D_OK) return st;
+  const uint64_t held = (uint64_t)g->num_pages * g->page_size * g->KH;
+  m->codes = held * (g->D * c->bits / 8);
+  m->scales = held * (g->D / 32);
+  return DSA3D_OK;
+}
+
+bool cache_missing(const dsa3d_mx_cache& c, const MxSizes& m) {
+  return missing(c.k, m.codes) || missing(c.v, m.codes) || missing(c.k_scales, m.scales) ||
+         missing(c.v_scales, m.scales);
+}
+
+bool cache_aligned(const dsa3d_mx_cache& c) {
+  return aligned(c.k, 16) && aligned(c.v, 16) && aligned(c.k_scales, 16) &&
+         aligned(c.v_scales, 16);
+}
+
+}  // namespace
+
+extern "C" {
+
+dsa3d_status dsa3d_paged_append_mx(const dsa3d_paged_desc* desc, const void* k, const void* v,
+                                   const int32_t* cu_q, const int32_t* kv_lens,
+                                   const int32_t* pages, const dsa3d_mx_cache* cache,
+                                   hipStream_t stream) {
+  dsa3d::PagedGeometry g;
+  PagedSizes s;
+  MxSizes m;
+  const dsa3d_status st = check_cache(desc, cache, true, &g, &s, &m);
+  if (st != DSA3D_OK) return st;
+  const int64_t row = (int64_t)g.KH * g.D;
+  const uint64_t kb = strided_bytes(g.nq, g.ks, row, s.item),
+                 vb = strided_bytes(g.nq, g.vs, row, s.item);
+  if (!cu_q || !kv_lens || missing(k, kb) || missing(v, vb) || missing(pages, s.pages) ||
+      cache_missing(*cache, m))
+    return DSA3D_ERR_NULL_POINTER;
+  if (!aligned(k, 16) || !aligned(v, 16) || !cache_aligned(*cache) || !aligned(cu_q, 4) ||
+      !aligned(kv_lens, 4) || !aligned(pages, 4))
+    return DSA3D_ERR_MISALIGNED;
+  const Span in[] = {span_of(k, kb), span_of(v, vb), span_of(cu_q, s.cu),
+                     span_of(kv_lens, s.lens), span_of(pages, s.pages)};
+  const Span outs[] = {span_of(cache->k, m.codes), span_of(cache->v, m.codes),
+                       span_of(cache->k_scales, m.scales), span_of(cache->v_scales, m.scales)};
+  const dsa3d_status al = check_alias(in, 5, outs, 4);
+  if (al != DSA3D_OK) return al;
+  const hipError_t e = dsa3d::launch_paged_append_mx(g, desc->dtype == DSA3D_BF16, k, v, cu_q,
+                                                     kv_lens, pages, *cache, stream);
+  return e == hipSuccess ? DSA3D_OK : DSA3D_ERR_DEVICE;
+}
+
+dsa3d_status dsa3d_paged_read_mx(const dsa3d_paged_desc* desc, const dsa3d_mx_cache* cache,
+                                 const int32_t* pages, const int32_t* kv_lens,
+                                 const int32_t* cu_q, void* k, void* v, hipStream_t stream) {
+  dsa3d::PagedGeometry g;
+  PagedSizes s;
+  MxSizes m;
+  const dsa3d_status st = check_cache(desc, cache, true, &g, &s, &m);
+  if (st != DSA3D_OK) return st;
+  const int64_t row = (int64_t)g.KH * g.D;
+  const uint64_t kb = strided_bytes(g.nq, g.ks, row, s.item),
+                 vb = strided_bytes(g.nq, g.vs, row, s.item);
+  if (!cu_q || !kv_lens || missing(k, kb) || missing(v, vb) || missing(pages, s.pages) ||
+      cache_missing(*cache, m))
+    return DSA3D_ERR_NULL_POINTER;
+  if (!aligned(k, 16) || !aligned(v, 16) || !cache_aligned(*cache) || !aligned(cu_q, 4) ||
+      !aligned(kv_lens, 4) || !aligned(pages, 4))
+    return DSA3D_ERR_MISALIGNED;
+  const Span in[] = {span_of(cache->k, m.codes),         span_of(cache->v, m.codes),
+                     span_of(cache->k_scales, m.scales), span_of(cache->v_scales, m.scales),
+                     span_of(cu_q, s.cu),                span_of(kv_lens, s.lens),
+                     span_of(pages, s.pages)};
+  const Span outs[] = {span_of(k, kb), span_of(v, vb)};
+  const dsa3d_status al = check_alias(in, 7, outs, 2);
+  if (al != DSA3D_OK) return al;
+  const hipError_t e = dsa3d::launch_paged_read_mx(g, desc->dtype == DSA3D_BF16, *cache, pages,
+                                                   kv_lens, cu_q, k, v, stream);
+  return e == hipSuccess ? DSA3D_OK : DSA3D_ERR_DEVICE;
+}
+
+size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32_t bits) {
+  dsa3d::PagedGeometry g;
+  PagedSizes s;
+  if (check_paged(desc, false, &g, &s) != DSA3D_OK || check_bits(bits) != DSA3D_OK) return 0;
+  return dsa3d::paged_workspace(g);
+}
+
+dsa3d_status dsa3d_paged_forward_mx(const dsa3d_paged_desc* desc, const void* q,
+                                    const dsa3d_mx_cache* cache, const int32_t* pages,
+                                    const int32_t* kv_lens, const int32_t* cu_q,
+                                    const float* bias_table, const int32_t* bias_map, void* out,
+                                    float* lse, void* workspace, size_t workspace_bytes,
+                                    hipStream_t stream) {
+  dsa3d::PagedGeometry g;
+  PagedSizes s;
+  MxSizes m;
+  const dsa3d_status st = check_cache(desc, cache, false, &g, &s, &m);
+  if (st != DSA3D_OK) return st;
+  if (!cu_q || !kv_lens || missing(q, s.q) || missing(out, s.out) || missing(pages, s.pages) ||
+      cache_missing(*cache, m) || missing(bias_table, s.table) || missing(bias_map, s.map))
+    return DSA3D_ERR_NULL_POINTER;
+  const uint64_t need = dsa3d::paged_workspace(g);
+  if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return DSA3D_ERR_WORKSPACE;
+  if (!aligned(q, 16) || !cache_aligned(*cache) || !aligned(out, 16) || !aligned(lse, 4) ||
+      !aligned(cu_q, 4) || !aligned(kv_lens, 4) || !aligned(pages, 4) ||
+      !aligned(bias_table, 4) || !aligned(bias_map, 4) || !aligned(workspace, 256))
+    return DSA3D_ERR_MISALIGNED;
+  const Span in[] = {span_of(q, s.q),
+                     span_of(cache->k, m.codes),
+                     span_of(cache->v, m.codes),
+                     span_of(cache->k_scales, m.scales),
+                     span_of(cache->v_scales, m.scales),
+                     span_of(pages, s.pages),
+                     span_of(kv_lens, s.lens),
+                     span_of(cu_q, s.cu),
+                     span_of(bias_table, s.table),
+                     span_of(bias_map, s.map)};
+  const Span outs[] = {span_of(out, s.out), span_of(lse, lse ? s.lse : 0),
+                       span_of(workspace, need)};
+  const dsa3d_status al = check_alias(in, 10, outs, 3);
+  if (al != DSA3D_OK) return al;
+  const hipError_t e = dsa3d::launch_paged_forward_mx(
+      g, desc->dtype == DSA3D_BF16, q, *cache, pages, kv_lens, cu_q, bias_table, bias_map, out,
+      lse, workspace, stream);
   return e == hipSuccess ? DSA3D_OK : DSA3D_ERR_DEVICE;
 }
 

@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "dsa3d_mx.h"
+
 namespace dsa3d {
 
 // How a launch deals (unit, slot) pairs out over the 8 XCDs (see work_of).
@@ -95,5 +97,17 @@ hipError_t launch_paged_join(const PagedGeometry& g, bool bf16, const float* par
 hipError_t launch_paged_append(const PagedGeometry& g, bool bf16, const void* k, const void* v,
                                const int32_t* cu_q, const int32_t* kv_lens, const int32_t* pages,
                                void* k_pages, void* v_pages, hipStream_t stream);
+hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,
+                                   const dsa3d_mx_cache& cache, const int32_t* pages,
+                                   const int32_t* kv_lens, const int32_t* cu_q,
+                                   const float* table, const int32_t* map, void* out, float* lse,
+                                   void* workspace, hipStream_t stream);
+hipError_t launch_paged_append_mx(const PagedGeometry& g, bool bf16, const void* k, const void* v,
+                                  const int32_t* cu_q, const int32_t* kv_lens,
+                                  const int32_t* pages, const dsa3d_mx_cache& cache,
+                                  hipStream_t stream);
+hipError_t launch_paged_read_mx(const PagedGeometry& g, bool bf16, const dsa3d_mx_cache& cache,
+                                const int32_t* pages, const int32_t* kv_lens, const int32_t* cu_q,
+                                void* k, void* v, hipStream_t stream);
 
 }  // namespace dsa3d

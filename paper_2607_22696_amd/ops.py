@@ -14,11 +14,14 @@ import torch
 from ._binding import (dsa3d_backward, dsa3d_backward_timed, dsa3d_backward_workspace_size,
                        dsa3d_dwconv3d_backward, dsa3d_dwconv3d_backward_workspace_size,
                        dsa3d_dwconv3d_forward, dsa3d_forward, dsa3d_paged_append,
-                       dsa3d_paged_forward, dsa3d_paged_forward_workspace_size, dsa3d_pw_backward,
+                       dsa3d_paged_append_mx, dsa3d_paged_forward, dsa3d_paged_forward_mx,
+                       dsa3d_paged_forward_mx_workspace_size, dsa3d_paged_forward_workspace_size,
+                       dsa3d_paged_read_mx, dsa3d_pw_backward,
                        dsa3d_pw_backward_workspace_size, dsa3d_pw_forward, dsa3d_relative_buckets,
                        dsa3d_seq_backward, dsa3d_seq_backward_workspace_size, dsa3d_seq_forward,
                        dsa3d_win_backward, dsa3d_win_backward_workspace_size, dsa3d_win_forward,
-                       make_conv_desc, make_desc, make_paged_desc, make_seq_desc, make_win_desc)
+                       make_conv_desc, make_desc, make_mx_cache, make_paged_desc, make_seq_desc,
+                       make_win_desc)
 
 _IO_DTYPES = {torch.bfloat16: "bf16", torch.float32: "f32"}
 
@@ -634,5 +637,143 @@ def paged_forward(q, k_pages, v_pages, pages, kv_lens, cu_q, causal=True, scale=
     if need and (workspace is None or workspace.numel() < need):
         workspace = torch.empty(need, dtype=torch.uint8, device=dev)
     _launch(dev, dsa3d_paged_forward, desc, q, k_pages, v_pages, pages, kv_lens, cu_q, rel_table,
+            rel_buckets, out, lse, workspace, need)
+    return out, lse
+
+
+# ------------------------------------------------------------------- a paged cache in 8 or 4 bits
+
+_MX_BLOCK = 32  # channels that share a power of two
+
+
+def paged_cache_mx(num_pages, page_size, kv_heads, head_dim, bits=8, device="cuda"):
+    """An empty cache for the calls below: (k, v, k_scales, v_scales), uint8 tensors
+    [num_pages, kv_heads, page_size, head_dim * bits / 8] of elements and
+    [num_pages, kv_heads, page_size, head_dim / 32] of powers of two (see paged_append_mx)."""
+    chk = _Checks("paged_cache_mx")
+    if bits not in (4, 8):
+        chk.problems.append(f"bits: {bits} (expected 8 or 4)")
+    if head_dim not in (64, 128):
+        chk.problems.append(f"head_dim: {head_dim} (expected 64 or 128)")
+    chk.done()
+    shape = (num_pages, kv_heads, page_size)
+    sizes = (head_dim * bits // 8,) * 2 + (head_dim // _MX_BLOCK,) * 2
+    return tuple(torch.zeros(*shape, n, dtype=torch.uint8, device=device) for n in sizes)
+
+
+def _cache_mx(chk, cache, pages, kv_lens, cu_q, device):
+    """Checks the cache; returns (cache of the library, requests, num_pages, page_size, kv_heads,
+    head_dim, columns)."""
+    if not isinstance(cache, (tuple, list)) or len(cache) != 4 or \
+            not all(isinstance(t, torch.Tensor) and t.dim() == 4 for t in cache):
+        chk.problems.append("cache: expected (k, v, k_scales, v_scales), uint8 tensors "
+                            "[pages, kv_heads, page_size, bytes]")
+        chk.done()
+    k, v, k_scales, v_scales = cache
+    num, heads, size, wide = k.shape
+    D = k_scales.shape[3] * _MX_BLOCK
+    bits = 4 if 2 * wide == D else 8
+    for name, t, n in (("k", k, D * bits // 8), ("v", v, D * bits // 8),
+                       ("k_scales", k_scales, D // _MX_BLOCK),
+                       ("v_scales", v_scales, D // _MX_BLOCK)):
+        chk.tensor(f"cache {name}", t, (num, heads, size, n), torch.uint8, device)
+    batch = _cu(chk, "cu_q", cu_q, device)
+    _ints(chk, "kv_lens", kv_lens, (batch,), device)
+    if not isinstance(pages, torch.Tensor) or pages.dim() != 2:
+        chk.problems.append("pages: expected an int32 [requests, columns] tensor")
+        chk.done()
+    _ints(chk, "pages", pages, (batch, pages.shape[1]), device)
+    return make_mx_cache(*cache, bits), batch, num, size, heads, D, pages.shape[1]
+
+
+def paged_append_mx(k, v, cache, pages, kv_lens, cu_q):
+    """Writes the new tokens' k, v [rows, kv_heads, head_dim] (bf16 or float32, packed by cu_q, rows
+    any distance apart) into a cache of 8 or 4 bits (paged_cache_mx), in place; requests, pages and
+    dropped tokens as for paged_append.  Every 32 channels of a token and head are rounded to 8-bit
+    (e4m3) or 4-bit (e2m1) floats times the least power of two with which none saturates; a block
+    that is not finite reads as NaN."""
+    chk = _Checks("paged_append_mx")
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        chk.problems.append("k: expected a [rows, kv_heads, head_dim] tensor")
+        chk.done()
+    if k.dtype not in _IO_DTYPES:
+        chk.problems.append(f"k: unsupported dtype {k.dtype}")
+        chk.done()
+    if not k.is_cuda:
+        chk.problems.append(f"k: not a CUDA tensor ({k.device})")
+    dev = k.device
+    held, batch, num, size, heads, D, columns = _cache_mx(chk, cache, pages, kv_lens, cu_q, dev)
+    ks = _rows(chk, "k", k, heads, D, k.dtype, dev, k.shape[0])
+    vs = _rows(chk, "v", v, heads, D, k.dtype, dev, k.shape[0])
+    chk.done()
+    desc = make_paged_desc(batch, k.shape[0], heads, heads, D, num, size, columns,
+                           dtype=_IO_DTYPES[k.dtype], k_stride=ks, v_stride=vs)
+    _launch(dev, dsa3d_paged_append_mx, desc, k, v, cu_q, kv_lens, pages, held)
+
+
+def paged_read_mx(cache, pages, kv_lens, cu_q, rows, dtype=torch.bfloat16, k=None, v=None):
+    """Reads tokens of the cache back as packed rows [rows, kv_heads, head_dim], exactly: of request
+    b the last cu_q[b + 1] - cu_q[b] of its kv_lens[b] (a smaller kv_lens reads earlier ones).
+    Tokens without a page and rows behind the last request read as 0.  Returns (k, v), new tensors
+    of `dtype` (bf16 or float32) or the ones given."""
+    chk = _Checks("paged_read_mx")
+    if dtype not in _IO_DTYPES:
+        chk.problems.append(f"dtype: unsupported {dtype}")
+        chk.done()
+    if not isinstance(cu_q, torch.Tensor) or not cu_q.is_cuda:
+        chk.problems.append("cu_q: not a CUDA tensor")
+        if not isinstance(cu_q, torch.Tensor):
+            chk.done()
+    dev = cu_q.device
+    rows = _int32(chk, "rows", rows)
+    if rows < 0:
+        chk.problems.append(f"rows: {rows}")
+    held, batch, num, size, heads, D, columns = _cache_mx(chk, cache, pages, kv_lens, cu_q, dev)
+    ks = 0 if k is None else _rows(chk, "k", k, heads, D, dtype, dev, rows)
+    vs = 0 if v is None else _rows(chk, "v", v, heads, D, dtype, dev, rows)
+    chk.done()
+    desc = make_paged_desc(batch, rows, heads, heads, D, num, size, columns,
+                           dtype=_IO_DTYPES[dtype], k_stride=ks, v_stride=vs)
+    if k is None:
+        k = torch.empty(rows, heads, D, dtype=dtype, device=dev)
+    if v is None:
+        v = torch.empty(rows, heads, D, dtype=dtype, device=dev)
+    _launch(dev, dsa3d_paged_read_mx, desc, held, pages, kv_lens, cu_q, k, v)
+    return k, v
+
+
+def paged_forward_mx(q, cache, pages, kv_lens, cu_q, causal=True, scale=0.0, rel_table=None,
+                     rel_buckets=None, rel_min=0, max_kv=0, need_lse=False, out=None, lse=None,
+                     workspace=None):
+    """Attention of the newest tokens q [rows, heads, head_dim] (bf16 or float32) over a cache of 8
+    or 4 bits, as paged_forward over one of q's type: the values that the cache stands for enter
+    the products exactly.  Returns (out, lse)."""
+    chk = _Checks("paged_forward_mx")
+    dev = _lead_rows(chk, q)
+    nq, heads, D = q.shape
+    qs = _rows(chk, "q", q, heads, D, q.dtype, dev, nq)
+    held, batch, num, size, kv_heads, kD, columns = _cache_mx(chk, cache, pages, kv_lens, cu_q,
+                                                              dev)
+    if kD != D or kv_heads < 1 or heads % kv_heads:
+        chk.problems.append(f"cache: {kv_heads} heads x {kD} for queries of {heads} x {D}")
+    lo, span, buckets = _relative(chk, rel_table, rel_buckets, rel_min, heads, dev)
+    chk.optional("out", out, q.shape, q.dtype, dev)
+    if need_lse:
+        chk.optional("lse", lse, q.shape[:2], torch.float32, dev)
+    chk.workspace(workspace, dev)
+    max_kv = _int32(chk, "max_kv", max_kv)
+    chk.done()
+    desc = make_paged_desc(batch, nq, heads, kv_heads, D, num, size, columns, max_kv, causal,
+                           _IO_DTYPES[q.dtype], scale, lo, span, buckets, qs)
+    if out is None:
+        out = _like(q, dev)
+    if not need_lse:
+        lse = None
+    elif lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+    need = dsa3d_paged_forward_mx_workspace_size(desc, held.bits)
+    if need and (workspace is None or workspace.numel() < need):
+        workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+    _launch(dev, dsa3d_paged_forward_mx, desc, q, held, pages, kv_lens, cu_q, rel_table,
             rel_buckets, out, lse, workspace, need)
     return out, lse
