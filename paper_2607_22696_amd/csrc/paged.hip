@@ -521,12 +521,13 @@ hipError_t join_d(const PagedGeometry& g, const float* part_o, const float* part
 
 }  // namespace
 
-void set_plan(PagedGeometry& g) {
+int set_plan(PagedGeometry& g) {
   const PagedPlan p = paged_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = p.part;
   g.tiles = seq_spread(g.KH, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
+  return g.splits;
 }
 
 size_t paged_workspace(const PagedGeometry& g) {

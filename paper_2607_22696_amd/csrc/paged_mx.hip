@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "paged_device.h"
 
 namespace dsa3d {
@@ -51,7 +53,9 @@ struct Piece {
   static constexpr int kEights = W * 4 / BITS;  // chunks of 8 channels
   static constexpr int kBlocks = (kEights + 3) / 4;
   uint32_t w[W];
-  uint32_t scales;
+  // As narrow as in memory: widened where they are loaded, they are widened again at the end of a
+  // loop that they are carried over, which waits for them there.
+  typename std::conditional<kBlocks == 2, uint16_t, uint8_t>::type scales;
 
   __device__ inline void load(const uint8_t* at, const uint8_t* scale_at) {
     if constexpr (W >= 4) {
@@ -69,9 +73,10 @@ struct Piece {
   __device__ inline void clear(bool none) {  // zeros where there is no such key
 #pragma unroll
     for (int i = 0; i < W; ++i) w[i] = none ? 0u : w[i];
-    scales = none ? 0x7f7fu : scales;
+    scales = none ? (decltype(scales))0x7f7f : scales;
   }
   __device__ inline float power(int chunk) const {
+    if constexpr (kBlocks == 1) return power_of(scales);
     return power_of(scales >> (8 * (chunk / 4)) & 255u);
   }
   __device__ inline uint4 eight_at(int chunk) const {
@@ -118,6 +123,17 @@ __device__ inline int64_t place_of_key(const PagedGeometry& g, const int32_t* pa
   return ((int64_t)p * g.KH + u) * g.page_size + (j - page * g.page_size);
 }
 
+// The workgroup's key head, tile and part.  A part of a head's keys stays on one XCD, whose L2 then
+// serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
+// four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, LONG us
+// so).
+__device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split) {
+  if (!work_of(g.tiles, 1, w)) return false;
+  split = w.u / g.KH;
+  w.u -= split * g.KH;
+  return true;
+}
+
 // ------------------------------------------------------------------------- many rows
 
 // 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
@@ -141,8 +157,8 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   extern __shared__ float bias[];
 
   Work w;
-  if (!work_of(g.tiles, g.splits, w)) return;
-  const int split = w.head - w.u * g.splits;
+  int split;
+  if (!work_of_part(g, w, split)) return;
   Span1 s;
   if (!locate<kManyRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
@@ -270,191 +286,393 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 
 // ------------------------------------------------------------------------- few rows
 
-// 32 rows per workgroup; its waves share out the keys in blocks of 32 and read them each for itself,
-// without a barrier until the end: lane l has half the channels of key l % 32, which is the keys'
-// operand (the contraction's order is free as long as the queries have it too).  Values pass
-// through 32 rows of LDS that are the wave's own, to be read transposed.
-template <typename T, int D, int BITS, bool BIAS>
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// 16 x 16 blocks of v_mfma_f32_16x16x32_bf16: lane l has row (column) l % 16 of an operand and 8 of
+// the 32 contraction indices, those of quarter l / 16 of the wave; of the result column l % 16 and
+// rows 4 (l / 16) .. + 3.
+__device__ inline f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// alpha as two bf16 numbers: 16 bits of it.
+struct Two {
+  bf16x8_t h, l;
+};
+__device__ inline f32x4_t times(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
+  return mfma16(a, b, c);
+}
+__device__ inline f32x4_t times(const bf16x8_t& a, const Two& b, f32x4_t c) {
+  c = mfma16(a, b.l, c);
+  return mfma16(a, b.h, c);
+}
+__device__ inline f32x4_t times(const bf16x8_t& a, const Split& b, f32x4_t c) {
+  c = mfma16(a, b.l, c);
+  c = mfma16(a, b.m, c);
+  return mfma16(a, b.h, c);
+}
+template <typename T>
+struct Alpha;
+template <>
+struct Alpha<uint16_t> {
+  using Frag = Two;
+  static __device__ inline Two of(const float (&x)[8]) {
+    Two f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.h[e] = (__bf16)x[e];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f.l[e] = (__bf16)(x[e] - (float)f.h[e]);
+    return f;
+  }
+};
+template <>
+struct Alpha<float> {
+  using Frag = Split;
+  static __device__ inline Split of(const float (&x)[8]) {
+    F32x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y.x[e] = x[e];
+    return seq::split(y);
+  }
+};
+
+// x of the lanes 16 s .. 16 s + 15 in all four quarters, s = 0 .. 3.
+__device__ inline void quarters(uint32_t x, uint32_t (&y)[4]) {
+  const auto half = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const auto two = __builtin_amdgcn_permlane16_swap(half[i], half[i], false, false);
+    y[2 * i] = two[0];
+    y[2 * i + 1] = two[1];
+  }
+}
+// x joined over the four lanes that have the same column.
+template <typename Join>
+__device__ inline float over_quarters(float x, const Join& join) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  x = join(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false,
+                                                  false);
+  return join(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ inline float max_of(float x) {
+  return over_quarters(x, [](float a, float b) { return fmaxf(a, b); });
+}
+__device__ inline float sum_of(float x) {
+  return over_quarters(x, [](float a, float b) { return a + b; });
+}
+
+// A wave's 32 rows of values in LDS: chunks of 8 channels XOR-permuted by the row, so that neither
+// the writes (one chunk of 16 consecutive rows) nor the transposing reads (two neighbouring chunks
+// of 8 consecutive rows) meet in a bank.
+template <int D>
+__device__ inline int value_at(int row, int chan) {
+  const int f = D == 128 ? (row & 7) << 1 | (row >> 3 & 1)
+                         : (row >> 1 & 3) << 1 | (row >> 3 & 1);
+  return row * D + (((chan >> 3) ^ f) << 3) + (chan & 7);
+}
+// Channels d0 .. d0 + 15 as rows, over the 32 keys in the order in which two results hold them:
+// quarter h has keys 4 h .. + 3 and 16 + 4 h .. + 3.
+template <int D>
+__device__ inline bf16x8_t value_cols(const uint16_t* lds, int d0) {
+  typedef short s4_t __attribute__((ext_vector_type(4)));
+  typedef __attribute__((address_space(3))) s4_t lds_s4_t;
+  const int lane = threadIdx.x & 63, j = lane & 15;
+  const int row = 4 * (lane >> 4) + (j >> 2), chan = d0 + 4 * (j & 3);
+  const s4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + value_at<D>(row, chan)));
+  const s4_t hi =
+      __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + value_at<D>(row + 16, chan)));
+  const uint2 ul = __builtin_bit_cast(uint2, lo), uh = __builtin_bit_cast(uint2, hi);
+  return as_bf16x8(make_uint4(ul.x, ul.y, uh.x, uh.y));
+}
+
+// 16 RT rows per workgroup; its waves share out the keys in groups of 64 and read them each for
+// itself, without a barrier until the end.  Half a group at a time, lane l has a quarter of the
+// channels of keys l % 16 and 16 + l % 16, which is the keys' operand (the contraction's order is
+// free as long as the queries have it too).  Values pass through 32 rows of LDS that are the
+// wave's own, to be read transposed.  The places of the next group's keys are looked up one group
+// ahead, a key per lane, and its elements loaded half a group ahead.
+template <typename T, int D, int BITS, bool BIAS, int RT>
 __global__ __launch_bounds__(kThreads)
-__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
+__attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 4)))
 void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     const int32_t* __restrict__ pages, const int32_t* __restrict__ kv_lens,
                     const int32_t* __restrict__ cu_q, const float* __restrict__ table,
                     const int32_t* __restrict__ map, T* __restrict__ out,
                     float* __restrict__ lse, float* __restrict__ part_o,
                     float* __restrict__ part_l) {
-  constexpr int RB = D * BITS / 8, SB = D / 32, KB = 32, WAVES = kThreads / 64;
-  using Tl = Tile<uint16_t, D, KB, 64>;
+  constexpr int RB = D * BITS / 8, SB = D / 32, KB = 64, WAVES = kThreads / 64, ROWS = 16 * RT;
   using Frag = typename Type<T>::Frag;
-  using Half = Piece<BITS, RB / 8>;
-  constexpr int KS = D / 16, DB = D / 32, E = Tl::kElems;
-  // each wave's block of values; at the end the waves' results, half of the channels at a time
+  using AFrag = typename Alpha<T>::Frag;
+  using Quarter = Piece<BITS, RB / 16>;
+  constexpr int KS = D / 32, DC = D / 16, E = 32 * D;
+  // each wave's half group of values; at the end the waves' results of 16 rows in float32
   __shared__ __attribute__((aligned(16))) uint16_t lds[WAVES * E];
-  __shared__ float tops[WAVES][kFewRows], totals[WAVES][kFewRows];
+  __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS];
   extern __shared__ float bias[];
 
   Work w;
-  if (!work_of(g.tiles, g.splits, w)) return;
-  const int split = w.head - w.u * g.splits;
+  int split;
+  if (!work_of_part(g, w, split)) return;
   Span1 s;
-  if (!locate<kFewRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
-  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
-  const int first = s.k_lo + wave * KB;  // this wave's blocks: first, first + 128, ...
-  const int nblocks = s.k_hi > first ? (s.k_hi - first + WAVES * KB - 1) / (WAVES * KB) : 0;
-  auto place = [&](int i) {
-    return place_of_key(g, pages, s.b, w.u,
-                        min(first + i * (WAVES * KB) + (lane & 31), s.k_hi - 1));
-  };
-  auto load = [&](Half& kh, Half& vh, int64_t row) {
-    const int64_t r = max(row, (int64_t)0), at = r * RB + hh * (RB / 2), sc = r * SB + hh * SB / 2;
-    kh.load(c.k + at, c.ks + sc);
-    vh.load(c.v + at, c.vs + sc);
-  };
-  Half k0, v0, k1, v1;
-  int64_t row0 = 0, row1 = 0;
-  if (nblocks > 0) row0 = place(0);
-  if (nblocks > 1) row1 = place(1);
-  if (nblocks > 0) load(k0, v0, row0);
-  if (nblocks > 1) load(k1, v1, row1);
-  if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
-
-  const Row x = row_of(g, s, w.u, s.r0 + (lane & 31));
-  Frag qf[KS];
+  if (!locate<ROWS>(g, cu_q, kv_lens, w.slot, split, s)) return;
+  const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
+  // Queries first, so that waiting for them does not wait for keys.  A column without a row has the
+  // request's first one, and is never stored.
+  Row x[RT];
+  uint4 qw[RT][KS][sizeof(T) / 2];
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {  // channels hh D / 2 + 8 ks .. + 7
-    const T* from = q + x.q_at + hh * (D / 2) + 8 * ks;
-    if constexpr (sizeof(T) == 2) {
-      uint4 y = make_uint4(0, 0, 0, 0);
-      if (x.ok) y = *reinterpret_cast<const uint4*>(from);
-      qf[ks] = as_bf16x8(y);
-    } else {
-      F32x8 y = {};
-      if (x.ok) {
-        *reinterpret_cast<float4*>(y.x) = *reinterpret_cast<const float4*>(from);
-        *reinterpret_cast<float4*>(y.x + 4) = *reinterpret_cast<const float4*>(from + 4);
-      }
-      qf[ks] = seq::split(y);
+  for (int rt = 0; rt < RT; ++rt) {
+    x[rt] = row_of(g, s, w.u, s.r0 + 16 * rt + col);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {  // channels quarter D / 4 + 8 ks .. + 7
+      const T* from = q + x[rt].q_at + quarter * (D / 4) + 8 * ks;
+#pragma unroll
+      for (unsigned i = 0; i < sizeof(T) / 2; ++i)
+        qw[rt][ks][i] = reinterpret_cast<const uint4*>(from)[i];
     }
   }
-  const int pos = s.off + x.i;
-  const int last = min(g.causal ? min(s.seen - 1, pos) : s.seen - 1, s.k_hi - 1);
+  const int first = s.k_lo + wave * KB;  // this wave's groups: first, first + 256, ...
+  const int groups = s.k_hi > first ? (s.k_hi - first + WAVES * KB - 1) / (WAVES * KB) : 0;
+  // Key `lane` of group i, those past the last key repeat it, to be masked: its page number and,
+  // from that, its row among all pages' rows, -1 if it has none.
+  const int32_t* my_pages = pages + (int64_t)s.b * g.max_pages;
+  auto key_of = [&](int i) { return min(first + i * (WAVES * KB) + lane, s.k_hi - 1); };
+  auto page_of = [&](int j) { return my_pages[div_by((uint32_t)j, g.page_mul, g.page_shift)]; };
+  auto row_at = [&](int j, int p) -> int64_t {
+    const int page = div_by((uint32_t)j, g.page_mul, g.page_shift);
+    if (p < 0 || p >= g.num_pages) return -1;
+    return ((int64_t)p * g.KH + w.u) * g.page_size + (j - page * g.page_size);
+  };
+  struct Half {
+    Quarter k[2], v[2];
+  };
+  auto load = [&](Half& x, const uint32_t (&lo)[4], const uint32_t (&hi)[4], int half) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t r = (int64_t)((uint64_t)hi[2 * half + i] << 32 | lo[2 * half + i]);
+      const int64_t row = max(r, (int64_t)0);
+      const int64_t at = row * RB + quarter * (RB / 4), sc = row * SB + quarter * SB / 4;
+      x.k[i].load(c.k + at, c.ks + sc);
+      x.v[i].load(c.v + at, c.vs + sc);
+    }
+  };
+  Half a, b;
+  uint64_t there = 0;  // of the group in a and b
+  int next_page = 0;   // of the group behind it
+  if (groups > 0) {
+    const int64_t row = row_at(key_of(0), page_of(key_of(0)));
+    next_page = page_of(key_of(1));
+    uint32_t lo[4], hi[4];
+    quarters((uint32_t)row, lo);
+    quarters((uint32_t)(row >> 32), hi);
+    there = __ballot(row >= 0);
+    load(a, lo, hi, 0);
+    load(b, lo, hi, 1);
+  }
+  if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
+  Frag qf[RT][KS];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      if constexpr (sizeof(T) == 2) {
+        qf[rt][ks] = as_bf16x8(qw[rt][ks][0]);
+        asm volatile("" : "+v"(qf[rt][ks]));  // waited for here, not in the loop
+      } else {
+        F32x8 y;
+        *reinterpret_cast<uint4*>(y.x) = qw[rt][ks][0];
+        *reinterpret_cast<uint4*>(y.x + 4) = qw[rt][ks][1];
+        qf[rt][ks] = seq::split(y);
+        asm volatile("" : "+v"(qf[rt][ks].h), "+v"(qf[rt][ks].m), "+v"(qf[rt][ks].l));
+      }
+    }
   const int all_see =
       min(g.causal ? min(s.seen - 1, s.off + div_by(s.r0, g.group_mul, g.group_shift))
                    : s.seen - 1, s.k_hi - 1);
-  f32x16_t o[DB];
+  f32x4_t o[RT][DC];
+  float top[RT], base[RT], sum[RT];
 #pragma unroll
-  for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
-  Softmax sm;
+  for (int rt = 0; rt < RT; ++rt) {
+    top[rt] = -INFINITY;
+    base[rt] = sum[rt] = 0.0f;
+#pragma unroll
+    for (int dc = 0; dc < DC; ++dc) o[rt][dc] = f32x4_t{};
+  }
   const float scale = BIAS ? 1.0f : g.scale_log2;
   uint16_t* mine = lds + wave * E;
   if constexpr (BIAS) __syncthreads();
 
-  // Block i, whose elements are in kh and vh: these are free for block i + 2 once they are converted.
-  auto block = [&](int i, Half& kh, Half& vh, int64_t& row) {
-    const int kb = first + i * (WAVES * KB);
-    const uint32_t bits = (uint32_t)__ballot(row >= 0);
-    if (bits != ~0u) vh.clear(row < 0);
-    f32x16_t acc = f32x16_t{};
+  // Half a group, keys kb .. kb + 31, whose elements are in h; `then` may load into h.
+  auto work = [&](Half& h, int kb, uint32_t bits, const auto& then) {
+    f32x4_t acc[RT][2];
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) acc = times(as_bf16x8(kh.eight_at(ks)), qf[ks], acc);
+    for (int i = 0; i < 2; ++i) {
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-      *reinterpret_cast<uint4*>(mine + Tl::at(lane & 31, hh * (D / 2) + 8 * ks)) = vh.eight_at(ks);
-    if (i + 2 < nblocks) {
-      row = place(i + 2);
-      load(kh, vh, row);
+      for (int rt = 0; rt < RT; ++rt) acc[rt][i] = f32x4_t{};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8_t kf = as_bf16x8(h.k[i].eight_at(ks));
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) acc[rt][i] = times(kf, qf[rt][ks], acc[rt][i]);
+      }
     }
-    float t[16];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) t[e] = acc[e];
-    if constexpr (BIAS) add_bias(t, g, bias, x.head - w.u * g.group, kb, pos);
-    if (bits != ~0u || kb + 31 > all_see) {
-      asm volatile("");  // a branch: blocks that every row sees do not pay for it
-      const int seen = last - kb - 4 * hh;
-      const uint32_t have = bits >> (4 * hh);
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (c_row(e, 0) > seen || (have >> c_row(e, 0) & 1) == 0) t[e] = -INFINITY;
+      for (int ks = 0; ks < KS; ++ks)
+        *reinterpret_cast<uint4*>(mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
+            h.v[i].eight_at(ks);
+    if (bits != ~0u) {  // what lies where a page number leads to no key may be NaN
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if ((bits >> (16 * i + col) & 1) == 0) {
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks)
+            *reinterpret_cast<uint4*>(mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
+                make_uint4(0, 0, 0, 0);
+        }
     }
-    sm.raise_to(t, scale, o);
-    sm.weigh(t, scale);
-    Frag pf[2];
-    to_frags(t, pf);
+    // Loads moved up to before the conversions would need other registers, and copies of them that
+    // wait at the loop's end.
+    __builtin_amdgcn_sched_barrier(0);
+    then();
+    AFrag pf[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      // element e is key kb + 16 (e / 4) + 4 quarter + e % 4
+      float t[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) t[e] = acc[rt][e / 4][e % 4];
+      const int pos = s.off + x[rt].i;
+      if constexpr (BIAS) {
+        const float* tab = bias + (x[rt].head - w.u * g.group) * g.span;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int d = kb + 16 * (e / 4) + 4 * quarter + e % 4 - pos - g.rel_min;
+          t[e] = fmaf(t[e], g.scale_log2, tab[min(max(d, 0), g.span - 1)]);
+        }
+      }
+      if (bits != ~0u || kb + 31 > all_see) {
+        asm volatile("");  // a branch: blocks that every row sees do not pay for it
+        const int last = min(g.causal ? min(s.seen - 1, pos) : s.seen - 1, s.k_hi - 1);
+        const int seen = last - kb - 4 * quarter;
+        const uint32_t have = bits >> (4 * quarter);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (16 * (e / 4) + e % 4 > seen || (have >> (16 * (e / 4) + e % 4) & 1) == 0)
+            t[e] = -INFINITY;
+      }
+      float mx = fmaxf(t[0], t[1]);
+#pragma unroll
+      for (int e = 2; e < 8; ++e) mx = fmaxf(mx, t[e]);
+      mx = max_of(mx) * scale;  // scale > 0
+      const bool raise = mx > top[rt] + kSlack;
+      if (__any(raise)) {
+        const float corr = raise ? __builtin_amdgcn_exp2f(top[rt] - mx) : 1.0f;
+        if (raise) top[rt] = base[rt] = mx;
+        sum[rt] *= corr;
+#pragma unroll
+        for (int dc = 0; dc < DC; ++dc) o[rt][dc] *= corr;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        t[e] = __builtin_amdgcn_exp2f(fmaf(t[e], scale, -base[rt]));
+        sum[rt] += t[e];
+      }
+      pf[rt] = Alpha<T>::of(t);
+    }
     fence_wave();
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int dc = 0; dc < DC; ++dc) {
+      const bf16x8_t vf = value_cols<D>(mine, 16 * dc);
 #pragma unroll
-      for (int p = 0; p < 2; ++p) o[db] = times(Tl::a_cols(mine, db * 32, 0, p), pf[p], o[db]);
+      for (int rt = 0; rt < RT; ++rt) o[rt][dc] = times(vf, pf[rt], o[rt][dc]);
+    }
     fence_wave();
   };
-  for (int i = 0; i < nblocks; i += 2) {
-    block(i, k0, v0, row0);
-    if (i + 1 < nblocks) block(i + 1, k1, v1, row1);
+  // The last group apart: with no load behind a condition the compiler counts those in flight, and
+  // waits for no more than it needs.
+  int i = 0;
+  for (; i + 1 < groups; ++i) {
+    const int kb = first + i * (WAVES * KB);
+    const int64_t row = row_at(key_of(i + 1), next_page);
+    next_page = page_of(key_of(i + 2));
+    uint32_t lo[4], hi[4];
+    quarters((uint32_t)row, lo);
+    quarters((uint32_t)(row >> 32), hi);
+    work(a, kb, (uint32_t)there, [&] { load(a, lo, hi, 0); });
+    work(b, kb + 32, (uint32_t)(there >> 32), [&] { load(b, lo, hi, 1); });
+    there = __ballot(row >= 0);
+  }
+  if (groups > 0) {
+    const int kb = first + i * (WAVES * KB);
+    work(a, kb, (uint32_t)there, [] {});
+    if (kb + 32 < s.k_hi) work(b, kb + 32, (uint32_t)(there >> 32), [] {});
   }
 
-  // The waves' sums join over a common maximum, D / 2 channels at a time.
-  const float lw = pair_sum(sm.l);
-  if (hh == 0) {
-    tops[wave][lane] = sm.top;
-    totals[wave][lane] = lw;
+  // The waves' sums join over a common maximum, 16 rows at a time.
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const float total = sum_of(sum[rt]);
+    if (quarter == 0) {
+      tops[wave][16 * rt + col] = top[rt];
+      totals[wave][16 * rt + col] = total;
+    }
   }
   __syncthreads();
-  const int col = lane & 31;
   const auto most = [&](int r) {
-    return fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+    float y = tops[0][r];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) y = fmaxf(y, tops[i][r]);
+    return y;
   };
-  const float own = sm.top == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm.top - most(col));
-  const int count = min(s.rows - s.r0, kFewRows);
-  constexpr int CH = D / 8;  // chunks of four channels in a half
+  const int count = min(s.rows - s.r0, ROWS);
   float* sums = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
-    if (half) __syncthreads();
+  for (int rt = 0; rt < RT; ++rt) {
+    if (rt > 0) __syncthreads();
+    const float own =
+        top[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(top[rt] - most(16 * rt + col));
 #pragma unroll
-    for (int d = 0; d < DB / 2; ++d)
-#pragma unroll
-      for (int blk = 0; blk < 4; ++blk) {
-        const int chunk = d * 8 + 2 * blk + hh;  // permuted against bank conflicts
-        const f32x16_t& y = o[half * (DB / 2) + d];
-        *reinterpret_cast<float4*>(sums + (wave * kFewRows + col) * (D / 2) +
-                                   ((chunk ^ (col & (CH - 1))) << 2)) =
-            make_float4(y[4 * blk] * own, y[4 * blk + 1] * own, y[4 * blk + 2] * own,
-                        y[4 * blk + 3] * own);
-      }
+    for (int dc = 0; dc < DC; ++dc) {  // four channels, permuted against bank conflicts
+      const int chunk = 4 * dc + quarter;
+      const f32x4_t& y = o[rt][dc];
+      *reinterpret_cast<float4*>(sums + (wave * 16 + col) * D + ((chunk ^ col) << 2)) =
+          make_float4(y[0] * own, y[1] * own, y[2] * own, y[3] * own);
+    }
     __syncthreads();
-    for (int e = threadIdx.x; e < count * CH; e += kThreads) {
-      const int r = e / CH, chunk = e % CH;
-      const float tr = most(r);
+    for (int e = threadIdx.x; e < min(count - 16 * rt, 16) * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), chunk = e % (D / 4), at_row = 16 * rt + r;
+      const float tr = most(at_row);
       float total = 0.0f;
-      float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) {
-        float f = totals[i][r];
-        if (tops[i][r] != -INFINITY) f *= __builtin_amdgcn_exp2f(tops[i][r] - tr);
+        float f = totals[i][at_row];
+        if (tops[i][at_row] != -INFINITY) f *= __builtin_amdgcn_exp2f(tops[i][at_row] - tr);
         total += f;
-        const float4 y = *reinterpret_cast<const float4*>(
-            sums + (i * kFewRows + r) * (D / 2) + ((chunk ^ (r & (CH - 1))) << 2));
-        sum.x += y.x;
-        sum.y += y.y;
-        sum.z += y.z;
-        sum.w += y.w;
+        const float4 z =
+            *reinterpret_cast<const float4*>(sums + (i * 16 + r) * D + ((chunk ^ r) << 2));
+        y.x += z.x;
+        y.y += z.y;
+        y.z += z.z;
+        y.w += z.w;
       }
       const float inv = total > 0.0f ? 1.0f / total : total;
       const float l2 = total == 0.0f
                            ? -INFINITY
                            : (tr == -INFINITY ? 0.0f : tr) + __builtin_amdgcn_logf(total);
-      const float4 y = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-      const Row z = row_of(g, s, w.u, s.r0 + r);
-      const int at_chan = half * (D / 2) + chunk * 4;
-      const bool lead = half == 0 && chunk == 0;
+      y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+      const Row z = row_of(g, s, w.u, s.r0 + at_row);
       if (s.only) {
-        store_4(out + z.out_at * D + at_chan, y);
-        if (lead && lse != nullptr) lse[z.out_at] = l2 * kLn2;
-        if (lead && g.splits > 1) part_l[z.out_at * g.splits] = kDone;
+        store_4(out + z.out_at * D + chunk * 4, y);
+        if (chunk == 0 && lse != nullptr) lse[z.out_at] = l2 * kLn2;
+        if (chunk == 0 && g.splits > 1) part_l[z.out_at * g.splits] = kDone;
       } else {
         const int64_t at = z.out_at * g.splits + split;
-        if (total != 0.0f) store_4(part_o + at * D + at_chan, y);
-        if (lead) part_l[at] = part_lse(l2);
+        if (total != 0.0f) store_4(part_o + at * D + chunk * 4, y);
+        if (chunk == 0) part_l[at] = part_lse(l2);
       }
     }
   }
@@ -637,12 +855,13 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
   float* part_l = g.splits > 1 ? (float*)ws : nullptr;
   float* part_o = g.splits > 1 ? (float*)((char*)ws + round_256((size_t)g.splits * rows * 4))
                                : nullptr;
-  const void* fn = g.tile == kFewRows
-                       ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true>
-                               : (const void*)&mx_keys_kernel<T, D, BITS, false>)
-                       : (bias ? (const void*)&mx_rows_kernel<T, D, BITS, true>
-                               : (const void*)&mx_rows_kernel<T, D, BITS, false>);
-  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, g.splits), kThreads,
+  const void* fn = g.tile == 16   ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true, 1>
+                                          : (const void*)&mx_keys_kernel<T, D, BITS, false, 1>)
+                   : g.tile == 32 ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true, 2>
+                                          : (const void*)&mx_keys_kernel<T, D, BITS, false, 2>)
+                                  : (bias ? (const void*)&mx_rows_kernel<T, D, BITS, true>
+                                          : (const void*)&mx_rows_kernel<T, D, BITS, false>);
+  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, 1), kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1)
@@ -668,6 +887,15 @@ hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache
 }
 
 }  // namespace
+
+int set_plan_mx(PagedGeometry& g) {
+  const PagedPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
+  g.tile = p.tile;
+  g.splits = p.splits;
+  g.part = p.part;
+  g.tiles = seq_spread(g.KH * g.splits, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
+  return 1;
+}
 
 hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,
                                    const dsa3d_mx_cache& cache, const int32_t* pages,

@@ -55,4 +55,11 @@ inline PagedPlan paged_plan(int64_t tokens, int group, int kv_heads, int batch, 
   return p;
 }
 
+// The same over a cache of 8 or 4 bits, whose form with few rows has 16 or 32 of them.
+inline PagedPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv) {
+  PagedPlan p = paged_plan(tokens, group, kv_heads, batch, max_kv);
+  if (tokens * group <= (int64_t)16 * batch) p.tile = 16;
+  return p;
+}
+
 }  // namespace dsa3d

@@ -259,7 +259,7 @@ void divisor(int d, uint32_t* mul, uint32_t* shift) {
 }
 
 dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeometry* g,
-                         PagedSizes* s) {
+                         PagedSizes* s, int (*set_plan)(dsa3d::PagedGeometry&) = dsa3d::set_plan) {
   if (d == nullptr) return DSA3D_ERR_NULL_POINTER;
   if (d->batch < 1 || d->batch >= (1 << 24) || d->total_q < 0 || d->num_pages < 0 ||
       d->page_size < 1 || d->max_pages < 0 || d->max_kv < 0 ||
@@ -308,8 +308,8 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     return DSA3D_ERR_UNSUPPORTED;
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
-  dsa3d::set_plan(*g);
-  if (!append && dsa3d::seq_blocks(g->tiles, g->splits) > dsa3d::kMostBlocks)
+  const int per = set_plan(*g);
+  if (!append && dsa3d::seq_blocks(g->tiles, per) > dsa3d::kMostBlocks)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->out = (uint64_t)d->total_q * qrow * s->item;
@@ -417,7 +417,7 @@ dsa3d_status check_bits(int32_t bits) {
 dsa3d_status check_cache(const dsa3d_paged_desc* d, const dsa3d_mx_cache* c, bool rows,
                          dsa3d::PagedGeometry* g, PagedSizes* s, MxSizes* m) {
   if (c == nullptr) return DSA3D_ERR_NULL_POINTER;
-  dsa3d_status st = check_paged(d, rows, g, s);
+  dsa3d_status st = check_paged(d, rows, g, s, dsa3d::set_plan_mx);
   if (st == DSA3D_OK) st = check_bits(c->bits);
   if (st != DSA3D_OK) return st;
   const uint64_t held = (uint64_t)g->num_pages * g->page_size * g->KH;
@@ -501,7 +501,9 @@ dsa3d_status dsa3d_paged_read_mx(const dsa3d_paged_desc* desc, const dsa3d_mx_ca
 size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32_t bits) {
   dsa3d::PagedGeometry g;
   PagedSizes s;
-  if (check_paged(desc, false, &g, &s) != DSA3D_OK || check_bits(bits) != DSA3D_OK) return 0;
+  if (check_paged(desc, false, &g, &s, dsa3d::set_plan_mx) != DSA3D_OK ||
+      check_bits(bits) != DSA3D_OK)
+    return 0;
   return dsa3d::paged_workspace(g);
 }
 

@@ -84,7 +84,9 @@ struct PagedGeometry {
   Spread tiles;
 };
 
-void set_plan(PagedGeometry& g);  // tile, splits, part and tiles
+// Sets tile, splits, part and tiles; returns how many workgroups each (unit, slot) of tiles has.
+int set_plan(PagedGeometry& g);
+int set_plan_mx(PagedGeometry& g);  // for a cache of 8 or 4 bits
 size_t paged_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,
                                 const void* k_pages, const void* v_pages, const int32_t* pages,
