@@ -455,22 +455,22 @@ def make_mx_cache(k, v, k_scales, v_scales, bits) -> dsa3d_mx_cache:
     return dsa3d_mx_cache(_ptr(k), _ptr(v), _ptr(k_scales), _ptr(v_scales), bits)
 
 
-def _ref(struct):
-    return ctypes.byref(struct) if struct is not None else None
-
-
 def dsa3d_paged_append_mx(desc, k, v, cu_q, kv_lens, pages, cache, stream=None,
                           check=True) -> int:
-    st = load().dsa3d_paged_append_mx(_ref(desc), _ptr(k), _ptr(v), _ptr(cu_q), _ptr(kv_lens),
-                                      _ptr(pages), _ref(cache), _stream(stream))
+    st = load().dsa3d_paged_append_mx(ctypes.byref(desc) if desc is not None else None, _ptr(k),
+                                      _ptr(v), _ptr(cu_q), _ptr(kv_lens), _ptr(pages),
+                                      ctypes.byref(cache) if cache is not None else None,
+                                      _stream(stream))
     if check and st != DSA3D_OK:
         raise Dsa3dError(st, "dsa3d_paged_append_mx")
     return st
 
 
 def dsa3d_paged_read_mx(desc, cache, pages, kv_lens, cu_q, k, v, stream=None, check=True) -> int:
-    st = load().dsa3d_paged_read_mx(_ref(desc), _ref(cache), _ptr(pages), _ptr(kv_lens),
-                                    _ptr(cu_q), _ptr(k), _ptr(v), _stream(stream))
+    st = load().dsa3d_paged_read_mx(ctypes.byref(desc) if desc is not None else None,
+                                    ctypes.byref(cache) if cache is not None else None,
+                                    _ptr(pages), _ptr(kv_lens), _ptr(cu_q), _ptr(k), _ptr(v),
+                                    _stream(stream))
     if check and st != DSA3D_OK:
         raise Dsa3dError(st, "dsa3d_paged_read_mx")
     return st
@@ -483,8 +483,9 @@ def dsa3d_paged_forward_mx_workspace_size(desc, bits) -> int:
 def dsa3d_paged_forward_mx(desc, q, cache, pages, kv_lens, cu_q, bias_table, bias_map, out,
                            lse=None, workspace=None, workspace_bytes=0, stream=None,
                            check=True) -> int:
-    st = load().dsa3d_paged_forward_mx(_ref(desc), _ptr(q), _ref(cache), _ptr(pages),
-                                       _ptr(kv_lens), _ptr(cu_q), _ptr(bias_table),
+    st = load().dsa3d_paged_forward_mx(ctypes.byref(desc) if desc is not None else None, _ptr(q),
+                                       ctypes.byref(cache) if cache is not None else None,
+                                       _ptr(pages), _ptr(kv_lens), _ptr(cu_q), _ptr(bias_table),
                                        _ptr(bias_map), _ptr(out), _ptr(lse), _ptr(workspace),
                                        workspace_bytes, _stream(stream))
     if check and st != DSA3D_OK:

@@ -505,18 +505,12 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
   hipError_t e = seq_launch(fn, seq_blocks(g.tiles, g.splits), kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, k, v, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
-  if (e == hipSuccess && g.splits > 1)
-    e = launch_paged_join(g, sizeof(T) == 2, part_o, part_l, out, lse, s);
+  if (e == hipSuccess && g.splits > 1) {
+    constexpr int per = kThreads / 64;
+    e = seq_launch((const void*)&paged_join_kernel<T, D>, (rows + per - 1) / per, kThreads, 0,
+                   s, rows, g.splits, (const float*)part_o, (const float*)part_l, out, lse);
+  }
   return e;
-}
-
-template <typename T, int D>
-hipError_t join_d(const PagedGeometry& g, const float* part_o, const float* part_l, void* out,
-                  float* lse, hipStream_t s) {
-  const int64_t rows = (int64_t)g.nq * g.H;
-  constexpr int per = kThreads / 64;
-  return seq_launch((const void*)&paged_join_kernel<T, D>, (rows + per - 1) / per, kThreads, 0, s,
-                    rows, g.splits, part_o, part_l, (T*)out, lse);
 }
 
 }  // namespace
@@ -534,15 +528,6 @@ size_t paged_workspace(const PagedGeometry& g) {
   if (g.splits == 1) return 0;
   const size_t rows = (size_t)g.splits * g.nq * g.H;
   return round_256(rows * 4) + round_256(rows * g.D * 4);
-}
-
-hipError_t launch_paged_join(const PagedGeometry& g, bool bf16, const float* part_o,
-                             const float* part_l, void* out, float* lse, hipStream_t s) {
-  if (bf16)
-    return g.D == 64 ? join_d<uint16_t, 64>(g, part_o, part_l, out, lse, s)
-                     : join_d<uint16_t, 128>(g, part_o, part_l, out, lse, s);
-  return g.D == 64 ? join_d<float, 64>(g, part_o, part_l, out, lse, s)
-                   : join_d<float, 128>(g, part_o, part_l, out, lse, s);
 }
 
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,

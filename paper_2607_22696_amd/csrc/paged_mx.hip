@@ -316,12 +316,15 @@ template <>
 struct Alpha<uint16_t> {
   using Frag = Two;
   static __device__ inline Two of(const float (&x)[8]) {
-    Two f;
+    uint32_t h[4], l[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.h[e] = (__bf16)x[e];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) f.l[e] = (__bf16)(x[e] - (float)f.h[e]);
-    return f;
+    for (int i = 0; i < 4; ++i) {
+      float y[2] = {x[2 * i], x[2 * i + 1]};
+      h[i] = take_part(y);
+      l[i] = take_part(y);
+    }
+    return {as_bf16x8(make_uint4(h[0], h[1], h[2], h[3])),
+            as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]))};
   }
 };
 template <>
@@ -435,14 +438,19 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   const int first = s.k_lo + wave * KB;  // this wave's groups: first, first + 256, ...
   const int groups = s.k_hi > first ? (s.k_hi - first + WAVES * KB - 1) / (WAVES * KB) : 0;
   // Key `lane` of group i, those past the last key repeat it, to be masked: its page number and,
-  // from that, its row among all pages' rows, -1 if it has none.
+  // from that, its row among all pages' rows, handed to the lanes that load it.  Returns which keys
+  // have a row; the others' lanes load row 0.
   const int32_t* my_pages = pages + (int64_t)s.b * g.max_pages;
   auto key_of = [&](int i) { return min(first + i * (WAVES * KB) + lane, s.k_hi - 1); };
   auto page_of = [&](int j) { return my_pages[div_by((uint32_t)j, g.page_mul, g.page_shift)]; };
-  auto row_at = [&](int j, int p) -> int64_t {
-    const int page = div_by((uint32_t)j, g.page_mul, g.page_shift);
-    if (p < 0 || p >= g.num_pages) return -1;
-    return ((int64_t)p * g.KH + w.u) * g.page_size + (j - page * g.page_size);
+  auto places = [&](int i, int p, uint32_t (&lo)[4], uint32_t (&hi)[4]) {
+    const int j = key_of(i), page = div_by((uint32_t)j, g.page_mul, g.page_shift);
+    const bool ok = (uint32_t)p < (uint32_t)g.num_pages;
+    const int64_t row =
+        ok ? ((int64_t)p * g.KH + w.u) * g.page_size + (j - page * g.page_size) : 0;
+    quarters((uint32_t)row, lo);
+    quarters((uint32_t)(row >> 32), hi);
+    return (uint64_t)__ballot(ok);
   };
   struct Half {
     Quarter k[2], v[2];
@@ -450,8 +458,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   auto load = [&](Half& x, const uint32_t (&lo)[4], const uint32_t (&hi)[4], int half) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const int64_t r = (int64_t)((uint64_t)hi[2 * half + i] << 32 | lo[2 * half + i]);
-      const int64_t row = max(r, (int64_t)0);
+      const int64_t row = (int64_t)((uint64_t)hi[2 * half + i] << 32 | lo[2 * half + i]);
       const int64_t at = row * RB + quarter * (RB / 4), sc = row * SB + quarter * SB / 4;
       x.k[i].load(c.k + at, c.ks + sc);
       x.v[i].load(c.v + at, c.vs + sc);
@@ -461,12 +468,9 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   uint64_t there = 0;  // of the group in a and b
   int next_page = 0;   // of the group behind it
   if (groups > 0) {
-    const int64_t row = row_at(key_of(0), page_of(key_of(0)));
-    next_page = page_of(key_of(1));
     uint32_t lo[4], hi[4];
-    quarters((uint32_t)row, lo);
-    quarters((uint32_t)(row >> 32), hi);
-    there = __ballot(row >= 0);
+    there = places(0, page_of(key_of(0)), lo, hi);
+    next_page = page_of(key_of(1));
     load(a, lo, hi, 0);
     load(b, lo, hi, 1);
   }
@@ -596,14 +600,12 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   int i = 0;
   for (; i + 1 < groups; ++i) {
     const int kb = first + i * (WAVES * KB);
-    const int64_t row = row_at(key_of(i + 1), next_page);
-    next_page = page_of(key_of(i + 2));
     uint32_t lo[4], hi[4];
-    quarters((uint32_t)row, lo);
-    quarters((uint32_t)(row >> 32), hi);
+    const uint64_t next_there = places(i + 1, next_page, lo, hi);
+    next_page = page_of(key_of(i + 2));
     work(a, kb, (uint32_t)there, [&] { load(a, lo, hi, 0); });
     work(b, kb + 32, (uint32_t)(there >> 32), [&] { load(b, lo, hi, 1); });
-    there = __ballot(row >= 0);
+    there = next_there;
   }
   if (groups > 0) {
     const int kb = first + i * (WAVES * KB);
@@ -678,62 +680,144 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   }
 }
 
+// ------------------------------------------------------------------------- join
+
+// Joins the parts of each row, weights 2^(l - max l), as paged_join_kernel does, but for many parts
+// with W waves per row, each with its share of the parts, and every load on its way before the
+// first is waited for (64 rows of 63 parts: 12.6 us with one wave and loads behind a branch, 4.0
+// so).  A part without keys has -inf, and its results were never written.
+template <typename T, int D, int W, int AT_ONCE>
+__global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int splits,
+                                                           const float* __restrict__ part_o,
+                                                           const float* __restrict__ part_l,
+                                                           T* __restrict__ out,
+                                                           float* __restrict__ lse) {
+  constexpr int LANES = D / 4, SIDES = 64 / LANES, PER = kThreads / 64 / W;
+  __shared__ float4 sums[W == 1 ? 1 : W][LANES];
+  const int wave = wave_id(), lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)block_number() * PER + wave / W;
+  if (row >= rows) return;
+  const int nth = wave % W * SIDES + lane / LANES, c = lane % LANES * 4;
+  // every wave has all log-sum-exps, a part per lane (at most 64)
+  const float mine = lane < splits ? part_l[row * splits + lane] : -INFINITY;
+  if (__shfl(mine, 0) == kDone) return;
+  float top = mine;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  const float weight = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
+  float total = weight;
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int s0 = 0; s0 < splits; s0 += AT_ONCE * SIDES * W) {
+    float4 x[AT_ONCE];
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int s = min(s0 + i * SIDES * W + nth, splits - 1);
+      x[i] = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
+    }
+#pragma unroll
+    for (int i = 0; i < AT_ONCE; ++i) {
+      const int s = s0 + i * SIDES * W + nth;
+      const float ws = __shfl(weight, s & 63), ls = __shfl(mine, s & 63);
+      if (s < splits && ls != -INFINITY) {
+        sum.x = fmaf(ws, x[i].x, sum.x);
+        sum.y = fmaf(ws, x[i].y, sum.y);
+        sum.z = fmaf(ws, x[i].z, sum.z);
+        sum.w = fmaf(ws, x[i].w, sum.w);
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 32; d >= LANES; d >>= 1) {
+    sum.x += __shfl_xor(sum.x, d);
+    sum.y += __shfl_xor(sum.y, d);
+    sum.z += __shfl_xor(sum.z, d);
+    sum.w += __shfl_xor(sum.w, d);
+  }
+  if constexpr (W > 1) {  // a workgroup is one row
+    if (lane < LANES) sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave > 0 || lane >= LANES) return;
+    sum = sums[0][lane];
+#pragma unroll
+    for (int i = 1; i < W; ++i) {
+      const float4 y = sums[i][lane];
+      sum.x += y.x;
+      sum.y += y.y;
+      sum.z += y.z;
+      sum.w += y.w;
+    }
+  }
+  if (lane >= LANES) return;
+  const float inv = total > 0.0f ? 1.0f / total : total;
+  store_4(out + row * D + c, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+  if (lane == 0 && lse != nullptr) {
+    const float base = top == -INFINITY ? 0.0f : top;
+    lse[row] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+  }
+}
+
 // ------------------------------------------------------------------------- write and read
 
-// Rows of k and v as chunks of 8 channels, k's first: a wave takes 64 chunks of one token, or, where
-// tokens have 32 or fewer, as many tokens as it has room for.
+// Rows of k and v as chunks of 8 channels, a token's key first: chunk n is chunk n % per of token
+// n / per.  A wave takes `steps` times 64 chunks that follow each other, a chunk per lane and step,
+// and looks up the places of its tokens at once, a token per lane.
 struct Rows {
-  int per;     // chunks of a token's key and value together
-  int waves;   // waves per token
-  int tokens;  // tokens per wave
+  int per;                       // chunks of a token's key and value together, at least 16
+  uint32_t per_mul, per_shift;   // chunk / per
 };
-
-inline Rows rows_of(const PagedGeometry& g) {
-  const int per = 2 * g.KH * (g.D / 8);
-  return {per, (per + 63) / 64, per <= 32 ? 64 / per : 1};
-}
+constexpr int kManySteps = 8;    // at most 64 kManySteps / 16 + 1 tokens: a lane for each
 
 // This lane's chunk: token, half (0: key, 1: value), head, first channel; and the token's place.
 struct Chunk {
   int token, which, head, chan;
-  bool ok;        // there is such a chunk
-  int64_t place;  // row among all pages' rows of head 0's layout: page and row within it
-  int page, row;
+  bool ok;            // there is such a chunk
+  int64_t place;      // the head's row among all pages' rows, -1: none
 };
 
-__device__ inline Chunk chunk_of(const PagedGeometry& g, const Rows& r, const int32_t* cu_q,
-                                 const int32_t* kv_lens, const int32_t* pages) {
+template <int STEPS>
+__device__ inline void chunks_of(Chunk (&x)[STEPS], const PagedGeometry& g, const Rows& r,
+                                 const int32_t* cu_q, const int32_t* kv_lens,
+                                 const int32_t* pages) {
   const int lane = threadIdx.x & 63;
-  const uint32_t wid = (uint32_t)block_number() * (kThreads / 64) + wave_id();
-  const uint32_t group = wid / r.waves;
-  const int base = (int)min((uint64_t)group * r.tokens, (uint64_t)g.nq);
-  const int nth = r.tokens == 1 ? 0 : lane / r.per;
-  const int c = r.tokens == 1 ? (int)(wid - group * r.waves) * 64 + lane : lane - nth * r.per;
-  Chunk x;
-  x.token = base + nth;
-  x.ok = c < r.per && nth < r.tokens && nth < g.nq - base;
-  x.which = c >= r.per / 2;
-  const int chan = (c - x.which * (r.per / 2)) * 8;
-  x.head = chan / g.D;
-  x.chan = chan - x.head * g.D;
-  x.page = -1;
-  x.row = 0;
-  for (int i = 0; i < min(r.tokens, g.nq - base); ++i) {  // the same for all lanes
-    const int tok = base + i;
-    const int b = search(g.B, tok, [&](int k) { return cu_at(cu_q, k, g.nq); });
-    if (b >= g.B) continue;
+  const uint64_t base =
+      ((uint64_t)(uint32_t)block_number() * (kThreads / 64) + wave_id()) * (64 * STEPS);
+  const int first = (int)min(base / (uint32_t)r.per, (uint64_t)g.nq);
+  const uint32_t skip = (uint32_t)(base - (uint64_t)(uint32_t)first * (uint32_t)r.per);
+  // Token first + lane: the last request that begins at it or before (up to 64 of them are held by
+  // a lane each), its position, its page.
+  const int tok = first + lane < g.nq && first + lane >= first ? first + lane : g.nq - 1;
+  const int ends = g.B <= 64 ? cu_at(cu_q, min(lane, g.B - 1) + 1, g.nq) : 0;
+  int b = 0;
+  for (int n = g.B + 1; n > 1; n -= n / 2) {
+    const int mid = min(b + n / 2, g.B);
+    if ((g.B <= 64 ? __shfl(ends, mid - 1) : cu_at(cu_q, mid, g.nq)) <= tok) b = mid;
+  }
+  int page = -1, row = 0;
+  if (b < g.B) {
     const int begin = cu_at(cu_q, b, g.nq), n = max(cu_at(cu_q, b + 1, g.nq), begin) - begin;
     const int64_t at = (int64_t)kv_lens[b] - n + (tok - begin);
-    if (tok < begin || tok - begin >= n || at < 0 || at >= (int64_t)g.max_pages * g.page_size)
-      continue;
-    const int page = div_by((uint32_t)at, g.page_mul, g.page_shift);
-    const int p = pages[(int64_t)b * g.max_pages + page];
-    if (p < 0 || p >= g.num_pages || i != nth) continue;
-    x.page = p;
-    x.row = (int)(at - (int64_t)page * g.page_size);
+    if (tok >= begin && tok - begin < n && at >= 0 && at < (int64_t)g.max_pages * g.page_size) {
+      const int nth = div_by((uint32_t)at, g.page_mul, g.page_shift);
+      page = pages[(int64_t)b * g.max_pages + nth];
+      row = (int)(at - (int64_t)nth * g.page_size);
+      if (page < 0 || page >= g.num_pages) page = -1;
+    }
   }
-  x.place = x.page < 0 ? -1 : ((int64_t)x.page * g.KH + x.head) * g.page_size + x.row;
-  return x;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const uint32_t n = skip + 64 * i + lane;
+    const int nth = div_by(n, r.per_mul, r.per_shift), c = (int)n - nth * r.per;
+    x[i].token = first + nth;
+    x[i].ok = nth < g.nq - first;
+    x[i].which = c >= r.per / 2;
+    const int chan = (c - x[i].which * (r.per / 2)) * 8;
+    x[i].head = chan / g.D;
+    x[i].chan = chan - x[i].head * g.D;
+    const int p = __shfl(page, nth), at = __shfl(row, nth);
+    x[i].place = p < 0 ? -1 : ((int64_t)p * g.KH + x[i].head) * g.page_size + at;
+  }
 }
 
 template <typename T>
@@ -764,84 +848,143 @@ __device__ inline uint32_t scale_byte(uint32_t a) {
   return a >= kOver ? 255u : max(e, 10u + kLess) - kLess;
 }
 
-template <typename T, int BITS>
+template <typename T, int D, int BITS, int STEPS>
 __global__ __launch_bounds__(kThreads) void mx_append_kernel(
     PagedGeometry g, Rows r, const T* __restrict__ k, const T* __restrict__ v,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ kv_lens,
     const int32_t* __restrict__ pages, MxPages to) {
-  const Chunk c = chunk_of(g, r, cu_q, kv_lens, pages);
-  const bool ok = c.ok && c.place >= 0;
-  float x[8] = {};
-  if (ok)
-    load_8(x, (c.which ? v + c.token * g.vs : k + c.token * g.ks) + c.head * g.D + c.chan);
-  uint32_t a = 0;
+  g.D = D;
+  Chunk c[STEPS];
+  chunks_of(c, g, r, cu_q, kv_lens, pages);
+  float x[STEPS][8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) a = max(a, __float_as_uint(x[i]) & 0x7fffffffu);
-  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, true));  // lane ^ 1
-  a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true));  // lane ^ 2
-  const uint32_t byte = scale_byte<BITS>(a);
-  if (!ok) return;
-  const bool none = byte == 255u;
-  const float power = power_of(none ? 127u : byte);
+  for (int i = 0; i < STEPS; ++i) {
+    if (c[i].ok && c[i].place >= 0) {
+      load_8(x[i], (c[i].which ? v + c[i].token * g.vs : k + c[i].token * g.ks) +
+                       c[i].head * D + c[i].chan);
+    } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = none ? 0.0f : x[i];
-  uint8_t* codes = c.which ? to.v : to.k;
-  uint8_t* scales = c.which ? to.vs : to.ks;
-  if constexpr (BITS == 8) {
-    typedef short s2_t __attribute__((ext_vector_type(2)));
-    uint32_t u[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      s2_t y = {0, 0};
-      y = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(y, x[4 * i], x[4 * i + 1], power, false);
-      y = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(y, x[4 * i + 2], x[4 * i + 3], power, true);
-      u[i] = __builtin_bit_cast(uint32_t, y);
+      for (int e = 0; e < 8; ++e) x[i][e] = 0.0f;
     }
-    *reinterpret_cast<uint2*>(codes + c.place * g.D + c.chan) = make_uint2(u[0], u[1]);
-  } else {
-    uint32_t u = 0;
-    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[0], x[1], power, 0);
-    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[2], x[3], power, 1);
-    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[4], x[5], power, 2);
-    u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, x[6], x[7], power, 3);
-    *reinterpret_cast<uint32_t*>(codes + (c.place * g.D + c.chan) / 2) = u;
   }
-  if (c.chan % 32 == 0) scales[(c.place * g.D + c.chan) / 32] = (uint8_t)byte;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    uint32_t a = 0;  // the block's largest: four lanes have it
+#pragma unroll
+    for (int e = 0; e < 8; ++e) a = max(a, __float_as_uint(x[i][e]) & 0x7fffffffu);
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, true));  // ^ 1
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true));  // ^ 2
+    if (!c[i].ok || c[i].place < 0) continue;
+    const uint32_t byte = scale_byte<BITS>(a);
+    const bool none = byte == 255u;
+    const float power = power_of(none ? 127u : byte);
+    float (&y)[8] = x[i];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = none ? 0.0f : y[e];
+    uint8_t* codes = c[i].which ? to.v : to.k;
+    uint8_t* scales = c[i].which ? to.vs : to.ks;
+    const int64_t at = c[i].place * D + c[i].chan;
+    if constexpr (BITS == 8) {
+      typedef short s2_t __attribute__((ext_vector_type(2)));
+      uint32_t u[2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        s2_t z = {0, 0};
+        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y[4 * h], y[4 * h + 1], power, false);
+        z = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(z, y[4 * h + 2], y[4 * h + 3], power, true);
+        u[h] = __builtin_bit_cast(uint32_t, z);
+      }
+      *reinterpret_cast<uint2*>(codes + at) = make_uint2(u[0], u[1]);
+    } else {
+      uint32_t u = 0;
+      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[0], y[1], power, 0);
+      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[2], y[3], power, 1);
+      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[4], y[5], power, 2);
+      u = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(u, y[6], y[7], power, 3);
+      *reinterpret_cast<uint32_t*>(codes + at / 2) = u;
+    }
+    if (c[i].chan % 32 == 0) scales[at / 32] = (uint8_t)byte;
+  }
 }
 
-template <typename T, int BITS>
+template <typename T, int D, int BITS, int STEPS>
 __global__ __launch_bounds__(kThreads) void mx_read_kernel(
     PagedGeometry g, Rows r, MxPages from, const int32_t* __restrict__ pages,
     const int32_t* __restrict__ kv_lens, const int32_t* __restrict__ cu_q, T* __restrict__ k,
     T* __restrict__ v) {
-  const Chunk c = chunk_of(g, r, cu_q, kv_lens, pages);
-  if (!c.ok) return;
-  uint4 y = make_uint4(0, 0, 0, 0);
-  if (c.place >= 0) {
-    const uint8_t* codes = c.which ? from.v : from.k;
-    const int64_t at = c.place * g.D + c.chan;
-    const float power = power_of((c.which ? from.vs : from.ks)[at / 32]);
-    if constexpr (BITS == 8) {
-      const uint2 u = *reinterpret_cast<const uint2*>(codes + at);
-      y = eight(u.x, u.y, power);
-    } else {
-      y = eight(*reinterpret_cast<const uint32_t*>(codes + at / 2), power);
-    }
+  g.D = D;
+  Chunk c[STEPS];
+  chunks_of(c, g, r, cu_q, kv_lens, pages);
+  uint2 u[STEPS];
+  uint8_t byte[STEPS];
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    u[i] = make_uint2(0, 0);
+    byte[i] = 127;
+    if (!c[i].ok || c[i].place < 0) continue;
+    const uint8_t* codes = c[i].which ? from.v : from.k;
+    const int64_t at = c[i].place * D + c[i].chan;
+    byte[i] = (c[i].which ? from.vs : from.ks)[at / 32];
+    if constexpr (BITS == 8)
+      u[i] = *reinterpret_cast<const uint2*>(codes + at);
+    else
+      u[i].x = *reinterpret_cast<const uint32_t*>(codes + at / 2);
   }
-  T* to = (c.which ? v + c.token * g.vs : k + c.token * g.ks) + c.head * g.D + c.chan;
-  if constexpr (sizeof(T) == 2) {
-    *reinterpret_cast<uint4*>(to) = y;
-  } else {  // a bf16 number is a float32 number's upper half
-    *reinterpret_cast<uint4*>(to) =
-        make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
-    *reinterpret_cast<uint4*>(to + 4) =
-        make_uint4(y.z << 16, y.z & 0xffff0000u, y.w << 16, y.w & 0xffff0000u);
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    if (!c[i].ok) continue;
+    const float power = power_of(byte[i]);
+    const uint4 y = BITS == 8 ? eight(u[i].x, u[i].y, power) : eight(u[i].x, power);
+    T* to = (c[i].which ? v + c[i].token * g.vs : k + c[i].token * g.ks) + c[i].head * D +
+            c[i].chan;
+    if constexpr (sizeof(T) == 2) {
+      *reinterpret_cast<uint4*>(to) = y;
+    } else {  // a bf16 number is a float32 number's upper half
+      *reinterpret_cast<uint4*>(to) =
+          make_uint4(y.x << 16, y.x & 0xffff0000u, y.y << 16, y.y & 0xffff0000u);
+      *reinterpret_cast<uint4*>(to + 4) =
+          make_uint4(y.z << 16, y.z & 0xffff0000u, y.w << 16, y.w & 0xffff0000u);
+    }
   }
 }
 
-int64_t row_blocks(const PagedGeometry& g, const Rows& r) {
-  const int64_t waves = ((int64_t)g.nq + r.tokens - 1) / r.tokens * r.waves;
-  return (waves + kThreads / 64 - 1) / (kThreads / 64);
+template <typename T, int D, int BITS>
+const void* append_fn(bool many) {
+  return many ? (const void*)&mx_append_kernel<T, D, BITS, kManySteps>
+              : (const void*)&mx_append_kernel<T, D, BITS, 1>;
+}
+template <typename T, int D, int BITS>
+const void* read_fn(bool many) {
+  return many ? (const void*)&mx_read_kernel<T, D, BITS, kManySteps>
+              : (const void*)&mx_read_kernel<T, D, BITS, 1>;
+}
+
+// How rows are dealt out: one step per wave where that fills the card no more than twice over
+// (4,096 waves), for the shortest chain.
+struct RowsPlan {
+  Rows r;
+  bool many;
+  int64_t blocks;
+};
+RowsPlan plan_rows(const PagedGeometry& g) {
+  RowsPlan p;
+  p.r.per = 2 * g.KH * (g.D / 8);
+  p.r.per_mul = 0;
+  divisor(p.r.per, &p.r.per_mul, &p.r.per_shift);
+  const int64_t steps = ((int64_t)g.nq * p.r.per + 63) / 64;
+  p.many = steps > 4096;
+  const int each = (p.many ? kManySteps : 1) * (kThreads / 64);
+  p.blocks = (steps + each - 1) / each;
+  return p;
+}
+
+// The form for the call's type, channels and bits.
+typedef const void* (*Form)(bool);
+Form form(const PagedGeometry& g, bool bf16, int bits, Form b64_8, Form b128_8, Form b64_4,
+          Form b128_4, Form f64_8, Form f128_8, Form f64_4, Form f128_4) {
+  const Form all[2][2][2] = {{{f64_4, f64_8}, {f128_4, f128_8}},
+                             {{b64_4, b64_8}, {b128_4, b128_8}}};
+  return all[bf16][g.D == 128][bits == 8];
 }
 
 MxPages pages_of(const dsa3d_mx_cache& c) { return {c.k, c.v, c.k_scales, c.v_scales}; }
@@ -864,8 +1007,15 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
   hipError_t e = seq_launch(fn, seq_blocks(g.tiles, 1), kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
-  if (e == hipSuccess && g.splits > 1)
-    e = launch_paged_join(g, sizeof(T) == 2, part_o, part_l, out, lse, s);
+  if (e == hipSuccess && g.splits > 1) {
+    constexpr int all = kThreads / 64;
+    const bool wide = g.splits > 8;
+    e = seq_launch(wide              ? (const void*)&mx_join_kernel<T, D, all, 8>
+                   : g.splits > 4    ? (const void*)&mx_join_kernel<T, D, 1, 4>
+                                     : (const void*)&mx_join_kernel<T, D, 1, 2>,
+                   wide ? rows : (rows + all - 1) / all, kThreads, 0, s, rows, g.splits,
+                   (const float*)part_o, (const float*)part_l, out, lse);
+  }
   return e;
 }
 
@@ -912,26 +1062,26 @@ hipError_t launch_paged_append_mx(const PagedGeometry& g, bool bf16, const void*
                                   const int32_t* pages, const dsa3d_mx_cache& cache,
                                   hipStream_t s) {
   if (g.nq == 0) return hipSuccess;
-  const Rows r = rows_of(g);
+  const RowsPlan p = plan_rows(g);
   const MxPages c = pages_of(cache);
-  const void* fn = bf16 ? (cache.bits == 8 ? (const void*)&mx_append_kernel<uint16_t, 8>
-                                           : (const void*)&mx_append_kernel<uint16_t, 4>)
-                        : (cache.bits == 8 ? (const void*)&mx_append_kernel<float, 8>
-                                           : (const void*)&mx_append_kernel<float, 4>);
-  return seq_launch(fn, row_blocks(g, r), kThreads, 0, s, g, r, k, v, cu_q, kv_lens, pages, c);
+  const void* fn = form(
+      g, bf16, cache.bits, append_fn<uint16_t, 64, 8>, append_fn<uint16_t, 128, 8>,
+      append_fn<uint16_t, 64, 4>, append_fn<uint16_t, 128, 4>, append_fn<float, 64, 8>,
+      append_fn<float, 128, 8>, append_fn<float, 64, 4>, append_fn<float, 128, 4>)(p.many);
+  return seq_launch(fn, p.blocks, kThreads, 0, s, g, p.r, k, v, cu_q, kv_lens, pages, c);
 }
 
 hipError_t launch_paged_read_mx(const PagedGeometry& g, bool bf16, const dsa3d_mx_cache& cache,
                                 const int32_t* pages, const int32_t* kv_lens, const int32_t* cu_q,
                                 void* k, void* v, hipStream_t s) {
   if (g.nq == 0) return hipSuccess;
-  const Rows r = rows_of(g);
+  const RowsPlan p = plan_rows(g);
   const MxPages c = pages_of(cache);
-  const void* fn = bf16 ? (cache.bits == 8 ? (const void*)&mx_read_kernel<uint16_t, 8>
-                                           : (const void*)&mx_read_kernel<uint16_t, 4>)
-                        : (cache.bits == 8 ? (const void*)&mx_read_kernel<float, 8>
-                                           : (const void*)&mx_read_kernel<float, 4>);
-  return seq_launch(fn, row_blocks(g, r), kThreads, 0, s, g, r, c, pages, kv_lens, cu_q, k, v);
+  const void* fn = form(
+      g, bf16, cache.bits, read_fn<uint16_t, 64, 8>, read_fn<uint16_t, 128, 8>,
+      read_fn<uint16_t, 64, 4>, read_fn<uint16_t, 128, 4>, read_fn<float, 64, 8>,
+      read_fn<float, 128, 8>, read_fn<float, 64, 4>, read_fn<float, 128, 4>)(p.many);
+  return seq_launch(fn, p.blocks, kThreads, 0, s, g, p.r, c, pages, kv_lens, cu_q, k, v);
 }
 
 }  // namespace dsa3d

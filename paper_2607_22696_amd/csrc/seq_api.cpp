@@ -248,16 +248,6 @@ struct PagedSizes {
   uint64_t q, out, pages, cache, cu, lens, lse, table, map;
 };
 
-// x / d as (x * mul) >> shift, exact for 0 <= x < 2^31: with 2^(s-1) < d <= 2^s and
-// mul = floor(2^(31+s) / d) + 1, the product exceeds x 2^(31+s) / d by at most x < 2^31 <=
-// 2^(31+s) / d, less than the step to the next whole quotient.
-void divisor(int d, uint32_t* mul, uint32_t* shift) {
-  int s = 0;
-  while ((1ll << s) < d) ++s;
-  *mul = d == 1 ? 1u : (uint32_t)((1ull << (31 + s)) / d + 1);
-  *shift = d == 1 ? 0 : 31 + s;
-}
-
 dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeometry* g,
                          PagedSizes* s, int (*set_plan)(dsa3d::PagedGeometry&) = dsa3d::set_plan) {
   if (d == nullptr) return DSA3D_ERR_NULL_POINTER;
@@ -298,8 +288,8 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
   g->page_size = d->page_size;
   g->max_pages = d->max_pages;
   g->max_kv = (int)std::min<int64_t>(most, 1 << 30);
-  divisor(g->page_size, &g->page_mul, &g->page_shift);
-  divisor(g->group, &g->group_mul, &g->group_shift);
+  dsa3d::divisor(g->page_size, &g->page_mul, &g->page_shift);
+  dsa3d::divisor(g->group, &g->group_mul, &g->group_shift);
   g->causal = d->causal;
   g->nb = append ? 0 : d->rel_buckets;
   g->rel_min = g->nb > 0 ? d->rel_min : 0;

@@ -68,6 +68,16 @@ hipError_t launch_seq_backward(const SeqGeometry& g, bool bf16, const SeqTensors
                                const void* dout, void* dq, void* dk, void* dv, float* d_table,
                                void* workspace, hipStream_t stream);
 
+// x / d as (x * mul) >> shift, exact for 0 <= x < 2^31: with 2^(s-1) < d <= 2^s and
+// mul = floor(2^(31+s) / d) + 1, the product exceeds x 2^(31+s) / d by at most x < 2^31 <=
+// 2^(31+s) / d, less than the step to the next whole quotient.
+inline void divisor(int d, uint32_t* mul, uint32_t* shift) {
+  int s = 0;
+  while ((1ll << s) < d) ++s;
+  *mul = d == 1 ? 1u : (uint32_t)((1ull << (31 + s)) / d + 1);
+  *shift = d == 1 ? 0 : 31 + s;
+}
+
 struct PagedGeometry {
   int B, nq;
   int H, KH, group, D;
@@ -93,9 +103,6 @@ hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q
                                 const int32_t* kv_lens, const int32_t* cu_q, const float* table,
                                 const int32_t* map, void* out, float* lse, void* workspace,
                                 hipStream_t stream);
-// Joins the parts of each row that the workspace holds (log-sum-exps, then results).
-hipError_t launch_paged_join(const PagedGeometry& g, bool bf16, const float* part_o,
-                             const float* part_l, void* out, float* lse, hipStream_t stream);
 hipError_t launch_paged_append(const PagedGeometry& g, bool bf16, const void* k, const void* v,
                                const int32_t* cu_q, const int32_t* kv_lens, const int32_t* pages,
                                void* k_pages, void* v_pages, hipStream_t stream);

@@ -664,6 +664,29 @@ def paged_cache_mx(num_pages, page_size, kv_heads, head_dim, bits=8, device="cud
 def _cache_mx(chk, cache, pages, kv_lens, cu_q, device):
     """Checks the cache; returns (cache of the library, requests, num_pages, page_size, kv_heads,
     head_dim, columns)."""
+    try:  # all in order: the checks below take 5 us, as much as a launch
+        k, v, k_scales, v_scales = cache
+        shape, scales, batch = k.shape, k_scales.shape, kv_lens.shape[0]
+        num, heads, size, wide = shape
+        D = scales[3] * _MX_BLOCK
+        bits = 4 if 2 * wide == D else 8
+        u8, i32 = torch.uint8, torch.int32
+        if wide * 8 == D * bits and v.shape == shape and v_scales.shape == scales and \
+                len(scales) == 4 and scales[:3] == shape[:3] and k.dtype is u8 and v.dtype is u8 and \
+                k_scales.dtype is u8 and v_scales.dtype is u8 and k.device == device and \
+                v.device == device and k_scales.device == device and \
+                v_scales.device == device and k.is_contiguous() and v.is_contiguous() and \
+                k_scales.is_contiguous() and v_scales.is_contiguous() and batch >= 1 and \
+                kv_lens.dim() == 1 and cu_q.shape == (batch + 1,) and pages.dim() == 2 and \
+                pages.shape[0] == batch and kv_lens.dtype is i32 and cu_q.dtype is i32 and \
+                pages.dtype is i32 and kv_lens.device == device and cu_q.device == device and \
+                pages.device == device and kv_lens.is_contiguous() and \
+                cu_q.is_contiguous() and pages.is_contiguous():
+            held = make_mx_cache(k.data_ptr(), v.data_ptr(), k_scales.data_ptr(),
+                                 v_scales.data_ptr(), bits)
+            return held, batch, num, size, heads, D, pages.shape[1]
+    except (AttributeError, IndexError, TypeError, ValueError):
+        pass
     if not isinstance(cache, (tuple, list)) or len(cache) != 4 or \
             not all(isinstance(t, torch.Tensor) and t.dim() == 4 for t in cache):
         chk.problems.append("cache: expected (k, v, k_scales, v_scales), uint8 tensors "
@@ -735,9 +758,9 @@ def paged_read_mx(cache, pages, kv_lens, cu_q, rows, dtype=torch.bfloat16, k=Non
     desc = make_paged_desc(batch, rows, heads, heads, D, num, size, columns,
                            dtype=_IO_DTYPES[dtype], k_stride=ks, v_stride=vs)
     if k is None:
-        k = torch.empty(rows, heads, D, dtype=dtype, device=dev)
+        k = torch.empty((rows, heads, D), dtype=dtype, device=dev)
     if v is None:
-        v = torch.empty(rows, heads, D, dtype=dtype, device=dev)
+        v = torch.empty((rows, heads, D), dtype=dtype, device=dev)
     _launch(dev, dsa3d_paged_read_mx, desc, held, pages, kv_lens, cu_q, k, v)
     return k, v
 
