@@ -70,11 +70,6 @@ struct Piece {
     else
       scales = *scale_at;
   }
-  __device__ inline void clear(bool none) {  // zeros where there is no such key
-#pragma unroll
-    for (int i = 0; i < W; ++i) w[i] = none ? 0u : w[i];
-    scales = none ? (decltype(scales))0x7f7f : scales;
-  }
   __device__ inline float power(int chunk) const {
     if constexpr (kBlocks == 1) return power_of(scales);
     return power_of(scales >> (8 * (chunk / 4)) & 255u);
@@ -114,15 +109,6 @@ __device__ inline void fence_wave() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// Place of key j of the span's request among the rows of all pages of one head: -1 if none.
-__device__ inline int64_t place_of_key(const PagedGeometry& g, const int32_t* pages, int b, int u,
-                                       int j) {
-  const int page = div_by((uint32_t)j, g.page_mul, g.page_shift);
-  const int p = pages[(int64_t)b * g.max_pages + page];
-  if (p < 0 || p >= g.num_pages) return -1;
-  return ((int64_t)p * g.KH + u) * g.page_size + (j - page * g.page_size);
-}
-
 // The workgroup's key head, tile and part.  A part of a head's keys stays on one XCD, whose L2 then
 // serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
 // four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, LONG us
@@ -136,8 +122,45 @@ __device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split)
 
 // ------------------------------------------------------------------------- many rows
 
+// alpha's operand: 16 bits of it, as two bf16 numbers, or a float32's three parts.
+struct Two {
+  bf16x8_t h, l;
+};
+__device__ inline f32x16_t times(const bf16x8_t& a, const Two& b, f32x16_t c) {
+  c = mfma(a, b.l, c);
+  return mfma(a, b.h, c);
+}
+template <typename T>
+struct Alpha;
+template <>
+struct Alpha<uint16_t> {
+  using Frag = Two;
+  static __device__ inline Two of(const float* x) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y[2] = {x[2 * i], x[2 * i + 1]};
+      h[i] = take_part(y);
+      l[i] = take_part(y);
+    }
+    return {as_bf16x8(make_uint4(h[0], h[1], h[2], h[3])),
+            as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]))};
+  }
+};
+template <>
+struct Alpha<float> {
+  using Frag = Split;
+  static __device__ inline Split of(const float* x) {
+    F32x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y.x[e] = x[e];
+    return seq::split(y);
+  }
+};
+
 // 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
-// elements are loaded while the one before it is multiplied, converted once for all four waves.
+// elements are loaded two tiles ahead, converted once for all four waves, and the products of the
+// next 32 keys run beside the softmax of these.
 template <typename T, int D, int BITS, bool BIAS>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
@@ -150,7 +173,8 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   constexpr int KT = 64, RB = D * BITS / 8, SB = D / 32;
   using Tl = Tile<uint16_t, D, KT>;
   using Frag = typename Type<T>::Frag;
-  using Quarter = Piece<BITS, RB / 16>;  // four threads share a key
+  using AFrag = typename Alpha<T>::Frag;
+  using Quarter = Piece<BITS, RB / 16>;  // four lanes share a key
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
   __shared__ __attribute__((aligned(16))) uint16_t lds[4 * E];  // keys, values; twice
   __shared__ __attribute__((aligned(8))) uint16_t there[2][4];
@@ -162,20 +186,34 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   Span1 s;
   if (!locate<kManyRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
-  const int key = threadIdx.x / 4, part = threadIdx.x % 4;
-  // the place of this thread's key of a tile; keys past the last repeat it, to be masked
-  auto place = [&](int kt) {
-    return place_of_key(g, pages, s.b, w.u, min(s.k_lo + kt * KT + key, s.k_hi - 1));
+  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
+  const int rw = s.r0 + wave * 32;
+  const bool live = rw < s.rows;
+  const Row x = row_of(g, s, w.u, rw + (lane & 31));
+  Frag qf[KS];
+  load_frag<T, D>(qf, q + x.q_at, x.ok);
+
+  // A wave has 16 keys of a tile, a quarter of the channels per lane: 16 lanes write one chunk of 16
+  // rows to LDS, which meet in no bank.  Keys past the last repeat it, to be masked; one without a
+  // place has the first page's first row, to be cleared.
+  const int key = wave * 16 + (lane & 15), part = lane >> 4;
+  const int32_t* my_pages = pages + (int64_t)s.b * g.max_pages;
+  auto key_of = [&](int kt) { return min(s.k_lo + kt * KT + key, s.k_hi - 1); };
+  auto page_of = [&](int kt) {
+    return my_pages[div_by((uint32_t)key_of(kt), g.page_mul, g.page_shift)];
   };
   Quarter kq, vq;
-  auto load = [&](int64_t row) {
-    const int64_t r = max(row, (int64_t)0), at = r * RB + part * (RB / 4),
-                  sc = r * SB + part * SB / 4;
+  auto load = [&](int kt, int p) {  // returns which of the wave's keys have a place
+    const int j = key_of(kt), page = div_by((uint32_t)j, g.page_mul, g.page_shift);
+    const bool ok = (uint32_t)p < (uint32_t)g.num_pages;
+    const int64_t row =
+        ok ? ((int64_t)p * g.KH + w.u) * g.page_size + (j - page * g.page_size) : 0;
+    const int64_t at = row * RB + part * (RB / 4), sc = row * SB + part * SB / 4;
     kq.load(c.k + at, c.ks + sc);
     vq.load(c.v + at, c.vs + sc);
+    return (uint32_t)__ballot(ok) & 0xffffu;
   };
-  auto put = [&](int64_t row, int buf) {
-    if (__any(row < 0)) vq.clear(row < 0);
+  auto put = [&](uint32_t ok, int buf) {
     uint16_t* to = lds + 2 * E * buf;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
@@ -183,87 +221,112 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       *reinterpret_cast<uint4*>(to + at) = kq.eight_at(i);
       *reinterpret_cast<uint4*>(to + E + at) = vq.eight_at(i);
     }
-    const uint64_t ok = __ballot(row >= 0);  // the same four times for each key
-    if ((threadIdx.x & 63) == 0) {
-      uint32_t bits = 0;
+    if (ok != 0xffffu && (ok >> (lane & 15) & 1) == 0) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) bits |= (uint32_t)(ok >> (4 * i) & 1) << i;
-      there[buf][wave_id()] = (uint16_t)bits;
+      for (int i = 0; i < D / 32; ++i)
+        *reinterpret_cast<uint4*>(to + E + Tl::at(key, part * (D / 4) + 8 * i)) =
+            make_uint4(0, 0, 0, 0);
     }
+    if (lane == 0) there[buf][wave] = (uint16_t)ok;
   };
-  int64_t row0 = 0, row1 = 0;
+  uint32_t ok1 = 0;  // of the tile in kq and vq
+  int next_page = 0;
   if (ntiles > 0) {
-    row0 = place(0);
-    load(row0);
-    if (ntiles > 1) row1 = place(1);
+    const uint32_t ok0 = load(0, page_of(0));
+    const int page1 = page_of(1);
+    put(ok0, 0);
+    ok1 = load(1, page1);
+    next_page = page_of(2);
   }
   if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
 
-  const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
-  const int rw = s.r0 + wave * 32;
-  const bool live = rw < s.rows;
-  const Row x = row_of(g, s, w.u, rw + (lane & 31));
-  Frag qf[KS];
-  load_frag<T, D>(qf, q + x.q_at, x.ok);
   const int pos = s.off + x.i;
-  const int last = g.causal ? min(s.seen - 1, pos) : s.seen - 1;
-  int wave_last = live ? s.seen - 1 : -1, all_see = s.seen - 1;
-  if (live && g.causal) {
-    all_see = min(all_see, s.off + div_by(rw, g.group_mul, g.group_shift));
-    wave_last = min(wave_last, s.off + div_by(min(rw + 31, s.rows - 1), g.group_mul,
-                                              g.group_shift));
-  }
-
+  const int last = min(g.causal ? min(s.seen - 1, pos) : s.seen - 1, s.k_hi - 1);
+  const int all_see =
+      min(g.causal ? min(s.seen - 1, s.off + div_by(rw, g.group_mul, g.group_shift))
+                   : s.seen - 1, s.k_hi - 1);
   f32x16_t o[DB];
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
   Softmax sm;
   const float scale = BIAS ? 1.0f : g.scale_log2;
-  if (ntiles > 0) put(row0, 0);
-  if (ntiles > 1) load(row1);
+  auto products = [&](const uint16_t* kc, int b) {
+    f32x16_t acc = f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) acc = times(Tl::a_rows(kc, b * 32, ks), qf[ks], acc);
+    return acc;
+  };
+  auto mask = [&](float (&y)[16], int kb, uint32_t bits) {
+    if constexpr (BIAS) add_bias(y, g, bias, x.head - w.u * g.group, kb, pos);
+    if (bits != ~0u || kb + 31 > all_see) {
+      asm volatile("");  // a branch: blocks that every row sees do not pay for it
+      const int seen = last - kb - 4 * hh;
+      const uint32_t mine = bits >> (4 * hh);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (c_row(i, 0) > seen || (mine >> c_row(i, 0) & 1) == 0) y[i] = -INFINITY;
+    }
+  };
+  auto accumulate = [&](const uint16_t* vc, int b, const float (&y)[16]) {
+    const AFrag pf[2] = {Alpha<T>::of(y), Alpha<T>::of(y + 8)};
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        o[db] = times(Tl::a_cols(vc, db * 32, b, p), pf[p], o[db]);
+  };
   __syncthreads();
-  for (int kt = 0; kt < ntiles; ++kt) {
-    const int buf = kt & 1;
-    const int64_t row2 = kt + 2 < ntiles ? place(kt + 2) : 0;
-    const uint16_t *kc = lds + 2 * E * buf, *vc = kc + E;
-    const int kbase = s.k_lo + kt * KT;
-    const uint2 m = *reinterpret_cast<const uint2*>(there[buf]);
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int kb = kbase + b * 32;
-      const uint32_t bits = __builtin_amdgcn_readfirstlane(b == 0 ? m.x : m.y);
-      if (bits == 0 || min(wave_last, s.k_hi - 1) < kb) continue;
-      f32x16_t acc = f32x16_t{};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) acc = times(Tl::a_rows(kc, b * 32, ks), qf[ks], acc);
-      float y[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) y[i] = acc[i];
-      if constexpr (BIAS) add_bias(y, g, bias, x.head - w.u * g.group, kb, pos);
-      if (bits != ~0u || kb + 31 > min(all_see, s.k_hi - 1)) {
-        asm volatile("");  // a branch: blocks that every row sees do not pay for it
-        const int seen = min(last, s.k_hi - 1) - kb - 4 * hh;
-        const uint32_t mine = bits >> (4 * hh);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (c_row(i, 0) > seen || (mine >> c_row(i, 0) & 1) == 0) y[i] = -INFINITY;
+  // All tiles; LIVE: the wave has rows, else it only converts its share of them.  MORE: another
+  // tile follows, which is converted first and whose first products end this one.
+  auto run = [&](auto live_wave) {
+    constexpr bool LIVE = decltype(live_wave)::value;
+    f32x16_t next;
+    if constexpr (LIVE) next = products(lds, 0);
+    auto tile = [&](int kt, int buf, auto more) {
+      constexpr bool MORE = decltype(more)::value;
+      const uint16_t *kc = lds + 2 * E * buf, *kn = lds + 2 * E * (1 - buf);
+      const uint2 bits = *reinterpret_cast<const uint2*>(there[buf]);
+      if constexpr (MORE) {
+        put(ok1, 1 - buf);
+        __builtin_amdgcn_sched_barrier(0);  // the same registers, as in mx_keys_kernel
+        ok1 = load(kt + 2, next_page);
+        next_page = page_of(kt + 3);
       }
-      sm.raise_to(y, scale, o);
-      sm.weigh(y, scale);
-      Frag pf[2];
-      to_frags(y, pf);
 #pragma unroll
-      for (int p = 0; p < 2; ++p)
+      for (int b = 0; b < NB; ++b) {
+        float y[16];
+        if constexpr (LIVE) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          o[db] = times(Tl::a_cols(vc, db * 32, b, p), pf[p], o[db]);
+          for (int i = 0; i < 16; ++i) y[i] = next[i];
+          mask(y, s.k_lo + kt * KT + b * 32,
+               __builtin_amdgcn_readfirstlane(b == 0 ? bits.x : bits.y));
+          sm.raise_to(y, scale, o);
+        }
+        if (MORE && b == NB - 1) __syncthreads();  // the next tile is in LDS
+        if constexpr (LIVE) {
+          if constexpr (MORE) next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
+          else if (b + 1 < NB) next = products(kc, b + 1);
+          sm.weigh(y, scale);
+          accumulate(kc + E, b, y);
+        }
+      }
+      if constexpr (MORE) __syncthreads();  // and this one is free
+    };
+    int kt = 0;
+    for (; kt + 2 < ntiles; kt += 2) {
+      tile(kt, 0, std::true_type());
+      tile(kt + 1, 1, std::true_type());
     }
     if (kt + 1 < ntiles) {
-      put(row1, 1 - buf);
-      row1 = row2;
-      if (kt + 2 < ntiles) load(row1);
+      tile(kt, 0, std::true_type());
+      tile(kt + 1, 1, std::false_type());
+    } else {
+      tile(kt, 0, std::false_type());
     }
-    __syncthreads();
+  };
+  if (ntiles > 0) {
+    if (live) run(std::true_type());
+    else run(std::false_type());
   }
   const float ltot = pair_sum(sm.l);
   const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;
@@ -294,10 +357,6 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 __device__ inline f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-// alpha as two bf16 numbers: 16 bits of it.
-struct Two {
-  bf16x8_t h, l;
-};
 __device__ inline f32x4_t times(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return mfma16(a, b, c);
 }
@@ -310,34 +369,6 @@ __device__ inline f32x4_t times(const bf16x8_t& a, const Split& b, f32x4_t c) {
   c = mfma16(a, b.m, c);
   return mfma16(a, b.h, c);
 }
-template <typename T>
-struct Alpha;
-template <>
-struct Alpha<uint16_t> {
-  using Frag = Two;
-  static __device__ inline Two of(const float (&x)[8]) {
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[2] = {x[2 * i], x[2 * i + 1]};
-      h[i] = take_part(y);
-      l[i] = take_part(y);
-    }
-    return {as_bf16x8(make_uint4(h[0], h[1], h[2], h[3])),
-            as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]))};
-  }
-};
-template <>
-struct Alpha<float> {
-  using Frag = Split;
-  static __device__ inline Split of(const float (&x)[8]) {
-    F32x8 y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y.x[e] = x[e];
-    return seq::split(y);
-  }
-};
-
 // x of the lanes 16 s .. 16 s + 15 in all four quarters, s = 0 .. 3.
 __device__ inline void quarters(uint32_t x, uint32_t (&y)[4]) {
   const auto half = __builtin_amdgcn_permlane32_swap(x, x, false, false);
