@@ -502,7 +502,7 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
                   : (const void*)&paged_keys_kernel<T, D, false>)
           : (bias ? (const void*)&paged_rows_kernel<T, D, true>
                   : (const void*)&paged_rows_kernel<T, D, false>);
-  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, g.splits), kThreads,
+  hipError_t e = seq_launch(fn, g.blocks, kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, k, v, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1) {
@@ -515,13 +515,14 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const T* k, const T* v,
 
 }  // namespace
 
-int set_plan(PagedGeometry& g) {
+void set_plan(PagedGeometry& g) {
   const PagedPlan p = paged_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = p.part;
   g.tiles = seq_spread(g.KH, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
-  return g.splits;
+  g.blocks = seq_blocks(g.tiles, g.splits);
+  g.target = 0;
 }
 
 size_t paged_workspace(const PagedGeometry& g) {

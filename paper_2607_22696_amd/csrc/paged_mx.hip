@@ -451,6 +451,89 @@ __device__ inline bf16x8_t value_cols(const uint16_t* lds, int d0) {
   return as_bf16x8(make_uint4(ul.x, ul.y, uh.x, uh.y));
 }
 
+// What a workgroup of the form with few rows works on.
+struct Deal {
+  Span1 s;
+  int u, split, parts;  // key head; part of how many (all the workspace has where not dealt out)
+};
+
+// Up to 64 requests: a lane holds each, with one load of its offsets and length, and the parts of
+// their keys go by the sum of all lengths.  Longer parts come first (four classes), so that what is
+// dealt out last is short.
+template <int ROWS>
+__device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
+                            Deal& d) {
+  Span1& s = d.s;
+  if (g.target == 0) {
+    Work w;
+    if (!work_of_part(g, w, d.split)) return false;
+    d.u = w.u;
+    d.parts = g.splits;
+    return locate<ROWS>(g, cu_q, kv_lens, w.slot, d.split, s);
+  }
+  constexpr int STEP = 256;  // keys of the four waves' groups
+  const int block = block_number(), index = block / g.KH;
+  d.u = block - index * g.KH;
+  const int lane = threadIdx.x & 63, b = min(lane, g.B - 1);
+  const int raw = cu_q[b], raw_next = cu_q[b + 1], raw_m = kv_lens[b];  // three loads at once
+  const int begin = b == 0 ? 0 : min(max(raw, 0), g.nq), end = min(max(raw_next, 0), g.nq);
+  const int n = lane < g.B ? max(end - begin, 0) : 0, m = max(raw_m, 0);
+  const int keys = n > 0 ? min(m, g.max_kv) : 0;
+  const int tiles = (n * g.group + ROWS - 1) / ROWS;
+  float all = (float)tiles * (float)keys;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) all += __shfl_xor(all, x);
+  const float share = fminf(all / (float)g.target, (float)(1 << 30));
+  const int most = max(((int)share + STEP) / STEP * STEP, g.part);  // more than a share
+  const int parts = min(max((keys + most - 1) / most, 1), g.splits);
+  const int len = ((keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
+  const int count = tiles * parts;
+  const int size = min((int)((int64_t)len * 4 / (most + 1)), 3);  // the longest: 3
+  int start = 0, before = 0;
+#pragma unroll
+  for (int c = 3; c >= 0; --c) {
+    const int sum = prefix_sum(size == c ? count : 0);
+    if (size == c) start = before + sum - count;
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  const uint64_t who = __ballot(index >= start && index < start + count);
+  int r, tile;
+  if (who == 0) {  // rows behind the last request, which see nothing
+    s.b = g.B;
+    s.begin = __builtin_amdgcn_readlane(end, g.B - 1);
+    s.n = g.nq - s.begin;
+    s.m = 0;
+    d.parts = 1;
+    d.split = 0;
+    r = 0;
+    tile = index - before;
+    if (tile >= (s.n * g.group + ROWS - 1) / ROWS) return false;
+  } else {
+    const int l = __builtin_ctzll(who);
+    s.b = l;
+    s.begin = __builtin_amdgcn_readlane(begin, l);
+    s.n = __builtin_amdgcn_readlane(n, l);
+    s.m = __builtin_amdgcn_readlane(m, l);
+    d.parts = __builtin_amdgcn_readlane(parts, l);
+    r = index - __builtin_amdgcn_readlane(start, l);
+    tile = r / d.parts;
+    d.split = r - tile * d.parts;
+  }
+  const int part = who == 0 ? 0 : __builtin_amdgcn_readlane(len, __builtin_ctzll(who));
+  s.rows = s.n * g.group;
+  s.r0 = tile * ROWS;
+  s.off = s.m - s.n;
+  s.seen = min(s.m, g.max_kv);
+  int hi = s.seen;
+  if (g.causal)
+    hi = min(hi, s.off + div_by(min(s.r0 + ROWS, s.rows) - 1, g.group_mul, g.group_shift) + 1);
+  hi = max(hi, 0);
+  s.k_lo = min((int64_t)d.split * part, (int64_t)hi);
+  s.k_hi = min((int64_t)hi, (int64_t)s.k_lo + part);
+  s.only = d.parts == 1;
+  return true;
+}
+
 // 16 RT rows per workgroup; its waves share out the keys in groups of 64 and read them each for
 // itself, without a barrier until the end.  Half a group at a time, lane l has a quarter of the
 // channels of keys l % 16 and 16 + l % 16, which is the keys' operand (the contraction's order is
@@ -476,11 +559,10 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS];
   extern __shared__ float bias[];
 
-  Work w;
-  int split;
-  if (!work_of_part(g, w, split)) return;
-  Span1 s;
-  if (!locate<ROWS>(g, cu_q, kv_lens, w.slot, split, s)) return;
+  Deal w;
+  if (!deal<ROWS>(g, cu_q, kv_lens, w)) return;
+  const Span1& s = w.s;
+  const int split = w.split;
   const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
   // Queries first, so that waiting for them does not wait for keys.  A column without a row has the
   // request's first one, and is never stored.
@@ -676,6 +758,14 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   }
 
   // The waves' sums join over a common maximum, 16 rows at a time.
+  const int count = min(s.rows - s.r0, ROWS);
+  if (!s.only && split == 0 && w.parts < g.splits) {  // parts that there are none of
+    const int none = g.splits - w.parts;
+    for (int e = threadIdx.x; e < count * none; e += kThreads) {
+      const int r = e / none;
+      part_l[row_of(g, s, w.u, s.r0 + r).out_at * g.splits + w.parts + (e - r * none)] = -INFINITY;
+    }
+  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float total = sum_of(sum[rt]);
@@ -691,7 +781,6 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     for (int i = 1; i < WAVES; ++i) y = fmaxf(y, tops[i][r]);
     return y;
   };
-  const int count = min(s.rows - s.r0, ROWS);
   float* sums = reinterpret_cast<float*>(lds);
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -745,9 +834,9 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 // ------------------------------------------------------------------------- join
 
 // Joins the parts of each row, weights 2^(l - max l), as paged_join_kernel does, but for many parts
-// with W waves per row, each with its share of the parts, and every load on its way before the
-// first is waited for (64 rows of 63 parts: 12.6 us with one wave and loads behind a branch, 4.0
-// so).  A part without keys has -inf, and its results were never written.
+// with W waves per row, of which wave w has the parts w, w + W, ..., and with several loads on their
+// way before the first is waited for (64 rows of 63 parts: 12.6 us with one wave and loads behind
+// a branch, 4.0 so).  A part without keys has -inf, and its results were never written.
 template <typename T, int D, int W, int AT_ONCE>
 __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int splits,
                                                            const float* __restrict__ part_o,
@@ -755,34 +844,44 @@ __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int spl
                                                            T* __restrict__ out,
                                                            float* __restrict__ lse) {
   constexpr int LANES = D / 4, SIDES = 64 / LANES, PER = kThreads / 64 / W;
-  __shared__ float4 sums[W == 1 ? 1 : W][LANES];
-  const int wave = wave_id(), lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)block_number() * PER + wave / W;
-  if (row >= rows) return;
-  const int nth = wave % W * SIDES + lane / LANES, c = lane % LANES * 4;
-  // every wave has all log-sum-exps, a part per lane (at most 64)
-  const float mine = lane < splits ? part_l[row * splits + lane] : -INFINITY;
-  if (__shfl(mine, 0) == kDone) return;
+  __shared__ float4 sums[W][LANES];
+  __shared__ float tops[W], totals[W];
+  const int wave = wave_id() % W, lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)block_number() * PER + wave_id() / W;
+  if (row >= rows) return;  // a whole workgroup where W > 1
+  const int side = lane / LANES, c = lane % LANES * 4;
+  // lane l has part l W + wave
+  const float mine = lane * W + wave < splits ? part_l[row * splits + lane * W + wave] : -INFINITY;
+  if (part_l[row * splits] == kDone) return;
   float top = mine;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if constexpr (W > 1) {
+    tops[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) top = fmaxf(top, tops[i]);
+  }
   const float weight = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
   float total = weight;
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  // this wave's parts up to its last that is there
+  const uint64_t some = __ballot(mine != -INFINITY);
+  const int count = some == 0 ? 0 : 64 - __builtin_clzll(some);
   float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = 0; s0 < splits; s0 += AT_ONCE * SIDES * W) {
+  for (int s0 = 0; s0 < count; s0 += AT_ONCE * SIDES) {
     float4 x[AT_ONCE];
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      const int s = min(s0 + i * SIDES * W + nth, splits - 1);
+      const int s = min(s0 + i * SIDES + side, count - 1) * W + wave;
       x[i] = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
     }
 #pragma unroll
     for (int i = 0; i < AT_ONCE; ++i) {
-      const int s = s0 + i * SIDES * W + nth;
+      const int s = s0 + i * SIDES + side;
       const float ws = __shfl(weight, s & 63), ls = __shfl(mine, s & 63);
-      if (s < splits && ls != -INFINITY) {
+      if (s < count && ls != -INFINITY) {
         sum.x = fmaf(ws, x[i].x, sum.x);
         sum.y = fmaf(ws, x[i].y, sum.y);
         sum.z = fmaf(ws, x[i].z, sum.z);
@@ -797,8 +896,9 @@ __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int spl
     sum.z += __shfl_xor(sum.z, d);
     sum.w += __shfl_xor(sum.w, d);
   }
-  if constexpr (W > 1) {  // a workgroup is one row
+  if constexpr (W > 1) {
     if (lane < LANES) sums[wave][lane] = sum;
+    totals[wave] = total;
     __syncthreads();
     if (wave > 0 || lane >= LANES) return;
     sum = sums[0][lane];
@@ -809,6 +909,7 @@ __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int spl
       sum.y += y.y;
       sum.z += y.z;
       sum.w += y.w;
+      total += totals[i];
     }
   }
   if (lane >= LANES) return;
@@ -1066,12 +1167,12 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
                                           : (const void*)&mx_keys_kernel<T, D, BITS, false, 2>)
                                   : (bias ? (const void*)&mx_rows_kernel<T, D, BITS, true>
                                           : (const void*)&mx_rows_kernel<T, D, BITS, false>);
-  hipError_t e = seq_launch(fn, seq_blocks(g.tiles, 1), kThreads,
+  hipError_t e = seq_launch(fn, g.blocks, kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1) {
     constexpr int all = kThreads / 64;
-    const bool wide = g.splits > 8;
+    const bool wide = g.splits > 8;  // more than 64 parts only where the rows are few
     e = seq_launch(wide              ? (const void*)&mx_join_kernel<T, D, all, 8>
                    : g.splits > 4    ? (const void*)&mx_join_kernel<T, D, 1, 4>
                                      : (const void*)&mx_join_kernel<T, D, 1, 2>,
@@ -1100,13 +1201,19 @@ hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache
 
 }  // namespace
 
-int set_plan_mx(PagedGeometry& g) {
-  const PagedPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
+void set_plan_mx(PagedGeometry& g, int bits) {
+  const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv, 3);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = p.part;
-  g.tiles = seq_spread(g.KH * g.splits, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
-  return 1;
+  g.target = p.target;
+  if (p.target > 0) {
+    g.tiles = Spread{};
+    g.blocks = g.KH * p.bound;
+  } else {
+    g.tiles = seq_spread(g.KH * g.splits, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
+    g.blocks = seq_blocks(g.tiles, 1);
+  }
 }
 
 hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,

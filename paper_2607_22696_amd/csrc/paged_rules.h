@@ -55,10 +55,35 @@ inline PagedPlan paged_plan(int64_t tokens, int group, int kv_heads, int batch, 
   return p;
 }
 
-// The same over a cache of 8 or 4 bits, whose form with few rows has 16 or 32 of them.
-inline PagedPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv) {
-  PagedPlan p = paged_plan(tokens, group, kv_heads, batch, max_kv);
+// The same over a cache of 8 or 4 bits.
+constexpr int kDealt = 64;        // requests that a wave holds a lane each
+constexpr int kMostPartsMx = 256;
+constexpr int kLeastPartMx = 512;
+
+struct MxPlan {
+  int tile;          // 16, 32 or 128 rows per workgroup
+  int splits, part;  // most parts of a tile's keys, and least keys of a part
+  int target;        // > 0: parts go by the lengths that the GPU sees, about this many per key head
+  int64_t bound;     // and are at most this many per key head
+};
+
+// Few rows: up to 64 requests' keys are divided on the GPU, by all their lengths, into parts as
+// long as the work that `waves` workgroups per compute unit have each; more requests fill the card
+// without.
+inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv,
+                            int per_cu) {
+  const PagedPlan q = paged_plan(tokens, group, kv_heads, batch, max_kv);
+  MxPlan p = {q.tile, q.splits, q.part, 0, 0};
+  if (q.tile != kFewRows) return p;
   if (tokens * group <= (int64_t)16 * batch) p.tile = 16;
+  if (batch > kDealt) return p;
+  p.part = kLeastPartMx;
+  p.target = std::max(1, per_cu * 256 / kv_heads);
+  const int64_t slots = tokens * group / p.tile + batch + 1;
+  p.splits = (int)std::max<int64_t>(
+      1, std::min<int64_t>({max_kv / p.part, p.target + 1, kMostPartsMx}));
+  // sum of ceil(keys / part) <= target + one per tile; 8 for the rounding of the GPU's sum
+  p.bound = std::min<int64_t>(slots * p.splits, slots + p.target + 8);
   return p;
 }
 

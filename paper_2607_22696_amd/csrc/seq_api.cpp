@@ -248,8 +248,9 @@ struct PagedSizes {
   uint64_t q, out, pages, cache, cu, lens, lse, table, map;
 };
 
+// `bits`: of the cache, 0 where it has the descriptor's type.
 dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeometry* g,
-                         PagedSizes* s, int (*set_plan)(dsa3d::PagedGeometry&) = dsa3d::set_plan) {
+                         PagedSizes* s, int bits = 0) {
   if (d == nullptr) return DSA3D_ERR_NULL_POINTER;
   if (d->batch < 1 || d->batch >= (1 << 24) || d->total_q < 0 || d->num_pages < 0 ||
       d->page_size < 1 || d->max_pages < 0 || d->max_kv < 0 ||
@@ -298,8 +299,9 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     return DSA3D_ERR_UNSUPPORTED;
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
-  const int per = set_plan(*g);
-  if (!append && dsa3d::seq_blocks(g->tiles, per) > dsa3d::kMostBlocks)
+  if (bits == 0) dsa3d::set_plan(*g);
+  else dsa3d::set_plan_mx(*g, bits);
+  if (!append && g->blocks > dsa3d::kMostBlocks)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
   s->out = (uint64_t)d->total_q * qrow * s->item;
@@ -395,20 +397,21 @@ dsa3d_status dsa3d_paged_forward(const dsa3d_paged_desc* desc, const void* q, co
 
 namespace {
 
-// The cache's sizes in bytes instead of those of bf16 or float32 pages.
-struct MxSizes {
+struct MxSizes {  // the cache's bytes, instead of PagedSizes::cache
   uint64_t codes, scales;
 };
 
-dsa3d_status check_bits(int32_t bits) {
-  return bits == 8 || bits == 4 ? DSA3D_OK : DSA3D_ERR_UNSUPPORTED;
+dsa3d_status check_mx(const dsa3d_paged_desc* d, int32_t bits, bool rows,
+                      dsa3d::PagedGeometry* g, PagedSizes* s) {
+  const bool known = bits == 8 || bits == 4;
+  const dsa3d_status st = check_paged(d, rows, g, s, known ? bits : 8);
+  return st == DSA3D_OK && !known ? DSA3D_ERR_UNSUPPORTED : st;
 }
 
 dsa3d_status check_cache(const dsa3d_paged_desc* d, const dsa3d_mx_cache* c, bool rows,
                          dsa3d::PagedGeometry* g, PagedSizes* s, MxSizes* m) {
   if (c == nullptr) return DSA3D_ERR_NULL_POINTER;
-  dsa3d_status st = check_paged(d, rows, g, s, dsa3d::set_plan_mx);
-  if (st == DSA3D_OK) st = check_bits(c->bits);
+  const dsa3d_status st = check_mx(d, c->bits, rows, g, s);
   if (st != DSA3D_OK) return st;
   const uint64_t held = (uint64_t)g->num_pages * g->page_size * g->KH;
   m->codes = held * (g->D * c->bits / 8);
@@ -491,9 +494,7 @@ dsa3d_status dsa3d_paged_read_mx(const dsa3d_paged_desc* desc, const dsa3d_mx_ca
 size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32_t bits) {
   dsa3d::PagedGeometry g;
   PagedSizes s;
-  if (check_paged(desc, false, &g, &s, dsa3d::set_plan_mx) != DSA3D_OK ||
-      check_bits(bits) != DSA3D_OK)
-    return 0;
+  if (check_mx(desc, bits, false, &g, &s) != DSA3D_OK) return 0;
   return dsa3d::paged_workspace(g);
 }
 

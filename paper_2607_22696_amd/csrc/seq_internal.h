@@ -92,11 +92,12 @@ struct PagedGeometry {
   int splits;   // most parts of a tile's keys, and least keys of a part
   int part;
   Spread tiles;
+  int64_t blocks;  // workgroups of the launch
+  int target;      // > 0: parts by the lengths that the GPU sees (paged_rules.h)
 };
 
-// Sets tile, splits, part and tiles; returns how many workgroups each (unit, slot) of tiles has.
-int set_plan(PagedGeometry& g);
-int set_plan_mx(PagedGeometry& g);  // for a cache of 8 or 4 bits
+void set_plan(PagedGeometry& g);               // tile, splits, part, tiles and blocks
+void set_plan_mx(PagedGeometry& g, int bits);  // and target, for a cache of 8 or 4 bits
 size_t paged_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,
                                 const void* k_pages, const void* v_pages, const int32_t* pages,

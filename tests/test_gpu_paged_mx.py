@@ -129,6 +129,8 @@ APPEND = {
     "three_heads": dict(new=[2, 9], held=[30, 9], KH=3),
     "eight_wide_heads": dict(new=[1, 4], held=[33, 4], KH=8, D=128),
     "one_wide_head": dict(new=[1, 4, 1], held=[33, 4, 1], KH=1, D=128, page=1),
+    "70_requests": dict(new=[1, 0] * 35, held=[1 + 13 * b % 90 for b in range(70)]),
+    "many_steps": dict(new=[1900, 1, 1400], held=[1900, 7, 1450], KH=3, D=128, page=24),
 }
 
 
@@ -252,6 +254,22 @@ CASES = {
     "not_causal": dict(new=[5, 60], held=[70, 80], causal=False),
     "strided": dict(new=[1, 40], held=[70, 80], fused=True),
 }
+
+
+LONGER = {
+    # requests that a wave holds a lane each, with lengths of every class, and one more than that
+    "64_requests": dict(new=[1] * 64, held=[1 + 37 * b % 1900 for b in range(64)]),
+    "65_requests": dict(new=[1] * 65, held=[1 + 37 * b % 1900 for b in range(65)]),
+    "none_of_64": dict(new=[0, 1] * 32, held=[(53 * b) % 700 for b in range(64)], tail=5),
+    "many_parts": dict(new=[1, 1], held=[70000, 2001], H=2, KH=1, D=128, page=100),
+    "tiles_and_parts": dict(new=[9, 1, 40] + [1] * 13, held=[3000, 5000, 1200] + [20] * 13, KH=1),
+}
+
+
+@pytest.mark.parametrize("bits,dtype", ((8, "bf16"), (4, "bf16"), (4, "f32")))
+@pytest.mark.parametrize("name", LONGER)
+def test_dealt_out(name, bits, dtype):
+    Case(20 + len(name), dtype=dtype, bits=bits, **LONGER[name]).check()
 
 
 @pytest.mark.parametrize("bits", (8, 4))
