@@ -549,14 +549,20 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     const int32_t* __restrict__ map, T* __restrict__ out,
                     float* __restrict__ lse, float* __restrict__ part_o,
                     float* __restrict__ part_l) {
-  constexpr int RB = D * BITS / 8, SB = D / 32, KB = 64, WAVES = kThreads / 64, ROWS = 16 * RT;
+  constexpr int RB = D * BITS / 8, SB = D / 32, WAVES = kThreads / 64, ROWS = 16 * RT;
+  // keys of a group: 32 where 64 would not leave enough registers (spilled ones are waited for
+  // together with every load: 64 requests with 6 new tokens 181 us with 64, 135 with 32)
+  constexpr int KB = RT == 2 && D == 128 && BITS == 8 ? 32 : 64, NI = KB / 16;
+  constexpr uint64_t kAll = ~0ull >> (64 - KB);
   using Frag = typename Type<T>::Frag;
-  using AFrag = typename Alpha<T>::Frag;
+  // With two blocks of rows alpha is rounded to bf16, as in the form with many rows.
+  constexpr bool ROUND = RT > 1 && sizeof(T) == 2;
+  using AFrag = typename std::conditional<ROUND, bf16x8_t, typename Alpha<T>::Frag>::type;
   using Quarter = Piece<BITS, RB / 16>;
   constexpr int KS = D / 32, DC = D / 16, E = 32 * D;
   // each wave's half group of values; at the end the waves' results of 16 rows in float32
   __shared__ __attribute__((aligned(16))) uint16_t lds[WAVES * E];
-  __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS];
+  __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS], divides[WAVES][ROUND ? ROWS : 1];
   extern __shared__ float bias[];
 
   Deal w;
@@ -585,7 +591,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   // from that, its row among all pages' rows, handed to the lanes that load it.  Returns which keys
   // have a row; the others' lanes load row 0.
   const int32_t* my_pages = pages + (int64_t)s.b * g.max_pages;
-  auto key_of = [&](int i) { return min(first + i * (WAVES * KB) + lane, s.k_hi - 1); };
+  auto key_of = [&](int i) { return min(first + i * (WAVES * KB) + lane % KB, s.k_hi - 1); };
   auto page_of = [&](int j) { return my_pages[div_by((uint32_t)j, g.page_mul, g.page_shift)]; };
   auto places = [&](int i, int p, uint32_t (&lo)[4], uint32_t (&hi)[4]) {
     const int j = key_of(i), page = div_by((uint32_t)j, g.page_mul, g.page_shift);
@@ -594,29 +600,35 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         ok ? ((int64_t)p * g.KH + w.u) * g.page_size + (j - page * g.page_size) : 0;
     quarters((uint32_t)row, lo);
     quarters((uint32_t)(row >> 32), hi);
-    return (uint64_t)__ballot(ok);
+    return (uint64_t)__ballot(ok) & kAll;
   };
-  struct Half {
-    Quarter k[2], v[2];
+  Quarter kq[NI], vq[NI];  // of keys 16 i + col of a group
+  auto row_of_key = [](const uint32_t (&lo)[4], const uint32_t (&hi)[4], int i) {
+    return (int64_t)((uint64_t)hi[i] << 32 | lo[i]);
   };
-  auto load = [&](Half& x, const uint32_t (&lo)[4], const uint32_t (&hi)[4], int half) {
+  auto load_keys = [&](const uint32_t (&lo)[4], const uint32_t (&hi)[4]) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t row = (int64_t)((uint64_t)hi[2 * half + i] << 32 | lo[2 * half + i]);
-      const int64_t at = row * RB + quarter * (RB / 4), sc = row * SB + quarter * SB / 4;
-      x.k[i].load(c.k + at, c.ks + sc);
-      x.v[i].load(c.v + at, c.vs + sc);
+    for (int i = 0; i < NI; ++i) {
+      const int64_t row = row_of_key(lo, hi, i);
+      kq[i].load(c.k + (row * RB + quarter * (RB / 4)), c.ks + (row * SB + quarter * SB / 4));
     }
   };
-  Half a, b;
-  uint64_t there = 0;  // of the group in a and b
+  auto load_values = [&](const uint32_t (&lo)[4], const uint32_t (&hi)[4], int half) {
+#pragma unroll
+    for (int i = 2 * half; i < 2 * half + 2; ++i) {
+      const int64_t row = row_of_key(lo, hi, i);
+      vq[i].load(c.v + (row * RB + quarter * (RB / 4)), c.vs + (row * SB + quarter * SB / 4));
+    }
+  };
+  uint64_t there = 0;  // of the group in kq and vq
   int next_page = 0;   // of the group behind it
   if (groups > 0) {
     uint32_t lo[4], hi[4];
     there = places(0, page_of(key_of(0)), lo, hi);
     next_page = page_of(key_of(1));
-    load(a, lo, hi, 0);
-    load(b, lo, hi, 1);
+    load_keys(lo, hi);
+    load_values(lo, hi, 0);
+    if constexpr (NI == 4) load_values(lo, hi, 1);
   }
   if constexpr (BIAS) fill_bias(bias, g, table, map, w.u);
   Frag qf[RT][KS];
@@ -639,11 +651,11 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       min(g.causal ? min(s.seen - 1, s.off + div_by(s.r0, g.group_mul, g.group_shift))
                    : s.seen - 1, s.k_hi - 1);
   f32x4_t o[RT][DC];
-  float top[RT], base[RT], sum[RT];
+  float top[RT], base[RT], sum[RT], divide[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     top[rt] = -INFINITY;
-    base[rt] = sum[rt] = 0.0f;
+    base[rt] = sum[rt] = divide[rt] = 0.0f;
 #pragma unroll
     for (int dc = 0; dc < DC; ++dc) o[rt][dc] = f32x4_t{};
   }
@@ -651,111 +663,129 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   uint16_t* mine = lds + wave * E;
   if constexpr (BIAS) __syncthreads();
 
-  // Half a group, keys kb .. kb + 31, whose elements are in h; `then` may load into h.
-  auto work = [&](Half& h, int kb, uint32_t bits, const auto& then) {
-    f32x4_t acc[RT][2];
+  // A group, keys kb .. kb + 63, whose elements are in kq and vq; MORE: these then get the next
+  // group's (lo, hi), as soon as they are converted.
+  auto group = [&](int kb, uint64_t bits, const uint32_t (&lo)[4], const uint32_t (&hi)[4],
+                   auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    f32x4_t acc[RT][NI];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NI; ++i)
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) acc[rt][i] = f32x4_t{};
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const bf16x8_t kf = as_bf16x8(h.k[i].eight_at(ks));
+    for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        const bf16x8_t kf = as_bf16x8(kq[i].eight_at(ks));
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) acc[rt][i] = times(kf, qf[rt][ks], acc[rt][i]);
       }
-    }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-        *reinterpret_cast<uint4*>(mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
-            h.v[i].eight_at(ks);
-    if (bits != ~0u) {  // what lies where a page number leads to no key may be NaN
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        if ((bits >> (16 * i + col) & 1) == 0) {
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks)
-            *reinterpret_cast<uint4*>(mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
-                make_uint4(0, 0, 0, 0);
-        }
-    }
     // Loads moved up to before the conversions would need other registers, and copies of them that
     // wait at the loop's end.
     __builtin_amdgcn_sched_barrier(0);
-    then();
-    AFrag pf[RT];
+    if constexpr (MORE) load_keys(lo, hi);
+    AFrag pf[RT][NI / 2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       // element e is key kb + 16 (e / 4) + 4 quarter + e % 4
-      float t[8];
+      float t[4 * NI];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) t[e] = acc[rt][e / 4][e % 4];
+      for (int e = 0; e < 4 * NI; ++e) t[e] = acc[rt][e / 4][e % 4];
       const int pos = s.off + x[rt].i;
       if constexpr (BIAS) {
         const float* tab = bias + (x[rt].head - w.u * g.group) * g.span;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < 4 * NI; ++e) {
           const int d = kb + 16 * (e / 4) + 4 * quarter + e % 4 - pos - g.rel_min;
           t[e] = fmaf(t[e], g.scale_log2, tab[min(max(d, 0), g.span - 1)]);
         }
       }
-      if (bits != ~0u || kb + 31 > all_see) {
-        asm volatile("");  // a branch: blocks that every row sees do not pay for it
+      if (bits != kAll || kb + KB - 1 > all_see) {
+        asm volatile("");  // a branch: groups that every row sees do not pay for it
         const int last = min(g.causal ? min(s.seen - 1, pos) : s.seen - 1, s.k_hi - 1);
         const int seen = last - kb - 4 * quarter;
-        const uint32_t have = bits >> (4 * quarter);
+        const uint64_t have = bits >> (4 * quarter);
+        const uint32_t word[2] = {(uint32_t)have, (uint32_t)(have >> 32)};
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (16 * (e / 4) + e % 4 > seen || (have >> (16 * (e / 4) + e % 4) & 1) == 0)
+        for (int e = 0; e < 4 * NI; ++e)
+          if (16 * (e / 4) + e % 4 > seen || (word[e / 8] >> (16 * (e / 4 % 2) + e % 4) & 1) == 0)
             t[e] = -INFINITY;
       }
       float mx = fmaxf(t[0], t[1]);
 #pragma unroll
-      for (int e = 2; e < 8; ++e) mx = fmaxf(mx, t[e]);
+      for (int e = 2; e < 4 * NI; ++e) mx = fmaxf(mx, t[e]);
       mx = max_of(mx) * scale;  // scale > 0
       const bool raise = mx > top[rt] + kSlack;
       if (__any(raise)) {
         const float corr = raise ? __builtin_amdgcn_exp2f(top[rt] - mx) : 1.0f;
         if (raise) top[rt] = base[rt] = mx;
         sum[rt] *= corr;
+        divide[rt] *= corr;
 #pragma unroll
         for (int dc = 0; dc < DC; ++dc) o[rt][dc] *= corr;
       }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < 4 * NI; ++e) {
         t[e] = __builtin_amdgcn_exp2f(fmaf(t[e], scale, -base[rt]));
         sum[rt] += t[e];
       }
-      pf[rt] = Alpha<T>::of(t);
-    }
-    fence_wave();
 #pragma unroll
-    for (int dc = 0; dc < DC; ++dc) {
-      const bf16x8_t vf = value_cols<D>(mine, 16 * dc);
+      for (int i = 0; i < NI / 2; ++i) {
+        if constexpr (ROUND) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) o[rt][dc] = times(vf, pf[rt], o[rt][dc]);
+          for (int e = 0; e < 8; ++e) pf[rt][i][e] = (__bf16)t[8 * i + e];
+          const uint4 u = __builtin_bit_cast(uint4, pf[rt][i]);
+          divide[rt] = plus_both(plus_both(plus_both(plus_both(divide[rt], u.x), u.y), u.z), u.w);
+        } else {
+          pf[rt][i] = Alpha<T>::of(t + 8 * i);
+        }
+      }
     }
-    fence_wave();
+#pragma unroll
+    for (int half = 0; half < NI / 2; ++half) {
+      if (!MORE && half == 1 && kb + 32 >= s.k_hi) break;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          *reinterpret_cast<uint4*>(mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
+              vq[2 * half + i].eight_at(ks);
+      const uint32_t have = (uint32_t)(bits >> (32 * half));
+      if (have != ~0u) {  // what lies where a page number leads to no key may be NaN
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if ((have >> (16 * i + col) & 1) == 0) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+              *reinterpret_cast<uint4*>(
+                  mine + value_at<D>(16 * i + col, quarter * (D / 4) + 8 * ks)) =
+                  make_uint4(0, 0, 0, 0);
+          }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (MORE) load_values(lo, hi, half);
+      fence_wave();
+#pragma unroll
+      for (int dc = 0; dc < DC; ++dc) {
+        const bf16x8_t vf = value_cols<D>(mine, 16 * dc);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) o[rt][dc] = times(vf, pf[rt][half], o[rt][dc]);
+      }
+      fence_wave();
+    }
   };
   // The last group apart: with no load behind a condition the compiler counts those in flight, and
   // waits for no more than it needs.
   int i = 0;
+  uint32_t lo[4], hi[4];
   for (; i + 1 < groups; ++i) {
-    const int kb = first + i * (WAVES * KB);
-    uint32_t lo[4], hi[4];
     const uint64_t next_there = places(i + 1, next_page, lo, hi);
     next_page = page_of(key_of(i + 2));
-    work(a, kb, (uint32_t)there, [&] { load(a, lo, hi, 0); });
-    work(b, kb + 32, (uint32_t)(there >> 32), [&] { load(b, lo, hi, 1); });
+    group(first + i * (WAVES * KB), there, lo, hi, std::true_type());
     there = next_there;
   }
-  if (groups > 0) {
-    const int kb = first + i * (WAVES * KB);
-    work(a, kb, (uint32_t)there, [] {});
-    if (kb + 32 < s.k_hi) work(b, kb + 32, (uint32_t)(there >> 32), [] {});
-  }
+  if (groups > 0) group(first + i * (WAVES * KB), there, lo, hi, std::false_type());
 
   // The waves' sums join over a common maximum, 16 rows at a time.
   const int count = min(s.rows - s.r0, ROWS);
@@ -768,10 +798,11 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const float total = sum_of(sum[rt]);
+    const float total = sum_of(sum[rt]), by = ROUND ? sum_of(divide[rt]) : total;
     if (quarter == 0) {
       tops[wave][16 * rt + col] = top[rt];
       totals[wave][16 * rt + col] = total;
+      if (ROUND) divides[wave][16 * rt + col] = by;
     }
   }
   __syncthreads();
@@ -798,13 +829,14 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     for (int e = threadIdx.x; e < min(count - 16 * rt, 16) * (D / 4); e += kThreads) {
       const int r = e / (D / 4), chunk = e % (D / 4), at_row = 16 * rt + r;
       const float tr = most(at_row);
-      float total = 0.0f;
+      float total = 0.0f, by = 0.0f;
       float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) {
-        float f = totals[i][at_row];
-        if (tops[i][at_row] != -INFINITY) f *= __builtin_amdgcn_exp2f(tops[i][at_row] - tr);
-        total += f;
+        const float f = tops[i][at_row] == -INFINITY
+                            ? 1.0f : __builtin_amdgcn_exp2f(tops[i][at_row] - tr);
+        total = fmaf(totals[i][at_row], f, total);
+        if constexpr (ROUND) by = fmaf(divides[i][at_row], f, by);
         const float4 z =
             *reinterpret_cast<const float4*>(sums + (i * 16 + r) * D + ((chunk ^ r) << 2));
         y.x += z.x;
@@ -812,7 +844,8 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         y.z += z.z;
         y.w += z.w;
       }
-      const float inv = total > 0.0f ? 1.0f / total : total;
+      if constexpr (!ROUND) by = total;
+      const float inv = by > 0.0f ? 1.0f / by : by;
       const float l2 = total == 0.0f
                            ? -INFINITY
                            : (tr == -INFINITY ? 0.0f : tr) + __builtin_amdgcn_logf(total);
