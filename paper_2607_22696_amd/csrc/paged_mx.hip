@@ -111,8 +111,7 @@ __device__ inline void fence_wave() {
 
 // The workgroup's key head, tile and part.  A part of a head's keys stays on one XCD, whose L2 then
 // serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
-// four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, LONG us
-// so).
+// four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, 30 so).
 __device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split) {
   if (!work_of(g.tiles, 1, w)) return false;
   split = w.u / g.KH;
@@ -551,8 +550,9 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     float* __restrict__ part_l) {
   constexpr int RB = D * BITS / 8, SB = D / 32, WAVES = kThreads / 64, ROWS = 16 * RT;
   // keys of a group: 32 where 64 would not leave enough registers (spilled ones are waited for
-  // together with every load: 64 requests with 6 new tokens 181 us with 64, 135 with 32)
-  constexpr int KB = RT == 2 && D == 128 && BITS == 8 ? 32 : 64, NI = KB / 16;
+  // together with every load: 64 requests with 6 new tokens 181 us with 64, 135 with 32; with one
+  // new token in float32 129 and 117)
+  constexpr int KB = D == 128 && BITS == 8 && (RT == 2 || sizeof(T) == 4) ? 32 : 64, NI = KB / 16;
   constexpr uint64_t kAll = ~0ull >> (64 - KB);
   using Frag = typename Type<T>::Frag;
   // With two blocks of rows alpha is rounded to bf16, as in the form with many rows.
@@ -1235,7 +1235,7 @@ hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache
 }  // namespace
 
 void set_plan_mx(PagedGeometry& g, int bits) {
-  const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv, 3);
+  const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = p.part;
