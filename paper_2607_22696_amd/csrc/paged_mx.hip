@@ -963,7 +963,7 @@ struct Rows {
   int per;                       // chunks of a token's key and value together, at least 16
   uint32_t per_mul, per_shift;   // chunk / per
 };
-constexpr int kManySteps = 8;    // at most 64 kManySteps / 16 + 1 tokens: a lane for each
+constexpr int kMostSteps = 8;    // at most 64 kMostSteps / 16 + 1 tokens: a lane for each
 
 // This lane's chunk: token, half (0: key, 1: value), head, first channel; and the token's place.
 struct Chunk {
@@ -1145,37 +1145,39 @@ __global__ __launch_bounds__(kThreads) void mx_read_kernel(
 }
 
 template <typename T, int D, int BITS>
-const void* append_fn(bool many) {
-  return many ? (const void*)&mx_append_kernel<T, D, BITS, kManySteps>
-              : (const void*)&mx_append_kernel<T, D, BITS, 1>;
+const void* append_fn(int steps) {
+  return steps == 1   ? (const void*)&mx_append_kernel<T, D, BITS, 1>
+         : steps == 4 ? (const void*)&mx_append_kernel<T, D, BITS, 4>
+                      : (const void*)&mx_append_kernel<T, D, BITS, kMostSteps>;
 }
 template <typename T, int D, int BITS>
-const void* read_fn(bool many) {
-  return many ? (const void*)&mx_read_kernel<T, D, BITS, kManySteps>
-              : (const void*)&mx_read_kernel<T, D, BITS, 1>;
+const void* read_fn(int steps) {
+  return steps == 1   ? (const void*)&mx_read_kernel<T, D, BITS, 1>
+         : steps == 4 ? (const void*)&mx_read_kernel<T, D, BITS, 4>
+                      : (const void*)&mx_read_kernel<T, D, BITS, kMostSteps>;
 }
 
-// How rows are dealt out: one step per wave where that fills the card no more than twice over
-// (4,096 waves), for the shortest chain.
+// How rows are dealt out: one step per wave up to 4,096 of them (16 waves per compute unit), for the
+// shortest chain; then four, or eight where there are more than 65,536 (7,597 tokens of 8 heads x
+// 128 written to 4 bits: 13.1, 12.2, 13.1 us with 2, 4, 8 steps; 60,000 read: 89, 66, 64).
 struct RowsPlan {
   Rows r;
-  bool many;
+  int steps;
   int64_t blocks;
 };
 RowsPlan plan_rows(const PagedGeometry& g) {
   RowsPlan p;
   p.r.per = 2 * g.KH * (g.D / 8);
-  p.r.per_mul = 0;
   divisor(p.r.per, &p.r.per_mul, &p.r.per_shift);
   const int64_t steps = ((int64_t)g.nq * p.r.per + 63) / 64;
-  p.many = steps > 4096;
-  const int each = (p.many ? kManySteps : 1) * (kThreads / 64);
+  p.steps = steps <= 4096 ? 1 : steps <= 65536 ? 4 : kMostSteps;
+  const int each = p.steps * (kThreads / 64);
   p.blocks = (steps + each - 1) / each;
   return p;
 }
 
 // The form for the call's type, channels and bits.
-typedef const void* (*Form)(bool);
+typedef const void* (*Form)(int);
 Form form(const PagedGeometry& g, bool bf16, int bits, Form b64_8, Form b128_8, Form b64_4,
           Form b128_4, Form f64_8, Form f128_8, Form f64_4, Form f128_4) {
   const Form all[2][2][2] = {{{f64_4, f64_8}, {f128_4, f128_8}},
@@ -1269,7 +1271,7 @@ hipError_t launch_paged_append_mx(const PagedGeometry& g, bool bf16, const void*
   const void* fn = form(
       g, bf16, cache.bits, append_fn<uint16_t, 64, 8>, append_fn<uint16_t, 128, 8>,
       append_fn<uint16_t, 64, 4>, append_fn<uint16_t, 128, 4>, append_fn<float, 64, 8>,
-      append_fn<float, 128, 8>, append_fn<float, 64, 4>, append_fn<float, 128, 4>)(p.many);
+      append_fn<float, 128, 8>, append_fn<float, 64, 4>, append_fn<float, 128, 4>)(p.steps);
   return seq_launch(fn, p.blocks, kThreads, 0, s, g, p.r, k, v, cu_q, kv_lens, pages, c);
 }
 
@@ -1282,7 +1284,7 @@ hipError_t launch_paged_read_mx(const PagedGeometry& g, bool bf16, const dsa3d_m
   const void* fn = form(
       g, bf16, cache.bits, read_fn<uint16_t, 64, 8>, read_fn<uint16_t, 128, 8>,
       read_fn<uint16_t, 64, 4>, read_fn<uint16_t, 128, 4>, read_fn<float, 64, 8>,
-      read_fn<float, 128, 8>, read_fn<float, 64, 4>, read_fn<float, 128, 4>)(p.many);
+      read_fn<float, 128, 8>, read_fn<float, 64, 4>, read_fn<float, 128, 4>)(p.steps);
   return seq_launch(fn, p.blocks, kThreads, 0, s, g, p.r, c, pages, kv_lens, cu_q, k, v);
 }
 
