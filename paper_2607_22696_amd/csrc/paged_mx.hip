@@ -113,10 +113,105 @@ __device__ inline void fence_wave() {
 // serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
 // four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, 30 so).
 __device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split) {
-  if (!work_of(g.tiles, 1, w)) return false;
+  if (!work_of<false>(g.tiles, 1, w)) return false;  // low slots first
   split = w.u / g.KH;
   w.u -= split * g.KH;
   return true;
+}
+
+// Up to 64 requests, a lane each, with one load of their offsets and lengths.
+struct Held {
+  int begin, end, n, m, keys, tiles;
+};
+template <int ROWS>
+__device__ inline Held held_by_lane(const PagedGeometry& g, const int32_t* cu_q,
+                                    const int32_t* kv_lens) {
+  const int lane = threadIdx.x & 63, b = min(lane, g.B - 1);
+  const int raw = cu_q[b], raw_next = cu_q[b + 1], raw_m = kv_lens[b];  // three loads at once
+  Held h;
+  h.begin = b == 0 ? 0 : min(max(raw, 0), g.nq);
+  h.end = min(max(raw_next, 0), g.nq);
+  h.n = lane < g.B ? max(h.end - h.begin, 0) : 0;
+  h.m = max(raw_m, 0);
+  h.keys = h.n > 0 ? min(h.m, g.max_kv) : 0;
+  h.tiles = h.n * g.group / ROWS + (h.n * g.group % ROWS != 0);
+  return h;
+}
+
+// Deals numbers out to the lanes, `count` to each, those of size 3 first, then 2, 1 and 0, so that
+// what is dealt out last is short.  The lane that has number `index`, and which of its numbers that
+// is; behind the last one -1, and how far behind.
+__device__ inline int lane_of(int index, int count, int size, int& nth) {
+  int start = 0, before = 0;
+#pragma unroll
+  for (int c = 3; c >= 0; --c) {
+    const int sum = prefix_sum(size == c ? count : 0);
+    if (size == c) start = before + sum - count;
+    before += __builtin_amdgcn_readlane(sum, 63);
+  }
+  const uint64_t who = __ballot(index >= start && index < start + count);
+  if (who == 0) {
+    nth = index - before;
+    return -1;
+  }
+  const int l = __builtin_ctzll(who);
+  nth = index - __builtin_amdgcn_readlane(start, l);
+  return l;
+}
+
+// The span of tile `tile` of lane l's request, or of the rows behind the last one (l = -1), which
+// see nothing; false if there is no such tile.
+template <int ROWS>
+__device__ inline bool span_of(const PagedGeometry& g, const Held& h, int l, int tile, Span1& s) {
+  if (l < 0) {
+    s.b = g.B;
+    s.begin = __builtin_amdgcn_readlane(h.end, g.B - 1);
+    s.n = g.nq - s.begin;
+    s.m = 0;
+  } else {
+    s.b = l;
+    s.begin = __builtin_amdgcn_readlane(h.begin, l);
+    s.n = __builtin_amdgcn_readlane(h.n, l);
+    s.m = __builtin_amdgcn_readlane(h.m, l);
+  }
+  s.rows = s.n * g.group;
+  if (tile > (s.rows - 1) / ROWS || s.rows == 0) return false;
+  s.r0 = tile * ROWS;
+  s.off = s.m - s.n;
+  s.seen = min(s.m, g.max_kv);
+  int hi = s.seen;
+  if (g.causal)
+    hi = min(hi, s.off + div_by(min(s.r0 + ROWS, s.rows) - 1, g.group_mul, g.group_shift) + 1);
+  s.k_hi = max(hi, 0);
+  return true;
+}
+// Part `split` of its keys, `len` of them.
+__device__ inline void take_keys(Span1& s, int split, int len) {
+  s.k_lo = (int)min((int64_t)split * len, (int64_t)s.k_hi);
+  s.k_hi = (int)min((int64_t)s.k_hi, (int64_t)s.k_lo + len);
+}
+
+// Where a workgroup of the form with many rows is: up to 64 requests' tiles are numbered from those
+// with most keys to those with fewest, and within a request from the last one (under a causal mask
+// the longest); more requests' as they lie.  (Chunks of 512, 801 and 300 of 16,000, 801 and 5,000
+// tokens beside three single ones: ORDER us as they lie, 224 so.)
+__device__ inline bool locate_rows(const PagedGeometry& g, const int32_t* cu_q,
+                                   const int32_t* kv_lens, int slot, int split, Span1& s) {
+  if (g.B > kDealt)
+    return locate<kManyRows>(g, cu_q, kv_lens, g.tiles.slots - 1 - slot, split, s);
+  const Held h = held_by_lane<kManyRows>(g, cu_q, kv_lens);
+  int longest = h.keys;
+#pragma unroll
+  for (int x = 32; x > 0; x >>= 1) longest = max(longest, __shfl_xor(longest, x));
+  int r;
+  const int l = lane_of(slot, h.tiles, (int)((int64_t)h.keys * 4 / ((int64_t)longest + 1)), r);
+  const int tile = l < 0 ? r : __builtin_amdgcn_readlane(h.tiles, l) - 1 - r;
+  if (!span_of<kManyRows>(g, h, l, tile, s)) return false;
+  const int even = (s.k_hi + g.splits - 1) / g.splits;
+  const int len = max(g.part, (even + kFewKeys - 1) / kFewKeys * kFewKeys);
+  s.only = s.k_hi <= len;
+  take_keys(s, split, len);
+  return !(s.only && split > 0);
 }
 
 // ------------------------------------------------------------------------- many rows
@@ -158,7 +253,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   int split;
   if (!work_of_part(g, w, split)) return;
   Span1 s;
-  if (!locate<kManyRows>(g, cu_q, kv_lens, w.slot, split, s)) return;
+  if (!locate_rows(g, cu_q, kv_lens, w.slot, split, s)) return;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int rw = s.r0 + wave * 32;
@@ -302,10 +397,14 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         }
         if (MORE && b == NB - 1) __syncthreads();  // the next tile is in LDS
         if constexpr (LIVE) {
+          // ahead of the other workgroup's wave on this SIMD while the matrix cores have work: chunks
+          // 228 and 224 us, a prompt of 4,096 tokens over 4 bits 175 and 164
+          __builtin_amdgcn_s_setprio(1);
           if constexpr (MORE) next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
           else if (b + 1 < NB) next = products(kc, b + 1);
           sm.weigh(y, scale);
           accumulate(kc + E, b, y);
+          __builtin_amdgcn_s_setprio(0);
         }
       }
       if constexpr (MORE) __syncthreads();  // and this one is free
@@ -456,9 +555,7 @@ struct Deal {
   int u, split, parts;  // key head; part of how many (all the workspace has where not dealt out)
 };
 
-// Up to 64 requests: a lane holds each, with one load of its offsets and length, and the parts of
-// their keys go by the sum of all lengths.  Longer parts come first (four classes), so that what is
-// dealt out last is short.
+// Up to 64 requests' keys are divided by the sum of their lengths, and longer parts come first.
 template <int ROWS>
 __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
                             Deal& d) {
@@ -473,63 +570,22 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
   constexpr int STEP = 256;  // keys of the four waves' groups
   const int block = block_number(), index = block / g.KH;
   d.u = block - index * g.KH;
-  const int lane = threadIdx.x & 63, b = min(lane, g.B - 1);
-  const int raw = cu_q[b], raw_next = cu_q[b + 1], raw_m = kv_lens[b];  // three loads at once
-  const int begin = b == 0 ? 0 : min(max(raw, 0), g.nq), end = min(max(raw_next, 0), g.nq);
-  const int n = lane < g.B ? max(end - begin, 0) : 0, m = max(raw_m, 0);
-  const int keys = n > 0 ? min(m, g.max_kv) : 0;
-  const int tiles = (n * g.group + ROWS - 1) / ROWS;
-  float all = (float)tiles * (float)keys;
+  const Held h = held_by_lane<ROWS>(g, cu_q, kv_lens);
+  float all = (float)h.tiles * (float)h.keys;
 #pragma unroll
   for (int x = 32; x > 0; x >>= 1) all += __shfl_xor(all, x);
   const float share = fminf(all / (float)g.target, (float)(1 << 30));
   const int most = max(((int)share + STEP) / STEP * STEP, g.part);  // more than a share
-  const int parts = min(max((keys + most - 1) / most, 1), g.splits);
-  const int len = ((keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
-  const int count = tiles * parts;
-  const int size = min((int)((int64_t)len * 4 / (most + 1)), 3);  // the longest: 3
-  int start = 0, before = 0;
-#pragma unroll
-  for (int c = 3; c >= 0; --c) {
-    const int sum = prefix_sum(size == c ? count : 0);
-    if (size == c) start = before + sum - count;
-    before += __builtin_amdgcn_readlane(sum, 63);
-  }
-  const uint64_t who = __ballot(index >= start && index < start + count);
-  int r, tile;
-  if (who == 0) {  // rows behind the last request, which see nothing
-    s.b = g.B;
-    s.begin = __builtin_amdgcn_readlane(end, g.B - 1);
-    s.n = g.nq - s.begin;
-    s.m = 0;
-    d.parts = 1;
-    d.split = 0;
-    r = 0;
-    tile = index - before;
-    if (tile >= (s.n * g.group + ROWS - 1) / ROWS) return false;
-  } else {
-    const int l = __builtin_ctzll(who);
-    s.b = l;
-    s.begin = __builtin_amdgcn_readlane(begin, l);
-    s.n = __builtin_amdgcn_readlane(n, l);
-    s.m = __builtin_amdgcn_readlane(m, l);
-    d.parts = __builtin_amdgcn_readlane(parts, l);
-    r = index - __builtin_amdgcn_readlane(start, l);
-    tile = r / d.parts;
-    d.split = r - tile * d.parts;
-  }
-  const int part = who == 0 ? 0 : __builtin_amdgcn_readlane(len, __builtin_ctzll(who));
-  s.rows = s.n * g.group;
-  s.r0 = tile * ROWS;
-  s.off = s.m - s.n;
-  s.seen = min(s.m, g.max_kv);
-  int hi = s.seen;
-  if (g.causal)
-    hi = min(hi, s.off + div_by(min(s.r0 + ROWS, s.rows) - 1, g.group_mul, g.group_shift) + 1);
-  hi = max(hi, 0);
-  s.k_lo = min((int64_t)d.split * part, (int64_t)hi);
-  s.k_hi = min((int64_t)hi, (int64_t)s.k_lo + part);
+  const int parts = min(max((h.keys + most - 1) / most, 1), g.splits);
+  const int len = ((h.keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
+  int r;
+  const int l = lane_of(index, h.tiles * parts, min((int)((int64_t)len * 4 / (most + 1)), 3), r);
+  d.parts = l < 0 ? 1 : __builtin_amdgcn_readlane(parts, l);
+  const int tile = r / d.parts;
+  d.split = r - tile * d.parts;
+  if (!span_of<ROWS>(g, h, l, tile, s)) return false;
   s.only = d.parts == 1;
+  take_keys(s, d.split, l < 0 ? 0 : __builtin_amdgcn_readlane(len, l));
   return true;
 }
 
