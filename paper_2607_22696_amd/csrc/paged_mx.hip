@@ -113,7 +113,7 @@ __device__ inline void fence_wave() {
 // serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
 // four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, 30 so).
 __device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split) {
-  if (!work_of<false>(g.tiles, 1, w)) return false;  // low slots first
+  if (!work_of(g.tiles, 1, w)) return false;
   split = w.u / g.KH;
   w.u -= split * g.KH;
   return true;
@@ -191,27 +191,55 @@ __device__ inline void take_keys(Span1& s, int split, int len) {
   s.k_hi = (int)min((int64_t)s.k_hi, (int64_t)s.k_lo + len);
 }
 
-// Where a workgroup of the form with many rows is: up to 64 requests' tiles are numbered from those
-// with most keys to those with fewest, and within a request from the last one (under a causal mask
-// the longest); more requests' as they lie.  (Chunks of 512, 801 and 300 of 16,000, 801 and 5,000
-// tokens beside three single ones: ORDER us as they lie, 224 so.)
-__device__ inline bool locate_rows(const PagedGeometry& g, const int32_t* cu_q,
-                                   const int32_t* kv_lens, int slot, int split, Span1& s) {
-  if (g.B > kDealt)
-    return locate<kManyRows>(g, cu_q, kv_lens, g.tiles.slots - 1 - slot, split, s);
-  const Held h = held_by_lane<kManyRows>(g, cu_q, kv_lens);
-  int longest = h.keys;
+// What a workgroup works on.
+struct Deal {
+  Span1 s;
+  int u, split, parts;  // key head; part of how many (all the workspace has where not dealt out)
+};
+
+// Up to 64 requests' keys are divided by the sum of their lengths, and longer parts come first; a
+// request's tiles over the same part follow each other, the last (under a causal mask the longest)
+// first.  More requests as they lie, in parts that the host chose.  (A chunk of 400 of 30,000
+// tokens before 40 of 100 of 700, 32 / 8 heads: 784 us as they lie in parts chosen without the
+// lengths, 712 longest first, 318 divided; chunks
+// of 512, 801 and 300 of 16,000, 801 and 5,000 tokens beside three single ones 235 and 215.)
+template <int ROWS>
+__device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
+                            Deal& d) {
+  Span1& s = d.s;
+  if (g.target == 0) {
+    Work w;
+    if (!work_of_part(g, w, d.split)) return false;
+    d.u = w.u;
+    d.parts = g.splits;
+    return locate<ROWS>(g, cu_q, kv_lens, w.slot, d.split, s);
+  }
+  constexpr int STEP = 256;  // keys of the four waves' groups
+  const int block = block_number(), index = block / g.KH;
+  d.u = block - index * g.KH;
+  const Held h = held_by_lane<ROWS>(g, cu_q, kv_lens);
+  float all = (float)h.tiles * (float)h.keys;
 #pragma unroll
-  for (int x = 32; x > 0; x >>= 1) longest = max(longest, __shfl_xor(longest, x));
+  for (int x = 32; x > 0; x >>= 1) all += __shfl_xor(all, x);
+  const float share = fminf(all / (float)g.target, (float)(1 << 30));
+  const int most = max(((int)share + STEP) / STEP * STEP, g.part);  // more than a share
+  const int parts = min(max((h.keys + most - 1) / most, 1), g.splits);
+  const int len = ((h.keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
   int r;
-  const int l = lane_of(slot, h.tiles, (int)((int64_t)h.keys * 4 / ((int64_t)longest + 1)), r);
-  const int tile = l < 0 ? r : __builtin_amdgcn_readlane(h.tiles, l) - 1 - r;
-  if (!span_of<kManyRows>(g, h, l, tile, s)) return false;
-  const int even = (s.k_hi + g.splits - 1) / g.splits;
-  const int len = max(g.part, (even + kFewKeys - 1) / kFewKeys * kFewKeys);
-  s.only = s.k_hi <= len;
-  take_keys(s, split, len);
-  return !(s.only && split > 0);
+  const int l = lane_of(index, h.tiles * parts, min((int)((int64_t)len * 4 / (most + 1)), 3), r);
+  int tile = r;
+  d.split = 0;
+  d.parts = 1;
+  if (l >= 0) {
+    const int tiles = __builtin_amdgcn_readlane(h.tiles, l);
+    d.parts = __builtin_amdgcn_readlane(parts, l);
+    d.split = r / tiles;
+    tile = tiles - 1 - (r - d.split * tiles);
+  }
+  if (!span_of<ROWS>(g, h, l, tile, s)) return false;
+  s.only = d.parts == 1;
+  take_keys(s, d.split, l < 0 ? 0 : __builtin_amdgcn_readlane(len, l));
+  return true;
 }
 
 // ------------------------------------------------------------------------- many rows
@@ -249,11 +277,10 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   __shared__ __attribute__((aligned(8))) uint16_t there[2][4];
   extern __shared__ float bias[];
 
-  Work w;
-  int split;
-  if (!work_of_part(g, w, split)) return;
-  Span1 s;
-  if (!locate_rows(g, cu_q, kv_lens, w.slot, split, s)) return;
+  Deal w;
+  if (!deal<kManyRows>(g, cu_q, kv_lens, w)) return;
+  const Span1& s = w.s;
+  const int split = w.split;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int rw = s.r0 + wave * 32;
@@ -441,6 +468,8 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       for (int db = 0; db < DB; ++db) store_block(part_o + at * D, db, o[db], inv);
     }
     if (hh == 0) part_l[at] = part_lse(l2);
+    if (hh == 0 && split == 0)  // parts that there are none of
+      for (int i = w.parts; i < g.splits; ++i) part_l[at + i] = -INFINITY;
   }
 }
 
@@ -547,46 +576,6 @@ __device__ inline bf16x8_t value_cols(const uint16_t* lds, int d0) {
       __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4_t*)(lds + value_at<D>(row + 16, chan)));
   const uint2 ul = __builtin_bit_cast(uint2, lo), uh = __builtin_bit_cast(uint2, hi);
   return as_bf16x8(make_uint4(ul.x, ul.y, uh.x, uh.y));
-}
-
-// What a workgroup of the form with few rows works on.
-struct Deal {
-  Span1 s;
-  int u, split, parts;  // key head; part of how many (all the workspace has where not dealt out)
-};
-
-// Up to 64 requests' keys are divided by the sum of their lengths, and longer parts come first.
-template <int ROWS>
-__device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
-                            Deal& d) {
-  Span1& s = d.s;
-  if (g.target == 0) {
-    Work w;
-    if (!work_of_part(g, w, d.split)) return false;
-    d.u = w.u;
-    d.parts = g.splits;
-    return locate<ROWS>(g, cu_q, kv_lens, w.slot, d.split, s);
-  }
-  constexpr int STEP = 256;  // keys of the four waves' groups
-  const int block = block_number(), index = block / g.KH;
-  d.u = block - index * g.KH;
-  const Held h = held_by_lane<ROWS>(g, cu_q, kv_lens);
-  float all = (float)h.tiles * (float)h.keys;
-#pragma unroll
-  for (int x = 32; x > 0; x >>= 1) all += __shfl_xor(all, x);
-  const float share = fminf(all / (float)g.target, (float)(1 << 30));
-  const int most = max(((int)share + STEP) / STEP * STEP, g.part);  // more than a share
-  const int parts = min(max((h.keys + most - 1) / most, 1), g.splits);
-  const int len = ((h.keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
-  int r;
-  const int l = lane_of(index, h.tiles * parts, min((int)((int64_t)len * 4 / (most + 1)), 3), r);
-  d.parts = l < 0 ? 1 : __builtin_amdgcn_readlane(parts, l);
-  const int tile = r / d.parts;
-  d.split = r - tile * d.parts;
-  if (!span_of<ROWS>(g, h, l, tile, s)) return false;
-  s.only = d.parts == 1;
-  take_keys(s, d.split, l < 0 ? 0 : __builtin_amdgcn_readlane(len, l));
-  return true;
 }
 
 // 16 RT rows per workgroup; its waves share out the keys in groups of 64 and read them each for
@@ -925,88 +914,97 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 // Joins the parts of each row, weights 2^(l - max l), as paged_join_kernel does, but for many parts
 // with W waves per row, of which wave w has the parts w, w + W, ..., and with several loads on their
 // way before the first is waited for (64 rows of 63 parts: 12.6 us with one wave and loads behind
-// a branch, 4.0 so).  A part without keys has -inf, and its results were never written.
-template <typename T, int D, int W, int AT_ONCE>
+// a branch, 4.0 so).  A part without keys has -inf, and its results were never written.  A wave
+// looks at R rows at once and goes on with those that were not finished: a launch with many rows
+// has few of them, and often none (52,000 rows, half of them in three parts: 13 us with one each,
+// JOIN8 with 8).
+template <typename T, int D, int W, int AT_ONCE, int R>
 __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int splits,
                                                            const float* __restrict__ part_o,
                                                            const float* __restrict__ part_l,
                                                            T* __restrict__ out,
                                                            float* __restrict__ lse) {
   constexpr int LANES = D / 4, SIDES = 64 / LANES, PER = kThreads / 64 / W;
+  static_assert(W == 1 || R == 1, "several waves have one row");
   __shared__ float4 sums[W][LANES];
   __shared__ float tops[W], totals[W];
   const int wave = wave_id() % W, lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)block_number() * PER + wave_id() / W;
-  if (row >= rows) return;  // a whole workgroup where W > 1
+  const int64_t row0 = ((int64_t)block_number() * PER + wave_id() / W) * R;
+  if (row0 >= rows) return;  // a whole workgroup where W > 1
   const int side = lane / LANES, c = lane % LANES * 4;
-  // lane l has part l W + wave
-  const float mine = lane * W + wave < splits ? part_l[row * splits + lane * W + wave] : -INFINITY;
-  if (part_l[row * splits] == kDone) return;
-  float top = mine;
+  const int64_t look = row0 + lane;
+  uint64_t left = __ballot(lane < R && look < rows && part_l[min(look, rows - 1) * splits] != kDone);
+  for (; left != 0; left &= left - 1) {
+    const int64_t row = row0 + __builtin_ctzll(left);
+    // lane l has part l W + wave
+    const float mine = lane * W + wave < splits ? part_l[row * splits + lane * W + wave] : -INFINITY;
+    float top = mine;
 #pragma unroll
-  for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if constexpr (W > 1) {
-    tops[wave] = top;
-    __syncthreads();
+    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    if constexpr (W > 1) {
+      tops[wave] = top;
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = fmaxf(top, tops[i]);
-  }
-  const float weight = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
-  float total = weight;
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-  // this wave's parts up to its last that is there
-  const uint64_t some = __ballot(mine != -INFINITY);
-  const int count = some == 0 ? 0 : 64 - __builtin_clzll(some);
-  float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int s0 = 0; s0 < count; s0 += AT_ONCE * SIDES) {
-    float4 x[AT_ONCE];
-#pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int s = min(s0 + i * SIDES + side, count - 1) * W + wave;
-      x[i] = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
+      for (int i = 0; i < W; ++i) top = fmaxf(top, tops[i]);
     }
+    const float weight = mine == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mine - top);
+    float total = weight;
 #pragma unroll
-    for (int i = 0; i < AT_ONCE; ++i) {
-      const int s = s0 + i * SIDES + side;
-      const float ws = __shfl(weight, s & 63), ls = __shfl(mine, s & 63);
-      if (s < count && ls != -INFINITY) {
-        sum.x = fmaf(ws, x[i].x, sum.x);
-        sum.y = fmaf(ws, x[i].y, sum.y);
-        sum.z = fmaf(ws, x[i].z, sum.z);
-        sum.w = fmaf(ws, x[i].w, sum.w);
+    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+    // this wave's parts up to its last that is there
+    const uint64_t some = __ballot(mine != -INFINITY);
+    const int count = some == 0 ? 0 : 64 - __builtin_clzll(some);
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int s0 = 0; s0 < count; s0 += AT_ONCE * SIDES) {
+      float4 x[AT_ONCE];
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int s = min(s0 + i * SIDES + side, count - 1) * W + wave;
+        x[i] = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
+      }
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        const int s = s0 + i * SIDES + side;
+        const float ws = __shfl(weight, s & 63), ls = __shfl(mine, s & 63);
+        if (s < count && ls != -INFINITY) {
+          sum.x = fmaf(ws, x[i].x, sum.x);
+          sum.y = fmaf(ws, x[i].y, sum.y);
+          sum.z = fmaf(ws, x[i].z, sum.z);
+          sum.w = fmaf(ws, x[i].w, sum.w);
+        }
       }
     }
-  }
 #pragma unroll
-  for (int d = 32; d >= LANES; d >>= 1) {
-    sum.x += __shfl_xor(sum.x, d);
-    sum.y += __shfl_xor(sum.y, d);
-    sum.z += __shfl_xor(sum.z, d);
-    sum.w += __shfl_xor(sum.w, d);
-  }
-  if constexpr (W > 1) {
-    if (lane < LANES) sums[wave][lane] = sum;
-    totals[wave] = total;
-    __syncthreads();
-    if (wave > 0 || lane >= LANES) return;
-    sum = sums[0][lane];
-#pragma unroll
-    for (int i = 1; i < W; ++i) {
-      const float4 y = sums[i][lane];
-      sum.x += y.x;
-      sum.y += y.y;
-      sum.z += y.z;
-      sum.w += y.w;
-      total += totals[i];
+    for (int d = 32; d >= LANES; d >>= 1) {
+      sum.x += __shfl_xor(sum.x, d);
+      sum.y += __shfl_xor(sum.y, d);
+      sum.z += __shfl_xor(sum.z, d);
+      sum.w += __shfl_xor(sum.w, d);
     }
-  }
-  if (lane >= LANES) return;
-  const float inv = total > 0.0f ? 1.0f / total : total;
-  store_4(out + row * D + c, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
-  if (lane == 0 && lse != nullptr) {
-    const float base = top == -INFINITY ? 0.0f : top;
-    lse[row] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    if constexpr (W > 1) {
+      if (lane < LANES) sums[wave][lane] = sum;
+      totals[wave] = total;
+      __syncthreads();
+      if (wave > 0 || lane >= LANES) return;  // R is 1
+      sum = sums[0][lane];
+#pragma unroll
+      for (int i = 1; i < W; ++i) {
+        const float4 y = sums[i][lane];
+        sum.x += y.x;
+        sum.y += y.y;
+        sum.z += y.z;
+        sum.w += y.w;
+        total += totals[i];
+      }
+    }
+    if (lane < LANES) {
+      const float inv = total > 0.0f ? 1.0f / total : total;
+      store_4(out + row * D + c, make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+    }
+    if (lane == 0 && lse != nullptr) {
+      const float base = top == -INFINITY ? 0.0f : top;
+      lse[row] = total == 0.0f ? -INFINITY : (base + __builtin_amdgcn_logf(total)) * kLn2;
+    }
   }
 }
 
@@ -1262,12 +1260,14 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1) {
-    constexpr int all = kThreads / 64;
-    const bool wide = g.splits > 8;  // more than 64 parts only where the rows are few
-    e = seq_launch(wide              ? (const void*)&mx_join_kernel<T, D, all, 8>
-                   : g.splits > 4    ? (const void*)&mx_join_kernel<T, D, 1, 4>
-                                     : (const void*)&mx_join_kernel<T, D, 1, 2>,
-                   wide ? rows : (rows + all - 1) / all, kThreads, 0, s, rows, g.splits,
+    // more than 64 parts only where the rows are few
+    constexpr int waves = kThreads / 64, look = 8;
+    const bool many = rows > 16384, wide = !many && g.splits > 8;
+    const int each = many ? waves * look : wide ? 1 : waves;
+    e = seq_launch(many   ? (const void*)&mx_join_kernel<T, D, 1, 2, look>
+                   : wide ? (const void*)&mx_join_kernel<T, D, waves, 8, 1>
+                          : (const void*)&mx_join_kernel<T, D, 1, 4, 1>,
+                   (rows + each - 1) / each, kThreads, 0, s, rows, g.splits,
                    (const float*)part_o, (const float*)part_l, out, lse);
   }
   return e;
@@ -1293,7 +1293,7 @@ hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache
 }  // namespace
 
 void set_plan_mx(PagedGeometry& g, int bits) {
-  const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv);
+  const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv, g.D);
   g.tile = p.tile;
   g.splits = p.splits;
   g.part = p.part;

@@ -67,27 +67,38 @@ struct MxPlan {
   int64_t bound;     // and are at most this many per key head
 };
 
-// Rows per workgroup: 16 where the requests have no more on average, else as paged_plan.  Parts of
-// many rows: as paged_plan.  Of few rows: up to 64 requests' keys are divided on the GPU, by all
-// their lengths (more requests fill the card without), into parts of at least 512 keys (256: single
-// tokens of 64 requests 111 and 112 us, drafts of 5 tokens of 16 20.0 and 22.3, 12 biased ones
-// 21.0 and 22.0) and as many as there are workgroups at a time:
-//  - few requests, whose parts are equally long: what the card holds at once, two workgroups per
-//    compute unit (four requests of 31,000 to 120,000 tokens, 16 / 2 heads, 4 bits: 24 us in 512
-//    parts, 28 in 384, 29 in 768);
-//  - else three per compute unit, of which the longest go first (single tokens of 64 requests, 32 /
-//    8 heads, 8 bits: 120 us in 512, 111 in 768, 113 in 1,280; 4 bits 74, 67, 67).
-inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv) {
+// Rows per workgroup: 16 where the requests have no more on average, else as paged_plan.  Up to 64
+// requests' keys are divided on the GPU, by all their lengths (more requests fill the card
+// without), into parts of at least 512 keys (256: single tokens of 64 requests 111 and 112 us,
+// drafts of 5 tokens of 16 20.0 and 22.3, 12 biased ones 21.0 and 22.0), as many as there are
+// workgroups at a time:
+//  - two per compute unit, where few requests have parts of one length (four requests of 31,000 to
+//    120,000 tokens, 16 / 2 heads, 4 bits: 24 us in 512 parts, 28 in 384, 29 in 768) and for many
+//    rows, whose partial results cost most;
+//  - else three, of which the longest go first (single tokens of 64 requests, 32 / 8 heads, 8 bits:
+//    120 us in 512, 111 in 768, 113 in 1,280; 4 bits 74, 67, 67).
+// The workspace has room for all parts of all rows: for many rows at most 16, and 512 MiB unless
+// paged_plan had more.
+inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv,
+                            int head_dim) {
   const PagedPlan q = paged_plan(tokens, group, kv_heads, batch, max_kv);
-  MxPlan p = {q.tile, q.splits, q.part, 0, 0};
-  if (q.tile != kFewRows) return p;
-  if (tokens * group <= (int64_t)16 * batch) p.tile = 16;
+  const int64_t rows = tokens * group;
+  MxPlan p = {rows <= (int64_t)16 * batch ? 16 : q.tile, q.splits, q.part, 0, 0};
   if (batch > kDealt) return p;
   p.part = kLeastPartMx;
-  const int64_t slots = tokens * group / p.tile + batch + 1, all = slots * kv_heads;
-  p.target = (int)std::max<int64_t>(1, (all <= 64 ? 512 - all : 768) / kv_heads);
+  const int64_t slots = rows / p.tile + batch + 1, all = slots * kv_heads;
+  const bool few = q.tile == kFewRows;
+  p.target = (int)std::max<int64_t>(
+      1, (!few ? 512 : all <= 64 ? 512 - all : 768) / kv_heads);
+  const int64_t room = (int64_t)512 << 20, each = std::max<int64_t>(1, rows) * kv_heads * head_dim * 4;
+  int64_t most =
+      few ? kMostPartsMx : std::max<int64_t>(q.splits, std::min<int64_t>(16, room / each));
+  if (batch == 1) {  // ceil(keys / part), part >= tiles keys / target
+    const int64_t tiles = std::max<int64_t>(1, (rows + p.tile - 1) / p.tile);
+    most = std::min(most, (p.target + tiles - 1) / tiles);
+  }
   p.splits = (int)std::max<int64_t>(
-      1, std::min<int64_t>({max_kv / p.part, p.target + 1, kMostPartsMx}));
+      1, std::min<int64_t>({max_kv / p.part, p.target + 1, most}));
   // sum of ceil(keys / part) <= target + one per tile; 8 for the rounding of the GPU's sum
   p.bound = std::min<int64_t>(slots * p.splits, slots + p.target + 8);
   return p;
