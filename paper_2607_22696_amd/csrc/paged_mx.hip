@@ -46,16 +46,14 @@ __device__ inline uint4 eight(uint32_t u, float power) {
                     __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d));
 }
 
-// W words of elements of one key: CH = W 32 / BITS channels from a block's border on, or half a
-// block, with a byte of scales per block.
+// A quarter of a key's or value's channels, a block or half of one, as W words of elements and the
+// block's scale.
 template <int BITS, int W>
-struct Piece {
-  static constexpr int kEights = W * 4 / BITS;  // chunks of 8 channels
-  static constexpr int kBlocks = (kEights + 3) / 4;
+struct Quarter {
   uint32_t w[W];
-  // As narrow as in memory: widened where they are loaded, they are widened again at the end of a
-  // loop that they are carried over, which waits for them there.
-  typename std::conditional<kBlocks == 2, uint16_t, uint8_t>::type scales;
+  // As narrow as in memory: widened where it is loaded, it is widened again at the end of a loop
+  // that it is carried over, which waits for it there.
+  uint8_t scale;
 
   __device__ inline void load(const uint8_t* at, const uint8_t* scale_at) {
     if constexpr (W >= 4) {
@@ -65,20 +63,13 @@ struct Piece {
     } else {
       *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(at);
     }
-    if constexpr (kBlocks == 2)
-      scales = *reinterpret_cast<const uint16_t*>(scale_at);
-    else
-      scales = *scale_at;
+    scale = *scale_at;
   }
-  __device__ inline float power(int chunk) const {
-    if constexpr (kBlocks == 1) return power_of(scales);
-    return power_of(scales >> (8 * (chunk / 4)) & 255u);
-  }
-  __device__ inline uint4 eight_at(int chunk) const {
+  __device__ inline uint4 eight_at(int chunk) const {  // channels 8 chunk .. + 7 of the quarter
     if constexpr (BITS == 8)
-      return eight(w[2 * chunk], w[2 * chunk + 1], power(chunk));
+      return eight(w[2 * chunk], w[2 * chunk + 1], power_of(scale));
     else
-      return eight(w[chunk], power(chunk));
+      return eight(w[chunk], power_of(scale));
   }
 };
 
@@ -201,8 +192,8 @@ struct Deal {
 // request's tiles over the same part follow each other, the last (under a causal mask the longest)
 // first.  More requests as they lie, in parts that the host chose.  (A chunk of 400 of 30,000
 // tokens before 40 of 100 of 700, 32 / 8 heads: 784 us as they lie in parts chosen without the
-// lengths, 712 longest first, 318 divided; chunks
-// of 512, 801 and 300 of 16,000, 801 and 5,000 tokens beside three single ones 235 and 215.)
+// lengths, 712 longest first, 318 divided; chunks of 512, 801 and 300 of 16,000, 801 and 5,000
+// tokens beside three single ones 235 and 215.)
 template <int ROWS>
 __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
                             Deal& d) {
@@ -223,7 +214,7 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
   for (int x = 32; x > 0; x >>= 1) all += __shfl_xor(all, x);
   const float share = fminf(all / (float)g.target, (float)(1 << 30));
   const int most = max(((int)share + STEP) / STEP * STEP, g.part);  // more than a share
-  const int parts = min(max((h.keys + most - 1) / most, 1), g.splits);
+  const int parts = min(max(h.keys / most + (h.keys % most != 0), 1), g.splits);
   const int len = ((h.keys + parts - 1) / parts + STEP - 1) / STEP * STEP;
   int r;
   const int l = lane_of(index, h.tiles * parts, min((int)((int64_t)len * 4 / (most + 1)), 3), r);
@@ -235,6 +226,7 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
     d.parts = __builtin_amdgcn_readlane(parts, l);
     d.split = r / tiles;
     tile = tiles - 1 - (r - d.split * tiles);
+    if (d.split >= d.parts) return false;  // only where offsets decrease
   }
   if (!span_of<ROWS>(g, h, l, tile, s)) return false;
   s.only = d.parts == 1;
@@ -249,6 +241,7 @@ __device__ inline float plus_both(float x, uint32_t y) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, y),
                                          __builtin_bit_cast(bf16x2_t, 0x3f803f80u), x, false);
 }
+
 // 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
 // elements are loaded two tiles ahead, converted once for all four waves, and the products of the
 // next 32 keys run beside the softmax of these.
@@ -257,8 +250,8 @@ __device__ inline float plus_both(float x, uint32_t y) {
 // the rounded ones (lse is that of the others): where one key has most of a row, its rounding then
 // cancels.  Outputs are off by 1.3 times what their own rounding alone makes (0.0021 of their size
 // against 0.0016).  Two bf16 parts of alpha would leave that rounding alone, as in the form with
-// few rows, which waits for memory; here they cost half as many products again: chunks of 512, 801
-// and 300 tokens beside three single ones 280 us instead of 226.
+// 16 rows, which waits for memory; here they cost half as many products again: chunks of 512, 801
+// and 300 tokens beside three single ones took 280 us with them and 230 without.
 template <typename T, int D, int BITS, bool BIAS>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
@@ -271,7 +264,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   constexpr int KT = 64, RB = D * BITS / 8, SB = D / 32;
   using Tl = Tile<uint16_t, D, KT>;
   using Frag = typename Type<T>::Frag;
-  using Quarter = Piece<BITS, RB / 16>;  // four lanes share a key
+  using Part = Quarter<BITS, RB / 16>;  // four lanes share a key
   constexpr int KS = D / 16, DB = D / 32, NB = KT / 32, E = Tl::kElems;
   __shared__ __attribute__((aligned(16))) uint16_t lds[4 * E];  // keys, values; twice
   __shared__ __attribute__((aligned(8))) uint16_t there[2][4];
@@ -298,7 +291,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   auto page_of = [&](int kt) {
     return my_pages[div_by((uint32_t)key_of(kt), g.page_mul, g.page_shift)];
   };
-  Quarter kq, vq;
+  Part kq, vq;
   auto load = [&](int kt, int p) {  // returns which of the wave's keys have a place
     const int j = key_of(kt), page = div_by((uint32_t)j, g.page_mul, g.page_shift);
     const bool ok = (uint32_t)p < (uint32_t)g.num_pages;
@@ -579,11 +572,16 @@ __device__ inline bf16x8_t value_cols(const uint16_t* lds, int d0) {
 }
 
 // 16 RT rows per workgroup; its waves share out the keys in groups of 64 and read them each for
-// itself, without a barrier until the end.  Half a group at a time, lane l has a quarter of the
-// channels of keys l % 16 and 16 + l % 16, which is the keys' operand (the contraction's order is
-// free as long as the queries have it too).  Values pass through 32 rows of LDS that are the
-// wave's own, to be read transposed.  The places of the next group's keys are looked up one group
-// ahead, a key per lane, and its elements loaded half a group ahead.
+// itself, without a barrier until the end.  Lane l has a quarter of the channels of a group's keys
+// 16 i + l % 16, which is the keys' operand (the contraction's order is free as long as the queries
+// have it too).  Values pass, 32 keys at a time, through LDS that is the wave's own, to be read
+// transposed.  The places of the next group's keys are looked up one group ahead, a key per lane,
+// and its elements loaded as soon as this one's are converted.
+//
+// What bounds it is memory: single tokens of 64 requests, 32 / 8 heads x 128, read 554 MB in 8 bits
+// in 104 us (5.3 TB/s; a copy reaches 4.9) and 286 MB in 4 bits in 56 us (5.1 TB/s; conversions
+// issue 42% of the vector instructions' time).  Small calls wait for a chain: offsets and lengths,
+// page numbers, elements, then 1.5 us per group.
 template <typename T, int D, int BITS, bool BIAS, int RT>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 4)))
@@ -600,10 +598,11 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   constexpr int KB = D == 128 && BITS == 8 && (RT == 2 || sizeof(T) == 4) ? 32 : 64, NI = KB / 16;
   constexpr uint64_t kAll = ~0ull >> (64 - KB);
   using Frag = typename Type<T>::Frag;
-  // With two blocks of rows alpha is rounded to bf16, as in the form with many rows.
+  // With two blocks of rows alpha is rounded to bf16, as in the form with many rows (64 requests
+  // with 6 new tokens in 4 bits: 102 us with two parts of it, 95 so).
   constexpr bool ROUND = RT > 1 && sizeof(T) == 2;
   using AFrag = typename std::conditional<ROUND, bf16x8_t, typename Alpha<T>::Frag>::type;
-  using Quarter = Piece<BITS, RB / 16>;
+  using Part = Quarter<BITS, RB / 16>;
   constexpr int KS = D / 32, DC = D / 16, E = 32 * D;
   // each wave's half group of values; at the end the waves' results of 16 rows in float32
   __shared__ __attribute__((aligned(16))) uint16_t lds[WAVES * E];
@@ -630,7 +629,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         qw[rt][ks][i] = reinterpret_cast<const uint4*>(from)[i];
     }
   }
-  const int first = s.k_lo + wave * KB;  // this wave's groups: first, first + 256, ...
+  const int first = s.k_lo + wave * KB;  // this wave's groups: first, first + 4 KB, ...
   const int groups = s.k_hi > first ? (s.k_hi - first + WAVES * KB - 1) / (WAVES * KB) : 0;
   // Key `lane` of group i, those past the last key repeat it, to be masked: its page number and,
   // from that, its row among all pages' rows, handed to the lanes that load it.  Returns which keys
@@ -647,7 +646,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     quarters((uint32_t)(row >> 32), hi);
     return (uint64_t)__ballot(ok) & kAll;
   };
-  Quarter kq[NI], vq[NI];  // of keys 16 i + col of a group
+  Part kq[NI], vq[NI];  // of keys 16 i + col of a group
   auto row_of_key = [](const uint32_t (&lo)[4], const uint32_t (&hi)[4], int i) {
     return (int64_t)((uint64_t)hi[i] << 32 | lo[i]);
   };

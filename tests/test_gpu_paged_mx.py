@@ -262,6 +262,9 @@ LONGER = {
     "65_requests": dict(new=[1] * 65, held=[1 + 37 * b % 1900 for b in range(65)]),
     "none_of_64": dict(new=[0, 1] * 32, held=[(53 * b) % 700 for b in range(64)], tail=5),
     "many_parts": dict(new=[1, 1], held=[70000, 2001], H=2, KH=1, D=128, page=100),
+    "drafts_128": dict(new=[6, 5, 0, 7, 6, 3], held=[3000, 700, 50, 65, 2100, 33], D=128),
+    "drafts_64": dict(new=[6, 5, 0, 7, 6, 3], held=[3000, 700, 50, 65, 2100, 33], page=24),
+    "chunks_in_parts": dict(new=[100, 3, 1, 40], held=[9000, 700, 2600, 41], KH=1, H=4, D=128),
     "tiles_and_parts": dict(new=[9, 1, 40] + [1] * 13, held=[3000, 5000, 1200] + [20] * 13, KH=1),
 }
 
@@ -282,7 +285,7 @@ def test_attention(name, dtype, bits):
 @pytest.mark.parametrize("bits,D", ((8, 128), (4, 64)))
 @pytest.mark.parametrize("dtype", ("bf16", "f32"))
 @pytest.mark.parametrize("new,bias", [([1, 1, 2], (32, 128, False)), ([150, 3, 60], (32, 128, True)),
-                                      ([1, 4, 1], (6, 5, True))])
+                                      ([1, 4, 1], (6, 5, True)), ([6, 5, 7], (32, 128, False))])
 def test_bias(new, bias, dtype, bits, D):
     Case(50 + len(new), new, [900, 40, 200], bias=bias, dtype=dtype, D=D, bits=bits).check()
 
@@ -355,6 +358,16 @@ def test_a_block_that_is_not_finite(new, dtype):
         assert torch.isnan(hit).all()
         if which == 0:
             assert torch.isnan(lse[:n, 2:]).all()
+
+
+@pytest.mark.parametrize("new", ([1, 1, 2], [70, 1, 20]))
+def test_requests_that_share_pages(new):
+    """A common beginning is held once; a page may stand twice in a table."""
+    c = Case(64, new, [300, 200, 180], H=8, KH=2, D=128, bits=4)
+    c.pages[1, :6] = c.pages[0, :6]
+    c.pages[2, :6] = c.pages[0, :6]
+    c.pages[2, 7] = c.pages[2, 6]
+    c.check()
 
 
 def test_every_page_bad():
