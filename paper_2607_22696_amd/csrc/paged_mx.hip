@@ -282,17 +282,21 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   Frag qf[KS];
   load_frag<T, D>(qf, q + x.q_at, x.ok);
 
-  // A wave has 16 keys of a tile, a quarter of the channels per lane: 16 lanes write one chunk of 16
-  // rows to LDS, which meet in no bank.  Keys past the last repeat it, to be masked; one without a
-  // place has the first page's first row, to be cleared.
-  const int key = wave * 16 + (lane & 15), part = lane >> 4;
+  // A wave has 16 keys of a tile, a quarter of the channels per lane, in an order in which the chunks
+  // that 8 lanes write to LDS meet in no bank.  Keys past the last repeat it, to be masked; one
+  // without a place has the first page's first row, to be cleared.
+  auto key_of_lane = [](int l) {
+    return D == 128 ? (l & 1) | (l >> 3 & 1) << 1 | (l >> 1 & 3) << 2
+                    : (l >> 3 & 1) | (l & 7) << 1;
+  };
+  const int key = wave * 16 + key_of_lane(lane & 15), part = lane >> 4;
   const int32_t* my_pages = pages + (int64_t)s.b * g.max_pages;
   auto key_of = [&](int kt) { return min(s.k_lo + kt * KT + key, s.k_hi - 1); };
   auto page_of = [&](int kt) {
     return my_pages[div_by((uint32_t)key_of(kt), g.page_mul, g.page_shift)];
   };
   Part kq, vq;
-  auto load = [&](int kt, int p) {  // returns which of the wave's keys have a place
+  auto load = [&](int kt, int p) {  // returns which of the wave's keys have a place, by lane
     const int j = key_of(kt), page = div_by((uint32_t)j, g.page_mul, g.page_shift);
     const bool ok = (uint32_t)p < (uint32_t)g.num_pages;
     const int64_t row =
@@ -310,13 +314,18 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       *reinterpret_cast<uint4*>(to + at) = kq.eight_at(i);
       *reinterpret_cast<uint4*>(to + E + at) = vq.eight_at(i);
     }
-    if (ok != 0xffffu && (ok >> (lane & 15) & 1) == 0) {
+    uint32_t by_key = ok;
+    if (ok != 0xffffu) {
+      if ((ok >> (lane & 15) & 1) == 0) {
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        *reinterpret_cast<uint4*>(to + E + Tl::at(key, part * (D / 4) + 8 * i)) =
-            make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < D / 32; ++i)
+          *reinterpret_cast<uint4*>(to + E + Tl::at(key, part * (D / 4) + 8 * i)) =
+              make_uint4(0, 0, 0, 0);
+      }
+      by_key = 0;
+      for (int i = 0; i < 16; ++i) by_key |= (ok >> i & 1) << key_of_lane(i);
     }
-    if (lane == 0) there[buf][wave] = (uint16_t)ok;
+    if (lane == 0) there[buf][wave] = (uint16_t)by_key;
   };
   uint32_t ok1 = 0;  // of the tile in kq and vq
   int next_page = 0;
@@ -548,12 +557,11 @@ __device__ inline float sum_of(float x) {
 }
 
 // A wave's 32 rows of values in LDS: chunks of 8 channels XOR-permuted by the row, so that neither
-// the writes (one chunk of 16 consecutive rows) nor the transposing reads (two neighbouring chunks
-// of 8 consecutive rows) meet in a bank.
+// the writes (one chunk of 8 consecutive rows at a time, over 128 bytes of banks) nor the transposing
+// reads (two neighbouring chunks of 8 consecutive rows, over 256) meet in a bank.
 template <int D>
 __device__ inline int value_at(int row, int chan) {
-  const int f = D == 128 ? (row & 7) << 1 | (row >> 3 & 1)
-                         : (row >> 1 & 3) << 1 | (row >> 3 & 1);
+  const int f = D == 128 ? (row & 7) << 1 | (row >> 2 & 1) : row & 7;
   return row * D + (((chan >> 3) ^ f) << 3) + (chan & 7);
 }
 // Channels d0 .. d0 + 15 as rows, over the 32 keys in the order in which two results hold them:
