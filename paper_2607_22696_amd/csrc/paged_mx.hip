@@ -1267,9 +1267,9 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
                             cu_q, table, map, out, lse, part_o, part_l);
   if (e == hipSuccess && g.splits > 1) {
-    // more than 64 parts only where the rows are few
     constexpr int waves = kThreads / 64, look = 8;
-    const bool many = rows > 16384, wide = !many && g.splits > 8;
+    const bool many = rows > 16384 && g.splits <= 64;  // one wave has no more parts
+    const bool wide = !many && g.splits > 8;
     const int each = many ? waves * look : wide ? 1 : waves;
     e = seq_launch(many   ? (const void*)&mx_join_kernel<T, D, 1, 2, look>
                    : wide ? (const void*)&mx_join_kernel<T, D, waves, 8, 1>

@@ -8,7 +8,7 @@ import torch
 
 from oracle import mx
 from oracle import sequence as ref
-from tests.seq_util import TYPES, Bounds, near, rounded
+from tests.seq_util import E32, TYPES, Bounds, near, rounded
 
 import paper_2607_22696_amd as dsa
 
@@ -264,6 +264,7 @@ LONGER = {
     "many_parts": dict(new=[1, 1], held=[70000, 2001], H=2, KH=1, D=128, page=100),
     "drafts_128": dict(new=[6, 5, 0, 7, 6, 3], held=[3000, 700, 50, 65, 2100, 33], D=128),
     "drafts_64": dict(new=[6, 5, 0, 7, 6, 3], held=[3000, 700, 50, 65, 2100, 33], page=24),
+    "66_chunks": dict(new=[30] * 66, held=[30 + 31 * b for b in range(66)], KH=1, H=4),
     "chunks_in_parts": dict(new=[100, 3, 1, 40], held=[9000, 700, 2600, 41], KH=1, H=4, D=128),
     "tiles_and_parts": dict(new=[9, 1, 40] + [1] * 13, held=[3000, 5000, 1200] + [20] * 13, KH=1),
 }
@@ -368,6 +369,24 @@ def test_requests_that_share_pages(new):
     c.pages[2, :6] = c.pages[0, :6]
     c.pages[2, 7] = c.pages[2, 6]
     c.check()
+
+
+@pytest.mark.parametrize("new,H,KH", (([1] * 64, 288, 9), ([1, 1], 2, 1), ([40], 4, 1)))
+def test_a_long_text_of_repeated_pages(new, H, KH):
+    """204,800 tokens that stand in 16 pages, 800 times each: attention is that over 256 tokens, lse
+    larger by log 800.  More parts than a wave has lanes, also where there are many rows to join."""
+    held = [256] + [5] * (len(new) - 1)
+    c = Case(65, new, held, H=H, KH=KH, bits=4, causal=False)
+    o, l, out_bound, lse_bound = c.want()
+    more = 800 * 256 * E32  # the terms of the sums
+    one = c.pages[0, :16]
+    c.pages = np.concatenate([c.pages, np.full((len(new), 800 * 16 - c.pages.shape[1]), -1)], 1)
+    c.pages[0], c.held = np.tile(one, 800), [800 * 256] + held[1:]
+    out, lse = c.run()
+    l[:new[0]] += np.log(800)
+    mag = np.abs(c.v64[c.pages[0, :16]]).max()
+    near("out", out, o, out_bound + 2 * more * mag)
+    near("lse", lse, l, lse_bound + 2 * more + np.abs(l) * 4 * E32)
 
 
 def test_every_page_bad():
