@@ -1269,7 +1269,7 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
   if (e == hipSuccess && g.splits > 1) {
     constexpr int waves = kThreads / 64, look = 8;
     const bool many = rows > 16384 && g.splits <= 64;  // one wave has no more parts
-    const bool wide = !many && g.splits > 8;
+    const bool wide = !many && g.splits > 16;  // single tokens of 64 requests: 112.6 us, 111 so
     const int each = many ? waves * look : wide ? 1 : waves;
     e = seq_launch(many   ? (const void*)&mx_join_kernel<T, D, 1, 2, look>
                    : wide ? (const void*)&mx_join_kernel<T, D, waves, 8, 1>
