@@ -66,9 +66,8 @@ size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32
 
 /* Attention of the new tokens over the pages: out [total_q][heads][head_dim] and, when not NULL,
  * lse.  Keys and values enter the products as the bf16 numbers that they are; float32 queries and
- * alpha are made of bf16 parts, to 2^-24 of a product.  With bf16, alpha has 16 bits where requests
- * have 16 rows (new tokens times heads of a group) or fewer on average, else it is rounded to
- * bf16 and the result divided by the sum of the rounded. */
+ * alpha are made of bf16 parts, to 2^-24 of a product.  With bf16 queries alpha is made of two, to
+ * 2^-17 of itself. */
 dsa3d_status dsa3d_paged_forward_mx(const dsa3d_paged_desc* desc, const void* q,
                                     const dsa3d_mx_cache* cache, const int32_t* pages,
                                     const int32_t* kv_lens, const int32_t* cu_q,

@@ -73,9 +73,49 @@ struct Quarter {
   }
 };
 
-// The products of exact bf16 keys and values with queries and alpha, float32 ones in three parts.
+// Alpha as an operand: 16 bits of it as two bf16 numbers, or a float32's three parts.  (One bf16
+// number of it, the results divided by the sum of the rounded, takes less where products are the
+// time, chunks of 512, 801 and 300 tokens beside three single ones 206 us instead of 257, and 64
+// requests with 6 new tokens in 4 bits 86 instead of 93; but outputs are then off by 0.0020 to
+// 0.0021 of their size instead of the 0.0016 that their own rounding makes.)
+struct Two {
+  bf16x8_t h, l;
+};
+template <typename T>
+struct Alpha;
+template <>
+struct Alpha<uint16_t> {
+  using Frag = Two;
+  static __device__ inline Two of(const float* x) {
+    uint32_t h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y[2] = {x[2 * i], x[2 * i + 1]};
+      h[i] = take_part(y);
+      l[i] = take_part(y);
+    }
+    return {as_bf16x8(make_uint4(h[0], h[1], h[2], h[3])),
+            as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]))};
+  }
+};
+template <>
+struct Alpha<float> {
+  using Frag = Split;
+  static __device__ inline Split of(const float* x) {
+    F32x8 y;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y.x[e] = x[e];
+    return seq::split(y);
+  }
+};
+
+// The products of exact bf16 keys and values with queries and alpha, which may be of parts.
 __device__ inline f32x16_t times(const bf16x8_t& a, const bf16x8_t& b, const f32x16_t& c) {
   return mfma(a, b, c);
+}
+__device__ inline f32x16_t times(const bf16x8_t& a, const Two& b, f32x16_t c) {
+  c = mfma(a, b.l, c);
+  return mfma(a, b.h, c);
 }
 __device__ inline f32x16_t times(const bf16x8_t& a, const Split& b, f32x16_t c) {
   c = mfma(a, b.l, c);
@@ -236,22 +276,9 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
 
 // ------------------------------------------------------------------------- many rows
 
-// x + y.0 + y.1, the two bf16 numbers of a word.
-__device__ inline float plus_both(float x, uint32_t y) {
-  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, y),
-                                         __builtin_bit_cast(bf16x2_t, 0x3f803f80u), x, false);
-}
-
 // 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
 // elements are loaded two tiles ahead, converted once for all four waves, and the products of the
 // next 32 keys run beside the softmax of these.
-//
-// With bf16, alpha enters its products rounded to bf16, and the results are divided by the sum of
-// the rounded ones (lse is that of the others): where one key has most of a row, its rounding then
-// cancels.  Outputs are off by 1.3 times what their own rounding alone makes (0.0021 of their size
-// against 0.0016).  Two bf16 parts of alpha would leave that rounding alone, as in the form with
-// 16 rows, which waits for memory; here they cost half as many products again: chunks of 512, 801
-// and 300 tokens beside three single ones took 280 us with them and 230 without.
 template <typename T, int D, int BITS, bool BIAS>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
@@ -347,23 +374,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 #pragma unroll
   for (int db = 0; db < DB; ++db) o[db] = f32x16_t{};
   Softmax sm;
-  float divide = 0.0f;  // the sum of the rounded alphas
   const float scale = BIAS ? 1.0f : g.scale_log2;
-  auto raise_to = [&](const float (&y)[16]) {  // Softmax::raise_to with that sum
-    float mx = fmaxf(fmaxf(y[0], y[1]), y[2]);
-#pragma unroll
-    for (int i = 3; i < 16; ++i) mx = fmaxf(mx, y[i]);
-    mx = pair_max(mx) * scale;  // scale > 0
-    const bool raise = mx > sm.top + kSlack;
-    if (__any(raise)) {
-      const float corr = raise ? __builtin_amdgcn_exp2f(sm.top - mx) : 1.0f;
-      if (raise) sm.top = sm.base = mx;
-      sm.l *= corr;
-      divide *= corr;
-#pragma unroll
-      for (int db = 0; db < DB; ++db) o[db] *= corr;
-    }
-  };
   auto products = [&](const uint16_t* kc, int b) {
     f32x16_t acc = f32x16_t{};
 #pragma unroll
@@ -382,15 +393,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     }
   };
   auto accumulate = [&](const uint16_t* vc, int b, const float (&y)[16]) {
-    Frag pf[2];
-    to_frags(y, pf);
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const uint4 u = __builtin_bit_cast(uint4, pf[p]);
-        divide = plus_both(plus_both(plus_both(plus_both(divide, u.x), u.y), u.z), u.w);
-      }
-    }
+    const typename Alpha<T>::Frag pf[2] = {Alpha<T>::of(y), Alpha<T>::of(y + 8)};
 #pragma unroll
     for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -422,7 +425,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
           for (int i = 0; i < 16; ++i) y[i] = next[i];
           mask(y, s.k_lo + kt * KT + b * 32,
                __builtin_amdgcn_readfirstlane(b == 0 ? bits.x : bits.y));
-          raise_to(y);
+          sm.raise_to(y, scale, o);
         }
         if (MORE && b == NB - 1) __syncthreads();  // the next tile is in LDS
         if constexpr (LIVE) {
@@ -454,8 +457,8 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     if (live) run(std::true_type());
     else run(std::false_type());
   }
-  const float ltot = pair_sum(sm.l), by = sizeof(T) == 2 ? pair_sum(divide) : ltot;
-  const float inv = by > 0.0f ? 1.0f / by : by;
+  const float ltot = pair_sum(sm.l);
+  const float inv = ltot > 0.0f ? 1.0f / ltot : ltot;
   const float l2 = ltot == 0.0f ? -INFINITY : sm.base + __builtin_amdgcn_logf(ltot);
   if (!x.ok) return;
   if (s.only) {
@@ -485,10 +488,6 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 __device__ inline f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
-// alpha's operand: 16 bits of it, as two bf16 numbers, or a float32's three parts.
-struct Two {
-  bf16x8_t h, l;
-};
 __device__ inline f32x4_t times(const bf16x8_t& a, const bf16x8_t& b, const f32x4_t& c) {
   return mfma16(a, b, c);
 }
@@ -501,33 +500,6 @@ __device__ inline f32x4_t times(const bf16x8_t& a, const Split& b, f32x4_t c) {
   c = mfma16(a, b.m, c);
   return mfma16(a, b.h, c);
 }
-template <typename T>
-struct Alpha;
-template <>
-struct Alpha<uint16_t> {
-  using Frag = Two;
-  static __device__ inline Two of(const float* x) {
-    uint32_t h[4], l[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[2] = {x[2 * i], x[2 * i + 1]};
-      h[i] = take_part(y);
-      l[i] = take_part(y);
-    }
-    return {as_bf16x8(make_uint4(h[0], h[1], h[2], h[3])),
-            as_bf16x8(make_uint4(l[0], l[1], l[2], l[3]))};
-  }
-};
-template <>
-struct Alpha<float> {
-  using Frag = Split;
-  static __device__ inline Split of(const float* x) {
-    F32x8 y;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) y.x[e] = x[e];
-    return seq::split(y);
-  }
-};
 
 // x of the lanes 16 s .. 16 s + 15 in all four quarters, s = 0 .. 3.
 __device__ inline void quarters(uint32_t x, uint32_t (&y)[4]) {
@@ -606,15 +578,11 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   constexpr int KB = D == 128 && BITS == 8 && (RT == 2 || sizeof(T) == 4) ? 32 : 64, NI = KB / 16;
   constexpr uint64_t kAll = ~0ull >> (64 - KB);
   using Frag = typename Type<T>::Frag;
-  // With two blocks of rows alpha is rounded to bf16, as in the form with many rows (64 requests
-  // with 6 new tokens in 4 bits: 102 us with two parts of it, 95 so).
-  constexpr bool ROUND = RT > 1 && sizeof(T) == 2;
-  using AFrag = typename std::conditional<ROUND, bf16x8_t, typename Alpha<T>::Frag>::type;
   using Part = Quarter<BITS, RB / 16>;
   constexpr int KS = D / 32, DC = D / 16, E = 32 * D;
   // each wave's half group of values; at the end the waves' results of 16 rows in float32
   __shared__ __attribute__((aligned(16))) uint16_t lds[WAVES * E];
-  __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS], divides[WAVES][ROUND ? ROWS : 1];
+  __shared__ float tops[WAVES][ROWS], totals[WAVES][ROWS];
   extern __shared__ float bias[];
 
   Deal w;
@@ -703,11 +671,11 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       min(g.causal ? min(s.seen - 1, s.off + div_by(s.r0, g.group_mul, g.group_shift))
                    : s.seen - 1, s.k_hi - 1);
   f32x4_t o[RT][DC];
-  float top[RT], base[RT], sum[RT], divide[RT];
+  float top[RT], base[RT], sum[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     top[rt] = -INFINITY;
-    base[rt] = sum[rt] = divide[rt] = 0.0f;
+    base[rt] = sum[rt] = 0.0f;
 #pragma unroll
     for (int dc = 0; dc < DC; ++dc) o[rt][dc] = f32x4_t{};
   }
@@ -737,7 +705,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     // wait at the loop's end.
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (MORE) load_keys(lo, hi);
-    AFrag pf[RT][NI / 2];
+    typename Alpha<T>::Frag pf[RT][NI / 2];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       // element e is key kb + 16 (e / 4) + 4 quarter + e % 4
@@ -773,7 +741,6 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         const float corr = raise ? __builtin_amdgcn_exp2f(top[rt] - mx) : 1.0f;
         if (raise) top[rt] = base[rt] = mx;
         sum[rt] *= corr;
-        divide[rt] *= corr;
 #pragma unroll
         for (int dc = 0; dc < DC; ++dc) o[rt][dc] *= corr;
       }
@@ -783,16 +750,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         sum[rt] += t[e];
       }
 #pragma unroll
-      for (int i = 0; i < NI / 2; ++i) {
-        if constexpr (ROUND) {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) pf[rt][i][e] = (__bf16)t[8 * i + e];
-          const uint4 u = __builtin_bit_cast(uint4, pf[rt][i]);
-          divide[rt] = plus_both(plus_both(plus_both(plus_both(divide[rt], u.x), u.y), u.z), u.w);
-        } else {
-          pf[rt][i] = Alpha<T>::of(t + 8 * i);
-        }
-      }
+      for (int i = 0; i < NI / 2; ++i) pf[rt][i] = Alpha<T>::of(t + 8 * i);
     }
 #pragma unroll
     for (int half = 0; half < NI / 2; ++half) {
@@ -850,11 +808,10 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const float total = sum_of(sum[rt]), by = ROUND ? sum_of(divide[rt]) : total;
+    const float total = sum_of(sum[rt]);
     if (quarter == 0) {
       tops[wave][16 * rt + col] = top[rt];
       totals[wave][16 * rt + col] = total;
-      if (ROUND) divides[wave][16 * rt + col] = by;
     }
   }
   __syncthreads();
@@ -881,14 +838,13 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
     for (int e = threadIdx.x; e < min(count - 16 * rt, 16) * (D / 4); e += kThreads) {
       const int r = e / (D / 4), chunk = e % (D / 4), at_row = 16 * rt + r;
       const float tr = most(at_row);
-      float total = 0.0f, by = 0.0f;
+      float total = 0.0f;
       float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < WAVES; ++i) {
         const float f = tops[i][at_row] == -INFINITY
                             ? 1.0f : __builtin_amdgcn_exp2f(tops[i][at_row] - tr);
         total = fmaf(totals[i][at_row], f, total);
-        if constexpr (ROUND) by = fmaf(divides[i][at_row], f, by);
         const float4 z =
             *reinterpret_cast<const float4*>(sums + (i * 16 + r) * D + ((chunk ^ r) << 2));
         y.x += z.x;
@@ -896,8 +852,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         y.z += z.z;
         y.w += z.w;
       }
-      if constexpr (!ROUND) by = total;
-      const float inv = by > 0.0f ? 1.0f / by : by;
+      const float inv = total > 0.0f ? 1.0f / total : total;
       const float l2 = total == 0.0f
                            ? -INFINITY
                            : (tr == -INFINITY ? 0.0f : tr) + __builtin_amdgcn_logf(total);
