@@ -61,7 +61,9 @@ dsa3d_status dsa3d_paged_read_mx(const dsa3d_paged_desc* desc, const dsa3d_mx_ca
                                  const int32_t* pages, const int32_t* kv_lens,
                                  const int32_t* cu_q, void* k, void* v, hipStream_t stream);
 
-/* Workspace bytes dsa3d_paged_forward_mx needs; may be 0. */
+/* Workspace bytes dsa3d_paged_forward_mx needs; may be 0.  With up to 64 requests it does not grow
+ * with the longest cache that the descriptor allows: 16 bytes per row and head of out, and float32
+ * results of the parts that long caches are read in, some hundreds of 16 to 128 rows each. */
 size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32_t bits);
 
 /* Attention of the new tokens over the pages: out [total_q][heads][head_dim] and, when not NULL,

@@ -39,6 +39,11 @@ __device__ inline void fill_rows(int* tab, int* bad, const PagedGeometry& g, con
   }
 }
 
+// What the join reads of a part: its log-sum-exp (base 2); kDone as the first part's where the
+// row needs no join.
+constexpr float kDone = INFINITY;
+__device__ inline float part_lse(float l2) { return l2 == INFINITY ? NAN : l2; }
+
 // ------------------------------------------------------------------------- many rows
 
 // Where the cache rows of the 64 keys from `base` on lie, in bytes, by the first wave.  A key
@@ -523,6 +528,7 @@ void set_plan(PagedGeometry& g) {
   g.tiles = seq_spread(g.KH, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
   g.blocks = seq_blocks(g.tiles, g.splits);
   g.target = 0;
+  g.room = 0;
 }
 
 size_t paged_workspace(const PagedGeometry& g) {

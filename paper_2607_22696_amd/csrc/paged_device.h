@@ -58,11 +58,6 @@ __device__ inline bool locate(const PagedGeometry& g, const int32_t* cu_q, const
   return !(s.only && split > 0);
 }
 
-// What the join reads of a part: its log-sum-exp (base 2); kDone as the first part's where the
-// row needs no join.
-constexpr float kDone = INFINITY;
-__device__ inline float part_lse(float l2) { return l2 == INFINITY ? NAN : l2; }
-
 struct Row {
   int i, head;    // token of the request, head
   bool ok;

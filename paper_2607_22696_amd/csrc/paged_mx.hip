@@ -225,8 +225,27 @@ __device__ inline void take_keys(Span1& s, int split, int len) {
 // What a workgroup works on.
 struct Deal {
   Span1 s;
-  int u, split, parts;  // key head; part of how many (all the workspace has where not dealt out)
+  int u, split, parts;  // key head; part of how many (the most there are where not dealt out)
+  int nth, tiles;       // where dealt out and in parts: this one's number among the key head's parts
+                        // with partial results; how far on the tile's next part is
 };
+
+// Partial results: [part][key head][row of the tile] of the parts that are dealt out, else [row of
+// out][part]; log-sum-exps (base 2) and D channels in float32.  For each row of out, where they
+// are: x the number of its tile's first part, y from there to the next, z how many (0: none, the
+// row is in out), w key head x rows per tile + row of the tile.
+struct Parts {
+  int4* of;
+  float *l, *o;
+};
+template <int ROWS>
+__device__ inline int64_t part_row(const PagedGeometry& g, const Deal& w, int r, int64_t out_at) {
+  return g.target > 0 ? ((int64_t)w.nth * g.KH + w.u) * ROWS + r : out_at * g.splits + w.split;
+}
+template <int ROWS>
+__device__ inline int4 parts_of(const Deal& w, int r) {
+  return make_int4(w.nth, w.tiles, w.parts, w.u * ROWS + r);
+}
 
 // Up to 64 requests' keys are divided by the sum of their lengths, and longer parts come first; a
 // request's tiles over the same part follow each other, the last (under a causal mask the longest)
@@ -243,6 +262,7 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
     if (!work_of_part(g, w, d.split)) return false;
     d.u = w.u;
     d.parts = g.splits;
+    d.nth = d.tiles = 0;
     return locate<ROWS>(g, cu_q, kv_lens, w.slot, d.split, s);
   }
   constexpr int STEP = 256;  // keys of the four waves' groups
@@ -259,7 +279,7 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
   int r;
   const int l = lane_of(index, h.tiles * parts, min((int)((int64_t)len * 4 / (most + 1)), 3), r);
   int tile = r;
-  d.split = 0;
+  d.split = d.nth = d.tiles = 0;
   d.parts = 1;
   if (l >= 0) {
     const int tiles = __builtin_amdgcn_readlane(h.tiles, l);
@@ -267,6 +287,12 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
     d.split = r / tiles;
     tile = tiles - 1 - (r - d.split * tiles);
     if (d.split >= d.parts) return false;  // only where offsets decrease
+    if (d.parts > 1) {
+      const int mine = parts > 1 ? h.tiles * parts : 0;
+      d.nth = __builtin_amdgcn_readlane(prefix_sum(mine) - mine, l) + r;
+      d.tiles = tiles;
+      if (d.nth < 0 || d.nth >= g.room) return false;  // likewise
+    }
   }
   if (!span_of<ROWS>(g, h, l, tile, s)) return false;
   s.only = d.parts == 1;
@@ -286,8 +312,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     const int32_t* __restrict__ pages, const int32_t* __restrict__ kv_lens,
                     const int32_t* __restrict__ cu_q, const float* __restrict__ table,
                     const int32_t* __restrict__ map, T* __restrict__ out,
-                    float* __restrict__ lse, float* __restrict__ part_o,
-                    float* __restrict__ part_l) {
+                    float* __restrict__ lse, Parts to) {
   constexpr int KT = 64, RB = D * BITS / 8, SB = D / 32;
   using Tl = Tile<uint16_t, D, KT>;
   using Frag = typename Type<T>::Frag;
@@ -300,7 +325,6 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   Deal w;
   if (!deal<kManyRows>(g, cu_q, kv_lens, w)) return;
   const Span1& s = w.s;
-  const int split = w.split;
   const int ntiles = s.k_hi > s.k_lo ? (s.k_hi - s.k_lo + KT - 1) / KT : 0;
   const int lane = threadIdx.x & 63, wave = wave_id(), hh = lane >> 5;
   const int rw = s.r0 + wave * 32;
@@ -465,16 +489,16 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 #pragma unroll
     for (int db = 0; db < DB; ++db) store_block(out + x.out_at * D, db, o[db], inv);
     if (hh == 0 && lse != nullptr) lse[x.out_at] = l2 * kLn2;
-    if (hh == 0 && g.splits > 1) part_l[x.out_at * g.splits] = kDone;
+    if (hh == 0 && g.splits > 1) to.of[x.out_at] = make_int4(0, 0, 0, 0);
   } else {
-    const int64_t at = x.out_at * g.splits + split;
+    const int r = wave * 32 + (lane & 31);
+    const int64_t at = part_row<kManyRows>(g, w, r, x.out_at);
     if (ltot != 0.0f) {  // the join skips the parts of a row without keys
 #pragma unroll
-      for (int db = 0; db < DB; ++db) store_block(part_o + at * D, db, o[db], inv);
+      for (int db = 0; db < DB; ++db) store_block(to.o + at * D, db, o[db], inv);
     }
-    if (hh == 0) part_l[at] = part_lse(l2);
-    if (hh == 0 && split == 0)  // parts that there are none of
-      for (int i = w.parts; i < g.splits; ++i) part_l[at + i] = -INFINITY;
+    if (hh == 0) to.l[at] = l2;
+    if (hh == 0 && w.split == 0) to.of[x.out_at] = parts_of<kManyRows>(w, r);
   }
 }
 
@@ -569,8 +593,7 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     const int32_t* __restrict__ pages, const int32_t* __restrict__ kv_lens,
                     const int32_t* __restrict__ cu_q, const float* __restrict__ table,
                     const int32_t* __restrict__ map, T* __restrict__ out,
-                    float* __restrict__ lse, float* __restrict__ part_o,
-                    float* __restrict__ part_l) {
+                    float* __restrict__ lse, Parts to) {
   constexpr int RB = D * BITS / 8, SB = D / 32, WAVES = kThreads / 64, ROWS = 16 * RT;
   // keys of a group: 32 where 64 would not leave enough registers (spilled ones are waited for
   // together with every load: 64 requests with 6 new tokens 181 us with 64, 135 with 32; with one
@@ -588,7 +611,6 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
   Deal w;
   if (!deal<ROWS>(g, cu_q, kv_lens, w)) return;
   const Span1& s = w.s;
-  const int split = w.split;
   const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4, col = lane & 15;
   // Queries first, so that waiting for them does not wait for keys.  A column without a row has the
   // request's first one, and is never stored.
@@ -799,13 +821,6 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 
   // The waves' sums join over a common maximum, 16 rows at a time.
   const int count = min(s.rows - s.r0, ROWS);
-  if (!s.only && split == 0 && w.parts < g.splits) {  // parts that there are none of
-    const int none = g.splits - w.parts;
-    for (int e = threadIdx.x; e < count * none; e += kThreads) {
-      const int r = e / none;
-      part_l[row_of(g, s, w.u, s.r0 + r).out_at * g.splits + w.parts + (e - r * none)] = -INFINITY;
-    }
-  }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const float total = sum_of(sum[rt]);
@@ -861,11 +876,12 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
       if (s.only) {
         store_4(out + z.out_at * D + chunk * 4, y);
         if (chunk == 0 && lse != nullptr) lse[z.out_at] = l2 * kLn2;
-        if (chunk == 0 && g.splits > 1) part_l[z.out_at * g.splits] = kDone;
+        if (chunk == 0 && g.splits > 1) to.of[z.out_at] = make_int4(0, 0, 0, 0);
       } else {
-        const int64_t at = z.out_at * g.splits + split;
-        if (total != 0.0f) store_4(part_o + at * D + chunk * 4, y);
-        if (chunk == 0) part_l[at] = part_lse(l2);
+        const int64_t at = part_row<ROWS>(g, w, at_row, z.out_at);
+        if (total != 0.0f) store_4(to.o + at * D + chunk * 4, y);
+        if (chunk == 0) to.l[at] = l2;
+        if (chunk == 0 && w.split == 0) to.of[z.out_at] = parts_of<ROWS>(w, at_row);
       }
     }
   }
@@ -880,11 +896,12 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
 // looks at R rows at once and goes on with those that were not finished: a launch with many rows
 // has few of them, and often none (chunks of 30 requests, 441,000 rows, none of them in parts:
 // 1,633 us with one each, 1,580 with 8; 52,000 rows, half of them in three parts: 13 us either way).
+//
+// dealt: rows of a part over all key heads, and `most` parts have room; 0: parts are not dealt out,
+// and every row has `most` of them.
 template <typename T, int D, int W, int AT_ONCE, int R>
-__global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int splits,
-                                                           const float* __restrict__ part_o,
-                                                           const float* __restrict__ part_l,
-                                                           T* __restrict__ out,
+__global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int dealt, int64_t most,
+                                                           Parts from, T* __restrict__ out,
                                                            float* __restrict__ lse) {
   constexpr int LANES = D / 4, SIDES = 64 / LANES, PER = kThreads / 64 / W;
   static_assert(W == 1 || R == 1, "several waves have one row");
@@ -894,12 +911,28 @@ __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int spl
   const int64_t row0 = ((int64_t)block_number() * PER + wave_id() / W) * R;
   if (row0 >= rows) return;  // a whole workgroup where W > 1
   const int side = lane / LANES, c = lane % LANES * 4;
-  const int64_t look = row0 + lane;
-  uint64_t left = __ballot(lane < R && look < rows && part_l[min(look, rows - 1) * splits] != kDone);
+  const int4 of = from.of[min(row0 + min(lane, R - 1), rows - 1)];
+  uint64_t left = __ballot(lane < R && row0 + lane < rows && of.z != 0);
   for (; left != 0; left &= left - 1) {
-    const int64_t row = row0 + __builtin_ctzll(left);
+    const int which = __builtin_ctzll(left);
+    const int64_t row = row0 + which;
+    int64_t first = row * most, step = 1;
+    int parts = (int)most;
+    if (dealt > 0) {
+      const int nth = __builtin_amdgcn_readlane(of.x, which);
+      const int next = __builtin_amdgcn_readlane(of.y, which);
+      const int in_part = __builtin_amdgcn_readlane(of.w, which);
+      parts = __builtin_amdgcn_readlane(of.z, which);
+      // Where offsets decrease a row may have been nobody's, and `of` anything.
+      if (nth < 0 || next < 0 || in_part < 0 || in_part >= dealt || parts < 0 ||
+          nth + (int64_t)(parts - 1) * next >= most)
+        continue;
+      first = (int64_t)nth * dealt + in_part;
+      step = (int64_t)next * dealt;
+    }
     // lane l has part l W + wave
-    const float mine = lane * W + wave < splits ? part_l[row * splits + lane * W + wave] : -INFINITY;
+    const float mine =
+        lane * W + wave < parts ? from.l[first + (lane * W + wave) * step] : -INFINITY;
     float top = mine;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -922,7 +955,7 @@ __global__ __launch_bounds__(kThreads) void mx_join_kernel(int64_t rows, int spl
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
         const int s = min(s0 + i * SIDES + side, count - 1) * W + wave;
-        x[i] = *reinterpret_cast<const float4*>(part_o + (row * splits + s) * D + c);
+        x[i] = *reinterpret_cast<const float4*>(from.o + (first + s * step) * D + c);
       }
 #pragma unroll
       for (int i = 0; i < AT_ONCE; ++i) {
@@ -1201,6 +1234,11 @@ Form form(const PagedGeometry& g, bool bf16, int bits, Form b64_8, Form b128_8, 
   return all[bf16][g.D == 128][bits == 8];
 }
 
+// Rows of partial results.
+int64_t part_rows(const PagedGeometry& g) {
+  return g.target > 0 ? g.room * g.KH * g.tile : (int64_t)g.splits * g.nq * g.H;
+}
+
 MxPages pages_of(const dsa3d_mx_cache& c) { return {c.k, c.v, c.k_scales, c.v_scales}; }
 
 template <typename T, int D, int BITS>
@@ -1209,9 +1247,12 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
                      const int32_t* map, T* out, float* lse, void* ws, hipStream_t s) {
   const bool bias = g.nb > 0;
   const int64_t rows = (int64_t)g.nq * g.H;
-  float* part_l = g.splits > 1 ? (float*)ws : nullptr;
-  float* part_o = g.splits > 1 ? (float*)((char*)ws + round_256((size_t)g.splits * rows * 4))
-                               : nullptr;
+  Parts p = {};
+  if (g.splits > 1) {
+    p.of = (int4*)ws;
+    p.l = (float*)((char*)ws + round_256((size_t)rows * sizeof(int4)));
+    p.o = (float*)((char*)p.l + round_256((size_t)part_rows(g) * 4));
+  }
   const void* fn = g.tile == 16   ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true, 1>
                                           : (const void*)&mx_keys_kernel<T, D, BITS, false, 1>)
                    : g.tile == 32 ? (bias ? (const void*)&mx_keys_kernel<T, D, BITS, true, 2>
@@ -1220,7 +1261,7 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
                                           : (const void*)&mx_rows_kernel<T, D, BITS, false>);
   hipError_t e = seq_launch(fn, g.blocks, kThreads,
                             bias ? (size_t)g.group * g.span * 4 : 0, s, g, q, c, pages, kv_lens,
-                            cu_q, table, map, out, lse, part_o, part_l);
+                            cu_q, table, map, out, lse, p);
   if (e == hipSuccess && g.splits > 1) {
     constexpr int waves = kThreads / 64, look = 8;
     const bool many = rows > 16384 && g.splits <= 64;  // one wave has no more parts
@@ -1229,8 +1270,8 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
     e = seq_launch(many   ? (const void*)&mx_join_kernel<T, D, 1, 2, look>
                    : wide ? (const void*)&mx_join_kernel<T, D, waves, 8, 1>
                           : (const void*)&mx_join_kernel<T, D, 1, 4, 1>,
-                   (rows + each - 1) / each, kThreads, 0, s, rows, g.splits,
-                   (const float*)part_o, (const float*)part_l, out, lse);
+                   (rows + each - 1) / each, kThreads, 0, s, rows,
+                   g.target > 0 ? g.KH * g.tile : 0, g.target > 0 ? g.room : g.splits, p, out, lse);
   }
   return e;
 }
@@ -1260,6 +1301,7 @@ void set_plan_mx(PagedGeometry& g, int bits) {
   g.splits = p.splits;
   g.part = p.part;
   g.target = p.target;
+  g.room = p.room;
   if (p.target > 0) {
     g.tiles = Spread{};
     g.blocks = g.KH * p.bound;
@@ -1267,6 +1309,12 @@ void set_plan_mx(PagedGeometry& g, int bits) {
     g.tiles = seq_spread(g.KH * g.splits, (int)((int64_t)g.nq * g.group / g.tile) + g.B + 1);
     g.blocks = seq_blocks(g.tiles, 1);
   }
+}
+
+size_t paged_mx_workspace(const PagedGeometry& g) {
+  if (g.splits <= 1) return 0;
+  const size_t n = part_rows(g);
+  return round_256((size_t)g.nq * g.H * sizeof(int4)) + round_256(n * 4) + n * g.D * 4;
 }
 
 hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,

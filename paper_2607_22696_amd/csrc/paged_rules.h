@@ -64,7 +64,8 @@ struct MxPlan {
   int tile;          // 16, 32 or 128 rows per workgroup
   int splits, part;  // most parts of a tile's keys, and least keys of a part
   int target;        // > 0: parts go by the lengths that the GPU sees, about this many per key head
-  int64_t bound;     // and are at most this many per key head
+  int64_t bound;     // and are at most this many per key head,
+  int64_t room;      // of which so many are of tiles that have several, and have partial results
 };
 
 // Rows per workgroup: 16 where the requests have no more on average, else as paged_plan.  Up to 64
@@ -77,13 +78,15 @@ struct MxPlan {
 //    rows, whose partial results cost most;
 //  - else three, of which the longest go first (single tokens of 64 requests, 32 / 8 heads, 8 bits:
 //    120 us in 512, 111 in 768, 113 in 1,280; 4 bits 74, 67, 67).
-// The workspace has room for all parts of all rows: for many rows at most 16, and 512 MiB unless
-// paged_plan had more.
+// For many rows at most 16, and 512 MiB of partial results if all rows had them, unless paged_plan
+// had more.  Partial results are numbered over the parts of tiles that have several: the workspace
+// does not grow with the longest cache that a call allows (64 requests with 8 new tokens each, 32 / 8
+// heads x 128, up to 131,072 tokens: 25 MiB, where room for each row's most parts was 782).
 inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv,
                             int head_dim) {
   const PagedPlan q = paged_plan(tokens, group, kv_heads, batch, max_kv);
   const int64_t rows = tokens * group;
-  MxPlan p = {rows <= (int64_t)16 * batch ? 16 : q.tile, q.splits, q.part, 0, 0};
+  MxPlan p = {rows <= (int64_t)16 * batch ? 16 : q.tile, q.splits, q.part, 0, 0, 0};
   if (batch > kDealt) return p;
   p.part = kLeastPartMx;
   const int64_t slots = rows / p.tile + batch + 1, all = slots * kv_heads;
@@ -101,6 +104,8 @@ inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, 
       1, std::min<int64_t>({max_kv / p.part, p.target + 1, most}));
   // sum of ceil(keys / part) <= target + one per tile; 8 for the rounding of the GPU's sum
   p.bound = std::min<int64_t>(slots * p.splits, slots + p.target + 8);
+  // ceil(keys / part) < 2 keys / part where it is 2 or more
+  p.room = p.splits > 1 ? std::min<int64_t>(p.bound, 2 * (int64_t)p.target + 8) : 0;
   return p;
 }
 

@@ -495,7 +495,7 @@ size_t dsa3d_paged_forward_mx_workspace_size(const dsa3d_paged_desc* desc, int32
   dsa3d::PagedGeometry g;
   PagedSizes s;
   if (check_mx(desc, bits, false, &g, &s) != DSA3D_OK) return 0;
-  return dsa3d::paged_workspace(g);
+  return dsa3d::paged_mx_workspace(g);
 }
 
 dsa3d_status dsa3d_paged_forward_mx(const dsa3d_paged_desc* desc, const void* q,
@@ -512,7 +512,7 @@ dsa3d_status dsa3d_paged_forward_mx(const dsa3d_paged_desc* desc, const void* q,
   if (!cu_q || !kv_lens || missing(q, s.q) || missing(out, s.out) || missing(pages, s.pages) ||
       cache_missing(*cache, m) || missing(bias_table, s.table) || missing(bias_map, s.map))
     return DSA3D_ERR_NULL_POINTER;
-  const uint64_t need = dsa3d::paged_workspace(g);
+  const uint64_t need = dsa3d::paged_mx_workspace(g);
   if (need > 0 && (workspace == nullptr || workspace_bytes < need)) return DSA3D_ERR_WORKSPACE;
   if (!aligned(q, 16) || !cache_aligned(*cache) || !aligned(out, 16) || !aligned(lse, 4) ||
       !aligned(cu_q, 4) || !aligned(kv_lens, 4) || !aligned(pages, 4) ||

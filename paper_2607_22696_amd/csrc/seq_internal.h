@@ -94,6 +94,7 @@ struct PagedGeometry {
   Spread tiles;
   int64_t blocks;  // workgroups of the launch
   int target;      // > 0: parts by the lengths that the GPU sees (paged_rules.h)
+  int64_t room;    // parts per key head with partial results, where target > 0
 };
 
 void set_plan(PagedGeometry& g);               // tile, splits, part, tiles and blocks
@@ -107,6 +108,7 @@ hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q
 hipError_t launch_paged_append(const PagedGeometry& g, bool bf16, const void* k, const void* v,
                                const int32_t* cu_q, const int32_t* kv_lens, const int32_t* pages,
                                void* k_pages, void* v_pages, hipStream_t stream);
+size_t paged_mx_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward_mx(const PagedGeometry& g, bool bf16, const void* q,
                                    const dsa3d_mx_cache& cache, const int32_t* pages,
                                    const int32_t* kv_lens, const int32_t* cu_q,
