@@ -5,9 +5,9 @@ import pytest
 import torch
 
 from oracle import sequence as ref
-from tests.mx_forms import PRECISE, plan_query
+from tests.mx_forms import FORMS, PRECISE, join_of, plan_query
 from tests.seq_util import Bounds
-from tests.test_paged_mx_rules import plans  # noqa: F401
+from tests.test_paged_mx_rules import parts_of, plans  # noqa: F401
 
 DIMS = (64, 128)
 
@@ -16,6 +16,21 @@ def test_precise_forms(plans):  # noqa: F811
     asked = [(tile, plan_query(c, D)) for tile, c in PRECISE.items() for D in DIMS]
     for (tile, _), plan in zip(asked, plans([q for _, q in asked])):
         assert plan[0] == tile and plan[1] == 1
+
+
+@pytest.mark.parametrize("D", DIMS)
+def test_forms(plans, D):  # noqa: F811
+    asked = [plan_query(c, D) for c, _ in FORMS.values()]
+    for (name, (c, form)), query, plan in zip(FORMS.items(), asked, plans(asked)):
+        rows = query[0] * c.get("H", 8)
+        assert (plan[0], plan[3] > 0, join_of(plan, rows)) == form, (name, plan)
+        if form[2] == "8 rows":
+            assert rows % 8 and 1 < plan[1] <= 64
+        if form[1]:  # some of its requests are in parts, and some are not
+            tiles = [-(-n * query[1] // plan[0]) for n in c["new"]]
+            parts = [p for p, _ in parts_of([m if n else 0 for n, m in zip(c["new"], c["held"])],
+                                            tiles, plan)]
+            assert min(parts) == 1 < max(parts), (name, parts)
 
 
 def bf16(x):
