@@ -78,6 +78,12 @@ struct MxPlan {
 //    rows, whose partial results cost most;
 //  - else three, of which the longest go first (single tokens of 64 requests, 32 / 8 heads, 8 bits:
 //    120 us in 512, 111 in 768, 113 in 1,280; 4 bits 74, 67, 67).
+//  The border by `all`, the workgroups without parts.  Single tokens, 32 / 8 heads x 128, 8 bits, us
+//  in 512 - all / 768 parts, n requests of 30,000 tokens and n of 3,000 to 60,000: n = 4 (all = 48)
+//  56/59 and 57/66, 6 (64) 74/76 and 81/87, 7 (72) 87/99 and 91/104, 8 (88) 97/97 and 104/110, 12 (128)
+//  157/138 and 159/160, 16 (168) 206/181 and 219/207.  The uneven ones of 7 and of 16 requests in
+//  float32 95/104, 220/209, in 4 bits 56/63, 122/117, at 64 channels 51/56, 112/111, with 6 new
+//  tokens each 99/111, 260/223.
 // For many rows at most 16, and 512 MiB of partial results if all rows had them, unless paged_plan
 // had more.  Partial results are numbered over the parts of tiles that have several: the workspace
 // does not grow with the longest cache that a call allows (64 requests with 8 new tokens each, 32 / 8
@@ -92,7 +98,7 @@ inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, 
   const int64_t slots = rows / p.tile + batch + 1, all = slots * kv_heads;
   const bool few = q.tile == kFewRows;
   p.target = (int)std::max<int64_t>(
-      1, (!few ? 512 : all <= 64 ? 512 - all : 768) / kv_heads);
+      1, (!few ? 512 : all <= 96 ? 512 - all : 768) / kv_heads);
   const int64_t room = (int64_t)512 << 20, each = std::max<int64_t>(1, rows) * kv_heads * head_dim * 4;
   int64_t most =
       few ? kMostPartsMx : std::max<int64_t>(q.splits, std::min<int64_t>(16, room / each));

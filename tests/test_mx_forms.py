@@ -62,3 +62,10 @@ def test_the_bound_tells_alphas_roundings_apart():
 @pytest.mark.parametrize("tile", PRECISE)
 def test_every_request_has_few_keys(tile):
     assert max(PRECISE[tile]["held"]) <= 70
+
+
+def test_few_requests_have_parts_for_one_round_of_workgroups(plans):  # noqa: F811
+    """Up to 96 workgroups without parts: two rounds' worth of three per compute unit is slower."""
+    for batch, target in ((1, 62), (4, 58), (6, 56), (7, 55), (8, 53), (12, 96), (16, 96), (64, 96)):
+        plan = plans([(batch, 4, 8, batch, 30000, 128)])[0]
+        assert plan[0] == 16 and plan[3] == target, (batch, plan)
