@@ -55,8 +55,9 @@ dsa3d_status dsa3d_paged_append_mx(const dsa3d_paged_desc* desc, const void* k, 
                                    hipStream_t stream);
 
 /* Reads the newest tokens back as rows k, v [total_q][kv_heads][head_dim] (k_stride, v_stride
- * apart; the one's rows must not lie between the other's): cu_q[b + 1] - cu_q[b] tokens of request b, the last of its kv_lens[b].  Tokens without a
- * place and rows behind the last request read as 0.  max_kv is not used. */
+ * apart; the one's rows must not lie between the other's, or DSA3D_ERR_ALIAS): cu_q[b + 1] - cu_q[b]
+ * tokens of request b, the last of its kv_lens[b].  Tokens without a place and rows behind the last
+ * request read as 0.  max_kv is not used. */
 dsa3d_status dsa3d_paged_read_mx(const dsa3d_paged_desc* desc, const dsa3d_mx_cache* cache,
                                  const int32_t* pages, const int32_t* kv_lens,
                                  const int32_t* cu_q, void* k, void* v, hipStream_t stream);

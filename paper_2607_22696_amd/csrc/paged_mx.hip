@@ -75,8 +75,8 @@ struct Quarter {
 
 // Alpha as an operand: 16 bits of it as two bf16 numbers, or a float32's three parts.  (One bf16
 // number of it, the results divided by the sum of the rounded, takes less where products are the
-// time, chunks of 512, 801 and 300 tokens beside three single ones 206 us instead of 257, and 64
-// requests with 6 new tokens in 4 bits 86 instead of 93; but outputs are then off by 0.0020 to
+// time, chunks of 512, 801 and 300 tokens beside three single ones 203 us instead of 252, and 64
+// requests with 6 new tokens in 4 bits 86 instead of 91; but outputs are then off by 0.0020 to
 // 0.0021 of their size instead of the 0.0016 that their own rounding makes.)
 struct Two {
   bf16x8_t h, l;
@@ -140,9 +140,8 @@ __device__ inline void fence_wave() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// The workgroup's key head, tile and part.  A part of a head's keys stays on one XCD, whose L2 then
-// serves it to the tiles of a request, and the parts lie on all of them (with whole heads on an XCD
-// four requests of 31,000 to 120,000 tokens, 16 / 2 heads, in 4 bits waited for one: 45 us, 30 so).
+// The workgroup's key head, tile and part where parts are not dealt out.  A part of a head's keys
+// stays on one XCD, whose L2 then serves it to the tiles of a request.
 __device__ inline bool work_of_part(const PagedGeometry& g, Work& w, int& split) {
   if (!work_of(g.tiles, 1, w)) return false;
   split = w.u / g.KH;
@@ -226,8 +225,8 @@ __device__ inline void take_keys(Span1& s, int split, int len) {
 struct Deal {
   Span1 s;
   int u, split, parts;  // key head; part of how many (the most there are where not dealt out)
-  int nth, tiles;       // where dealt out and in parts: this one's number among the key head's parts
-                        // with partial results; how far on the tile's next part is
+  int nth, tiles;       // where dealt out and in parts: this one's number among the key head's
+                        // parts with partial results; how far on the tile's next part is
 };
 
 // Partial results: [part][key head][row of the tile] of the parts that are dealt out, else [row of
@@ -249,10 +248,20 @@ __device__ inline int4 parts_of(const Deal& w, int r) {
 
 // Up to 64 requests' keys are divided by the sum of their lengths, and longer parts come first; a
 // request's tiles over the same part follow each other, the last (under a causal mask the longest)
-// first.  More requests as they lie, in parts that the host chose.  (A chunk of 400 of 30,000
-// tokens before 40 of 100 of 700, 32 / 8 heads: 784 us as they lie in parts chosen without the
-// lengths, 712 longest first, 318 divided; chunks of 512, 801 and 300 of 16,000, 801 and 5,000
-// tokens beside three single ones 235 and 215.)
+// first.  (A chunk of 400 of 30,000 tokens before 40 of 100 of 700, 32 / 8 heads, alpha in one bf16
+// number: 784 us as they lie in parts chosen without the lengths, 712 longest first, 318 divided;
+// chunks of 512, 801 and 300 of 16,000, 801 and 5,000 tokens beside three single ones 235 and 215.)
+// More requests, of which a wave does not hold one a lane, come as they lie, in parts that the host
+// chose: near what reading takes where they are alike (single tokens, 32 / 8 heads x 128, 128
+// requests of 200 to 8,000 tokens: 219 us), but a long one among short ones is waited for (120,000
+// tokens beside 63 requests of 200 to 2,000: 83 us, divided; beside 127: 532).
+//
+// Workgroups go round the XCDs by number.  Where the key heads are a multiple of 8 a head stays on
+// one XCD, whose L2 serves a part to all tiles that read it.  Fewer lie on several, each of which
+// reads the part (chunks as above with 8, 4, 2, 1 key heads and as many times 4 heads: 2.1, 2.5,
+// 2.8, 3.6 times their products' time at the rate of large ones); whole heads on an XCD would leave
+// six of them idle for 2 (four requests of 31,000 to 120,000 tokens, 16 / 2 heads, 4 bits: 45 us so,
+// 30 spread out).
 template <int ROWS>
 __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const int32_t* kv_lens,
                             Deal& d) {
@@ -304,7 +313,8 @@ __device__ inline bool deal(const PagedGeometry& g, const int32_t* cu_q, const i
 
 // 128 rows per workgroup, 32 per wave, tiles of 64 keys in LDS as bf16, two of them: a tile's
 // elements are loaded two tiles ahead, converted once for all four waves, and the products of the
-// next 32 keys run beside the softmax of these.
+// next 32 keys run beside the softmax of these.  At 128 channels bf16 spills 32 to 47 registers, all of
+// them around the last one or two tiles: the loop has none.
 template <typename T, int D, int BITS, bool BIAS>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(sizeof(T) == 2 ? 2 : 1, 2)))
@@ -454,7 +464,7 @@ void mx_rows_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
         if (MORE && b == NB - 1) __syncthreads();  // the next tile is in LDS
         if constexpr (LIVE) {
           // ahead of the other workgroup's wave on this SIMD while the matrix cores have work: chunks
-          // 228 and 224 us, a prompt of 4,096 tokens over 4 bits 175 and 164
+          // 251 and 245 us, at 64 channels 198 and 163, a prompt of 4,096 tokens 225 and 208
           __builtin_amdgcn_s_setprio(1);
           if constexpr (MORE) next = b + 1 < NB ? products(kc, b + 1) : products(kn, 0);
           else if (b + 1 < NB) next = products(kc, b + 1);
@@ -596,8 +606,8 @@ void mx_keys_kernel(PagedGeometry g, const T* __restrict__ q, MxPages c,
                     float* __restrict__ lse, Parts to) {
   constexpr int RB = D * BITS / 8, SB = D / 32, WAVES = kThreads / 64, ROWS = 16 * RT;
   // keys of a group: 32 where 64 would not leave enough registers (spilled ones are waited for
-  // together with every load: 64 requests with 6 new tokens 181 us with 64, 135 with 32; with one
-  // new token in float32 129 and 117)
+  // together with every load: 64 requests with 6 new tokens 168 us with 64, 125 with 32; with one
+  // new token in float32 127 and 115)
   constexpr int KB = D == 128 && BITS == 8 && (RT == 2 || sizeof(T) == 4) ? 32 : 64, NI = KB / 16;
   constexpr uint64_t kAll = ~0ull >> (64 - KB);
   using Frag = typename Type<T>::Frag;
@@ -1265,7 +1275,11 @@ hipError_t forward_d(const PagedGeometry& g, const T* q, const MxPages& c, const
   if (e == hipSuccess && g.splits > 1) {
     constexpr int waves = kThreads / 64, look = 8;
     const bool many = rows > 16384 && g.splits <= 64;  // one wave has no more parts
-    const bool wide = !many && g.splits > 16;  // single tokens of 64 requests: 112.6 us, 111 so
+    // One wave is better for few parts, four from 9 or so on: single tokens of n requests of 30,000
+    // tokens, 32 / 8 heads x 128, us with one / four, n = 64 (2 parts) 672.7/675.8, 16 (6)
+    // 180.6/181.3, 8 (12) 97.3/96.2, 4 (14) 57.2/56.5, 2 (29) 29.8/28.6, 1 (59) 25.4/24.0.  The host
+    // knows only how many there may be: 16 leaves single tokens of 64 requests of up to 8,000 to one.
+    const bool wide = !many && g.splits > 16;
     const int each = many ? waves * look : wide ? 1 : waves;
     e = seq_launch(many   ? (const void*)&mx_join_kernel<T, D, 1, 2, look>
                    : wide ? (const void*)&mx_join_kernel<T, D, waves, 8, 1>
@@ -1295,7 +1309,7 @@ hipError_t forward_t(const PagedGeometry& g, const void* q, const dsa3d_mx_cache
 
 }  // namespace
 
-void set_plan_mx(PagedGeometry& g, int bits) {
+void set_plan_mx(PagedGeometry& g) {
   const MxPlan p = paged_mx_plan(g.nq, g.group, g.KH, g.B, g.max_kv, g.D);
   g.tile = p.tile;
   g.splits = p.splits;

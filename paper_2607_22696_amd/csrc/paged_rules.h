@@ -69,25 +69,26 @@ struct MxPlan {
 };
 
 // Rows per workgroup: 16 where the requests have no more on average, else as paged_plan.  Up to 64
-// requests' keys are divided on the GPU, by all their lengths (more requests fill the card
-// without), into parts of at least 512 keys (256: single tokens of 64 requests 111 and 112 us,
-// drafts of 5 tokens of 16 20.0 and 22.3, 12 biased ones 21.0 and 22.0), as many as there are
-// workgroups at a time:
+// requests' keys are divided on the GPU, by all their lengths (more requests as by paged_plan, which
+// fills the card where they are alike: see deal in paged_mx.hip), into parts of at least 512 keys
+// (256: single tokens of 64 requests 111 and 112 us, drafts of 5 tokens of 16 20.0 and 22.3, 12
+// biased ones 21.0 and 22.0), as many as there are workgroups at a time:
 //  - two per compute unit, where few requests have parts of one length (four requests of 31,000 to
 //    120,000 tokens, 16 / 2 heads, 4 bits: 24 us in 512 parts, 28 in 384, 29 in 768) and for many
 //    rows, whose partial results cost most;
 //  - else three, of which the longest go first (single tokens of 64 requests, 32 / 8 heads, 8 bits:
 //    120 us in 512, 111 in 768, 113 in 1,280; 4 bits 74, 67, 67).
-//  The border by `all`, the workgroups without parts.  Single tokens, 32 / 8 heads x 128, 8 bits, us
-//  in 512 - all / 768 parts, n requests of 30,000 tokens and n of 3,000 to 60,000: n = 4 (all = 48)
-//  56/59 and 57/66, 6 (64) 74/76 and 81/87, 7 (72) 87/99 and 91/104, 8 (88) 97/97 and 104/110, 12 (128)
-//  157/138 and 159/160, 16 (168) 206/181 and 219/207.  The uneven ones of 7 and of 16 requests in
-//  float32 95/104, 220/209, in 4 bits 56/63, 122/117, at 64 channels 51/56, 112/111, with 6 new
-//  tokens each 99/111, 260/223.
-// For many rows at most 16, and 512 MiB of partial results if all rows had them, unless paged_plan
-// had more.  Partial results are numbered over the parts of tiles that have several: the workspace
-// does not grow with the longest cache that a call allows (64 requests with 8 new tokens each, 32 / 8
-// heads x 128, up to 131,072 tokens: 25 MiB, where room for each row's most parts was 782).
+// The border goes by `all`, the workgroups without parts.  Single tokens of n requests, 32 / 8 heads
+// x 128, 8 bits, us in 512 - all / 768 parts, of 30,000 tokens each and of 3,000 to 60,000: n = 4
+// (all = 48) 56/59 and 57/66, 6 (64) 74/76 and 81/87, 7 (72) 87/99 and 91/104, 8 (88) 97/97 and
+// 104/110, 12 (128) 157/138 and 159/160, 16 (168) 206/181 and 219/207.  The uneven ones of 7 and of
+// 16 in float32 95/104 and 220/209, in 4 bits 56/63 and 122/117, at 64 channels 51/56 and 112/111,
+// with 6 new tokens each 99/111 and 260/223.
+//
+// For many rows at most 16 parts, and 512 MiB of partial results if all rows had them, unless
+// paged_plan had more.  Partial results are numbered over the parts of tiles that have several: the
+// workspace does not grow with the longest cache that a call allows (64 requests with 8 new tokens
+// each, 32 / 8 heads x 128, up to 131,072 tokens: 25 MiB; room for each row's most parts was 782).
 inline MxPlan paged_mx_plan(int64_t tokens, int group, int kv_heads, int batch, int max_kv,
                             int head_dim) {
   const PagedPlan q = paged_plan(tokens, group, kv_heads, batch, max_kv);

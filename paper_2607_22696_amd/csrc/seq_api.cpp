@@ -248,9 +248,9 @@ struct PagedSizes {
   uint64_t q, out, pages, cache, cu, lens, lse, table, map;
 };
 
-// `bits`: of the cache, 0 where it has the descriptor's type.
+// `mx`: the cache is one of 8 or 4 bits, not of the descriptor's type.
 dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeometry* g,
-                         PagedSizes* s, int bits = 0) {
+                         PagedSizes* s, bool mx = false) {
   if (d == nullptr) return DSA3D_ERR_NULL_POINTER;
   if (d->batch < 1 || d->batch >= (1 << 24) || d->total_q < 0 || d->num_pages < 0 ||
       d->page_size < 1 || d->max_pages < 0 || d->max_kv < 0 ||
@@ -299,8 +299,8 @@ dsa3d_status check_paged(const dsa3d_paged_desc* d, bool append, dsa3d::PagedGeo
     return DSA3D_ERR_UNSUPPORTED;
   g->scale = d->scale != 0.0f ? d->scale : 1.0f / std::sqrt((float)d->head_dim);
   g->scale_log2 = g->scale * kLog2e;
-  if (bits == 0) dsa3d::set_plan(*g);
-  else dsa3d::set_plan_mx(*g, bits);
+  if (mx) dsa3d::set_plan_mx(*g);
+  else dsa3d::set_plan(*g);
   if (!append && g->blocks > dsa3d::kMostBlocks)
     return DSA3D_ERR_INVALID_SHAPE;
   s->q = strided_bytes(d->total_q, g->qs, qrow, s->item);
@@ -403,9 +403,8 @@ struct MxSizes {  // the cache's bytes, instead of PagedSizes::cache
 
 dsa3d_status check_mx(const dsa3d_paged_desc* d, int32_t bits, bool rows,
                       dsa3d::PagedGeometry* g, PagedSizes* s) {
-  const bool known = bits == 8 || bits == 4;
-  const dsa3d_status st = check_paged(d, rows, g, s, known ? bits : 8);
-  return st == DSA3D_OK && !known ? DSA3D_ERR_UNSUPPORTED : st;
+  const dsa3d_status st = check_paged(d, rows, g, s, true);
+  return st == DSA3D_OK && bits != 8 && bits != 4 ? DSA3D_ERR_UNSUPPORTED : st;
 }
 
 dsa3d_status check_cache(const dsa3d_paged_desc* d, const dsa3d_mx_cache* c, bool rows,

@@ -97,8 +97,8 @@ struct PagedGeometry {
   int64_t room;    // parts per key head with partial results, where target > 0
 };
 
-void set_plan(PagedGeometry& g);               // tile, splits, part, tiles and blocks
-void set_plan_mx(PagedGeometry& g, int bits);  // and target, for a cache of 8 or 4 bits
+void set_plan(PagedGeometry& g);     // tile, splits, part, tiles and blocks
+void set_plan_mx(PagedGeometry& g);  // and target and room, for a cache of 8 or 4 bits
 size_t paged_workspace(const PagedGeometry& g);
 hipError_t launch_paged_forward(const PagedGeometry& g, bool bf16, const void* q,
                                 const void* k_pages, const void* v_pages, const int32_t* pages,

@@ -738,7 +738,8 @@ def paged_read_mx(cache, pages, kv_lens, cu_q, rows, dtype=torch.bfloat16, k=Non
     """Reads tokens of the cache back as packed rows [rows, kv_heads, head_dim], exactly: of request
     b the last cu_q[b + 1] - cu_q[b] of its kv_lens[b] (a smaller kv_lens reads earlier ones).
     Tokens without a page and rows behind the last request read as 0.  Returns (k, v), new tensors
-    of `dtype` (bf16 or float32) or the ones given."""
+    of `dtype` (bf16 or float32) or the ones given, whose rows may lie apart but not the one's
+    between the other's."""
     chk = _Checks("paged_read_mx")
     if dtype not in _IO_DTYPES:
         chk.problems.append(f"dtype: unsupported {dtype}")
