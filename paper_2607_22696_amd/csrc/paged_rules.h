@@ -81,9 +81,9 @@ struct MxPlan {
 // The border goes by `all`, the workgroups without parts.  Single tokens of n requests, 32 / 8 heads
 // x 128, 8 bits, us in 512 - all / 768 parts, of 30,000 tokens each and of 3,000 to 60,000: n = 4
 // (all = 48) 56/59 and 57/66, 6 (64) 74/76 and 81/87, 7 (72) 87/99 and 91/104, 8 (88) 97/97 and
-// 104/110, 12 (128) 157/138 and 159/160, 16 (168) 206/181 and 219/207.  The uneven ones of 7 and of
-// 16 in float32 95/104 and 220/209, in 4 bits 56/63 and 122/117, at 64 channels 51/56 and 112/111,
-// with 6 new tokens each 99/111 and 260/223.
+// 104/110, 12 (128) 157/138 and 159/160, 16 (168) 206/181 and 219/207; 64 with 2 / 1 heads (73) 98/96
+// and 102/109.  The uneven ones of 7 and of 16 in float32 95/104 and 220/209, in 4 bits 56/63 and
+// 122/117, at 64 channels 51/56 and 112/111, with 6 new tokens each 99/111 and 260/223.
 //
 // For many rows at most 16 parts, and 512 MiB of partial results if all rows had them, unless
 // paged_plan had more.  Partial results are numbered over the parts of tiles that have several: the

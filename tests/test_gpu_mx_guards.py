@@ -126,3 +126,55 @@ def test_lengths_beyond_the_page_table_and_below_zero(new, dtype, bits):
     o, l, out_bound, lse_bound = c.want()
     near("out", out, o, out_bound)
     near("lse", lse, l, lse_bound)
+
+
+@pytest.mark.parametrize("name", ("single_tokens", "drafts", "chunks"))
+@pytest.mark.parametrize("dtype,D", KINDS)
+def test_lengths_that_change_after_the_capture(name, dtype, D):
+    """The room is that of every length that the page table allows: a graph captured at short
+    lengths and replayed at long ones stays within it and gives the eager call's bits."""
+    new, most = {"single_tokens": ([1, 1, 1], [6000, 900, 2600]),
+                 "drafts": ([6, 0, 7], [3000, 50, 2100]),
+                 "chunks": ([100, 3, 40], [4000, 700, 2600])}[name]
+    c = Case(530 + len(name), new, most, D=D, dtype=dtype, columns=300)
+    pages, cu = ints(c.pages), ints(ref.starts(new))
+    short = [n + 3 for n in new]
+    held = ints(short)
+    guard = Guards()
+    out, lse = guard(c.q.shape, c.q.dtype), guard(c.q.shape[:2], torch.float32)
+    room = guard((need_of(c, c.pages),), torch.uint8)
+
+    def call(**kw):
+        return dsa.paged_forward_mx(c.q, c.cache, pages, held, cu, need_lse=True, **kw)
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call(out=out, lse=lse, workspace=room)
+    for lengths in (most, short, [m // 2 for m in most], most):
+        held.copy_(ints(lengths))
+        want = [t.clone() for t in call()]
+        torch.cuda.synchronize()
+        graph.replay()
+        guard.check()
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
+@pytest.mark.parametrize("new,H", (([1] * 64, 2), ([9] * 64, 2), ([1] * 63 + [90], 4)))
+@pytest.mark.parametrize("dtype,bits", (("bf16", 4), ("f32", 8)))
+def test_64_requests_in_parts(new, H, dtype, bits):
+    """As many parts as are dealt out: each request has 8,192 tokens that stand in the same 16 pages,
+    32 times each, so that attention is that over 256 tokens and lse larger by log 32."""
+    c = Case(540 + len(new), new, [256] + [1] * 63, H=H, KH=1, bits=bits, dtype=dtype, causal=False)
+    c.pages = np.tile(c.pages[0, :16], (64, 1))
+    c.held = [256] * 64
+    o, l, out_bound, lse_bound = c.want()
+    pages = np.tile(c.pages, (1, 32))
+    guard = Guards()
+    c.held, more = [8192] * 64, 8192 * 2.0 ** -23  # the terms of the sums
+    out, lse = guarded(c, guard, pages, c.held, ref.starts(new))
+    guard.check()
+    l += np.log(32)
+    near("out", out, o, out_bound + 2 * more * np.abs(c.v64[c.pages[0]]).max())
+    near("lse", lse, l, lse_bound + 2 * more + np.abs(l) * 4 * 2.0 ** -23)
